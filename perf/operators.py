@@ -235,9 +235,10 @@ def run(state):
     op = case["op"]
     if op in ("attend", "append"):
         if own:
-            from paper_2601_10155_b200.binding import Q8Cache
-            lk = _context(case["n_q"], case["n_kv"], case["d"])
-            cache = Q8Cache(*state["cache"])
+            if "handle" not in state:                      # a program makes it with its cache and keeps it
+                from paper_2601_10155_b200.binding import Q8Cache
+                state["handle"] = Q8Cache(*state["cache"])
+            lk, cache = _context(case["n_q"], case["n_kv"], case["d"]), state["handle"]
             if op == "attend":
                 return lk.lookat_attend_q8(cache, state["q"], state["tables"], state["seq_lens"], out_fp16=case["fp16"])
             lk.lookat_q8_append(cache, state["k_new"], state["v_new"], state["tables"], state["seq_lens"], state["n_new"])
@@ -246,15 +247,16 @@ def run(state):
     torch._foreach_copy_(state["parts"], state["saved"])
     tables, seq_lens, refs, free_list, n_free = state["parts"]
     if own:
-        from paper_2601_10155_b200.binding import PageState
-        lk = _context(12, 12, 64)
-        pages = PageState(tables, seq_lens, refs, free_list, n_free, case["page"])
+        if "handle" not in state:
+            from paper_2601_10155_b200.binding import PagePools, PageState
+            state["handle"] = PageState(tables, seq_lens, refs, free_list, n_free, case["page"]), PagePools(state.get("pools", []))
+        lk, (pages, pools) = _context(12, 12, 64), state["handle"]
         if op == "extend":
-            lk.lookat_pages_extend(pages, state["n_new"], state["pools"])
+            lk.lookat_pages_extend(pages, state["n_new"], pools)
         elif op == "fork":
             lk.lookat_pages_fork(pages, state["parents"])
         else:
-            lk.lookat_pages_compact(pages, state["pools"])
+            lk.lookat_pages_compact(pages, pools)
     else:
         {"extend": _plain_extend, "fork": _plain_fork, "compact": _plain_compact}[op](state, tables, seq_lens, refs, free_list, n_free)
     return [tables, seq_lens, refs, free_list, n_free] + (state["pools"] if "pools" in state else [])
