@@ -9,7 +9,7 @@ context is created and its absence is an error, never a fallback.
 
 
 def __getattr__(name):
-    if name in ("Lookat", "LookatError", "load_library"):
+    if name in ("Lookat", "LookatError", "Q8Cache", "PageState", "PagePools", "load_library"):
         from . import binding
         return getattr(binding, name)
     raise AttributeError(name)

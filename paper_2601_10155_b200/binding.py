@@ -27,6 +27,8 @@ EXPORTS = [
     "lookat_gpt2_decode", "lookat_gpt2_layer_state", "lookat_gpt2_position", "lookat_gpt2_kernel_launches",
     "lookat_gpt2_set_profile", "lookat_gpt2_profile",
     "lookat_linear", "lookat_linear_qkv", "lookat_layernorm", "lookat_embed", "lookat_causal_attention", "lookat_argmax",
+    # include/lookat_q8.h
+    "lookat_q8_append", "lookat_attend_q8", "lookat_pages_extend", "lookat_pages_fork", "lookat_pages_compact",
 ]
 
 STATUS = {0: "LOOKAT_OK", 1: "LOOKAT_ERR_INVALID_ARG", 2: "LOOKAT_ERR_UNSUPPORTED",
@@ -55,6 +57,20 @@ LAYER_FIELDS = ("ln1_g", "ln1_b", "w_qkv", "b_qkv", "w_o", "b_o", "ln2_g", "ln2_
 
 class lookat_gpt2_layer(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in LAYER_FIELDS]
+
+
+class lookat_q8_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("k_amax", ctypes.c_void_p), ("v", ctypes.c_void_p), ("v_amax", ctypes.c_void_p),
+                ("n_pages", ctypes.c_int32), ("page", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+
+class lookat_page_state(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("tables", "seq_lens", "refs", "free_list", "n_free")] + \
+               [(n, ctypes.c_int32) for n in ("B", "max_pages", "n_pages", "page")]
+
+
+class lookat_page_pool(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("page_bytes", ctypes.c_int64)]
 
 
 _libs = {}
@@ -144,6 +160,17 @@ def load_library(debug: bool = False) -> ctypes.CDLL:
     lib.lookat_causal_attention.restype = i32
     lib.lookat_argmax.argtypes = [vp, vp, i32, i32, vp]
     lib.lookat_argmax.restype = i32
+    # the 8-bit paged cache (include/lookat_q8.h)
+    lib.lookat_q8_append.argtypes = [vp, ctypes.POINTER(lookat_q8_cache), vp, vp, i32, i32, vp, i32, vp, vp]
+    lib.lookat_q8_append.restype = i32
+    lib.lookat_attend_q8.argtypes = [vp, ctypes.POINTER(lookat_q8_cache), vp, i32, i32, vp, i32, vp, vp, i32]
+    lib.lookat_attend_q8.restype = i32
+    lib.lookat_pages_extend.argtypes = [vp, ctypes.POINTER(lookat_page_state), vp, ctypes.POINTER(lookat_page_pool), i32]
+    lib.lookat_pages_extend.restype = i32
+    lib.lookat_pages_fork.argtypes = [vp, ctypes.POINTER(lookat_page_state), vp]
+    lib.lookat_pages_fork.restype = i32
+    lib.lookat_pages_compact.argtypes = [vp, ctypes.POINTER(lookat_page_state), ctypes.POINTER(lookat_page_pool), i32, vp]
+    lib.lookat_pages_compact.restype = i32
     lib.lookat_is_debug_build.argtypes = []
     lib.lookat_is_debug_build.restype = i32
     _libs[debug] = lib
@@ -170,6 +197,85 @@ def _host(t, dtype, name, shape):
     if t.dtype != dtype or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must be contiguous {dtype} of shape {tuple(shape)}")
     return t.data_ptr()
+
+
+def _on(t, dtype, name, device, shape=None):
+    """_dev, and the tensor lies on the context's device."""
+    p = _dev(t, dtype, name, shape)
+    if t is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the context on {device}")
+    return p
+
+
+class Q8Cache:
+    """The arrays of an 8-bit paged cache (include/lookat_q8.h), checked once: k [n_pages][H_kv][page][d_k] and v
+    [n_pages][H_kv][page][d_v], int8 or float8_e4m3fn, k_amax and v_amax fp32 [n_pages][H_kv]."""
+
+    def __init__(self, k, k_amax, v, v_amax):
+        if not isinstance(k, torch.Tensor) or k.dtype not in (torch.int8, torch.float8_e4m3fn):
+            raise TypeError("k must be an int8 or float8_e4m3fn tensor")
+        if k.dim() != 4:
+            raise ValueError(f"k must have shape [n_pages][H_kv][page][d_k], got {tuple(k.shape)}")
+        n_pages, H, page, d_k = k.shape
+        if v.dim() != 4:
+            raise ValueError(f"v must have shape [n_pages][H_kv][page][d_v], got {tuple(v.shape)}")
+        self.k, self.k_amax, self.v, self.v_amax = k, k_amax, v, v_amax
+        self.n_pages, self.n_kv_heads, self.page, self.d_k, self.d_v = n_pages, H, page, d_k, v.shape[3]
+        self.device = k.device
+        self.c = lookat_q8_cache(_dev(k, k.dtype, "k"), _on(k_amax, torch.float32, "k_amax", k.device, (n_pages, H)),
+                                 _on(v, k.dtype, "v", k.device, (n_pages, H, page, v.shape[3])),
+                                 _on(v_amax, torch.float32, "v_amax", k.device, (n_pages, H)),
+                                 n_pages, page, 0 if k.dtype == torch.int8 else 1)
+
+    @classmethod
+    def empty(cls, n_pages, n_kv_heads, page, d_k, d_v, dtype=torch.int8, device="cuda"):
+        """A cache of unwritten pages."""
+        return cls(torch.zeros((n_pages, n_kv_heads, page, d_k), dtype=torch.uint8, device=device).view(dtype),
+                   torch.zeros((n_pages, n_kv_heads), dtype=torch.float32, device=device),
+                   torch.zeros((n_pages, n_kv_heads, page, d_v), dtype=torch.uint8, device=device).view(dtype),
+                   torch.zeros((n_pages, n_kv_heads), dtype=torch.float32, device=device))
+
+    def pools(self):
+        """The arrays that are kept by pages (for lookat_pages_extend and lookat_pages_compact)."""
+        return [self.k, self.k_amax, self.v, self.v_amax]
+
+
+class PageState:
+    """The pages of a batch (include/lookat_q8.h): int32 tensors tables [B][max_pages], seq_lens [B], refs [n_pages],
+    free_list [n_pages], n_free [1]."""
+
+    def __init__(self, tables, seq_lens, refs, free_list, n_free, page):
+        if tables.dim() != 2 or refs.dim() != 1:
+            raise ValueError("tables must have shape [B][max_pages], refs [n_pages]")
+        B, max_pages = tables.shape
+        n_pages, i32, dev = refs.shape[0], torch.int32, tables.device
+        self.tables, self.seq_lens, self.refs, self.free_list, self.n_free = tables, seq_lens, refs, free_list, n_free
+        self.B, self.max_pages, self.n_pages, self.page, self.device = B, max_pages, n_pages, page, dev
+        self.c = lookat_page_state(_dev(tables, i32, "tables"), _on(seq_lens, i32, "seq_lens", dev, (B,)), _on(refs, i32, "refs", dev),
+                                   _on(free_list, i32, "free_list", dev, (n_pages,)), _on(n_free, i32, "n_free", dev, (1,)),
+                                   B, max_pages, n_pages, page)
+
+    @classmethod
+    def empty(cls, B, max_pages, n_pages, page, device="cuda"):
+        """B empty rows over n_pages free pages (page 0 on top of the free list)."""
+        z = lambda *s: torch.zeros(s, dtype=torch.int32, device=device)  # noqa: E731
+        return cls(torch.full((B, max_pages), -1, dtype=torch.int32, device=device), z(B), z(n_pages),
+                   torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device),
+                   torch.full((1,), n_pages, dtype=torch.int32, device=device), page)
+
+
+class PagePools:
+    """Arrays that are kept by pages: tensors whose first dim is the page."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)
+        self.n_pages = self.tensors[0].shape[0] if self.tensors else None
+        self.device = self.tensors[0].device if self.tensors else None
+        self.c = (lookat_page_pool * max(1, len(self.tensors)))()
+        for i, t in enumerate(self.tensors):
+            if t.dim() < 1 or t.shape[0] != self.n_pages:
+                raise ValueError(f"pool {i} has {tuple(t.shape)}, not {self.n_pages} pages")
+            self.c[i] = lookat_page_pool(_on(t, t.dtype, f"pool {i}", self.device), t.numel() // max(1, t.shape[0]) * t.element_size())
 
 
 class Lookat:
@@ -362,6 +468,79 @@ class Lookat:
             _dev(v, torch.float16, "v", (B, c.n_kv_heads, L_max, c.d_v)), L_max, pos, n_splits,
             _host(out_host, torch.float32, "out_host", (B, c.n_q_heads, c.d_v))))
         return out_host
+
+    # -- the 8-bit paged cache (include/lookat_q8.h) --------------------------------
+    def _q8(self, cache, tables, seq_lens):
+        c = self.cfg
+        if (cache.n_kv_heads, cache.d_k, cache.d_v) != (c.n_kv_heads, c.d_k, c.d_v):
+            raise ValueError(f"the cache holds {cache.n_kv_heads} heads of {cache.d_k}/{cache.d_v} dims, "
+                             f"the context {c.n_kv_heads} of {c.d_k}/{c.d_v}")
+        if cache.device != self.device:
+            raise ValueError(f"the cache is on {cache.device}, the context on {self.device}")
+        if tables.dim() != 2:
+            raise ValueError(f"tables must have shape [B][max_pages], got {tuple(tables.shape)}")
+        B, max_pages = tables.shape
+        return B, max_pages, _on(tables, torch.int32, "tables", self.device), _on(seq_lens, torch.int32, "seq_lens", self.device, (B,))
+
+    def lookat_q8_append(self, cache, k_new, v_new, tables, seq_lens, n_new=None):
+        """Quantises the last n_new[b] (None: n) tokens of every row into its pages; k_new [B][H_kv][n][d_k]."""
+        c = self.cfg
+        B, max_pages, tb, sl = self._q8(cache, tables, seq_lens)
+        n = k_new.shape[2] if k_new.dim() == 4 else 0
+        self._check(self._lib.lookat_q8_append(
+            self._h, cache.c, _on(k_new, torch.float16, "k_new", self.device, (B, c.n_kv_heads, n, c.d_k)),
+            _on(v_new, torch.float16, "v_new", self.device, (B, c.n_kv_heads, n, c.d_v)), B, n, tb, max_pages, sl,
+            _on(n_new, torch.int32, "n_new", self.device, (B,))))
+
+    def lookat_attend_q8(self, cache, q, tables, seq_lens, out=None, out_fp16=False):
+        """Attention of the queries at the rows' last positions over the 8-bit cache; q [B][H_q][L_q][d_k] or, for one
+        token per row, [B][H_q][d_k]."""
+        c = self.cfg
+        B, max_pages, tb, sl = self._q8(cache, tables, seq_lens)
+        one = q.dim() == 3
+        L_q = 1 if one else q.shape[2]
+        dtype = torch.float16 if out_fp16 else torch.float32
+        shape = (B, c.n_q_heads, c.d_v) if one else (B, c.n_q_heads, L_q, c.d_v)
+        if out is None:
+            out = torch.empty(shape, dtype=dtype, device=self.device)
+            if torch.cuda.current_stream(self.device) != self.stream:
+                out.record_stream(self.stream)
+            po = out.data_ptr()
+        else:
+            po = _on(out, dtype, "out", self.device, shape)
+        self._check(self._lib.lookat_attend_q8(
+            self._h, cache.c, _on(q, torch.float16, "q", self.device, (B, c.n_q_heads, c.d_k) if one else (B, c.n_q_heads, L_q, c.d_k)),
+            B, L_q, tb, max_pages, sl, po, 1 if out_fp16 else 0))
+        return out
+
+    def _pages(self, state, pools):
+        if state.device != self.device:
+            raise ValueError(f"the page state is on {state.device}, the context on {self.device}")
+        if pools is None:
+            return None
+        if not isinstance(pools, PagePools):
+            pools = PagePools(pools)
+        if pools.tensors and (pools.n_pages != state.n_pages or pools.device != self.device):
+            raise ValueError(f"the pools have {pools.n_pages} pages on {pools.device}, the state {state.n_pages} on {state.device}")
+        return pools
+
+    def lookat_pages_extend(self, state, n_new, pools):
+        """Pages for n_new[b] more tokens per row (n_new all 0 afterwards if there are too few); pools: the tensors kept
+        by pages, or a PagePools of them."""
+        pools = self._pages(state, pools)
+        self._check(self._lib.lookat_pages_extend(self._h, state.c, _on(n_new, torch.int32, "n_new", self.device, (state.B,)),
+                                                  pools.c, len(pools.tensors)))
+
+    def lookat_pages_fork(self, state, parents):
+        """Row b continues from row parents[b]; -1 empties it."""
+        self._pages(state, None)
+        self._check(self._lib.lookat_pages_fork(self._h, state.c, _on(parents, torch.int32, "parents", self.device, (state.B,))))
+
+    def lookat_pages_compact(self, state, pools, remap=None):
+        """Live pages into the lowest ids; remap: optional int32 [n_pages] that gets each page's new id (-1: not live)."""
+        pools = self._pages(state, pools)
+        self._check(self._lib.lookat_pages_compact(self._h, state.c, pools.c, len(pools.tensors),
+                                                   _on(remap, torch.int32, "remap", self.device, (state.n_pages,))))
 
     def lookat_kernel_launches(self) -> int:
         return int(self._lib.lookat_kernel_launches(self._h))

@@ -7,6 +7,7 @@
 #include <new>
 
 #include "common.cuh"
+#include "q8.cuh"
 
 namespace lookat {
 
@@ -48,6 +49,31 @@ lookat_status ensure(Ctx *ctx, void **ptr, size_t *cap, size_t need_bytes, const
     }
     *ptr = p;
     *cap = need_bytes;
+    return LOOKAT_OK;
+}
+
+lookat_status workspace(Ctx *ctx, Workspace &w, size_t bytes, bool zeroed, const char *what)
+{
+    if (bytes <= w.cap) return LOOKAT_OK;
+    cudaStreamCaptureStatus capturing = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(ctx->stream, &capturing) != cudaSuccess || capturing != cudaStreamCaptureStatusNone) {
+        cudaGetLastError();
+        return set_error(ctx, LOOKAT_ERR_INVALID_ARG, "%s: the workspace would have to grow during a stream capture; make one call of this size before it", what);
+    }
+    const size_t cap = bytes > 2 * w.cap ? bytes : 2 * w.cap;
+    void *p = nullptr;
+    if (w.n_outgrown >= (int)(sizeof(w.outgrown) / sizeof(w.outgrown[0])) || cudaMalloc(&p, cap) != cudaSuccess) {
+        cudaGetLastError();
+        return set_error(ctx, LOOKAT_ERR_NOMEM, "%s: no device memory for %zu bytes", what, cap);
+    }
+    if (zeroed && cudaMemsetAsync(p, 0, cap, ctx->stream) != cudaSuccess) {
+        cudaGetLastError();
+        cudaFree(p);
+        return set_error(ctx, LOOKAT_ERR_CUDA, "%s: memset failed", what);
+    }
+    if (w.ptr) w.outgrown[w.n_outgrown++] = w.ptr;
+    w.ptr = p;
+    w.cap = cap;
     return LOOKAT_OK;
 }
 
@@ -284,6 +310,10 @@ void lookat_destroy(lookat_ctx *handle)
                     ctx->step_q,  ctx->step_k,  ctx->step_out};
     for (void *p : bufs)
         if (p) cudaFree(p);
+    for (Workspace *w : {&ctx->q8_partials, &ctx->q8_tickets, &ctx->page_lists, &ctx->page_marks}) {
+        if (w->ptr) cudaFree(w->ptr);
+        for (int i = 0; i < w->n_outgrown; ++i) cudaFree(w->outgrown[i]);
+    }
     if (ctx->timeout_flag) cudaFreeHost(ctx->timeout_flag);
     if (ctx->status_word) cudaFreeHost(ctx->status_word);
     for (int i = 0; i < ctx->ev_cap; ++i) {
@@ -307,6 +337,10 @@ const char *lookat_last_error(const lookat_ctx *handle)
         *(volatile int *)ctx->status_word = 0;
         if (word & kStatusCopyTimeout)
             snprintf(ctx->err, sizeof(ctx->err), "attend: a bounded wait for a bulk copy ran out; the output of that call is not valid");
+        else if (word & kStatusNoPages)
+            snprintf(ctx->err, sizeof(ctx->err), "pages_extend: too few free pages or table entries; nothing was changed and n_new was set to 0");
+        else if (word & kStatusBadPage)
+            snprintf(ctx->err, sizeof(ctx->err), "8-bit cache: a page id, length or count outside its range was met; its tokens were left out");
         else
             snprintf(ctx->err, sizeof(ctx->err),
                      "debug check: a code >= K was found in a code cache and clamped to K - 1; results computed from it are not valid");

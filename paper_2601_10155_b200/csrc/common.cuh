@@ -10,6 +10,15 @@
 
 namespace lookat {
 
+// Scratch that captured graphs may name: an outgrown buffer is kept until the context is destroyed (capacities double, so
+// 48 of them are never reached).
+struct Workspace {
+    void *ptr;
+    size_t cap;                            // bytes
+    void *outgrown[48];
+    int n_outgrown;
+};
+
 // Context: configuration, stream, scratch owned by the library.
 struct Ctx {
     lookat_config cfg;
@@ -45,6 +54,8 @@ struct Ctx {
     void *step_q, *step_k;
     float *step_out;
     size_t step_q_cap, step_k_cap, step_out_cap;   // bytes
+    // 8-bit paged cache: partial results and arrival counters of the attention; lists of pages, tables being rewritten
+    Workspace q8_partials, q8_tickets, page_lists, page_marks;
 
     // per-launch timing of the attend kernel: an event pair per timed launch, read only after the timed run
     int timing;

@@ -1,0 +1,77 @@
+// Internal declarations of the 8-bit paged cache (include/lookat_q8.h): argument blocks, workspaces, the arithmetic of
+// the stored numbers.
+#pragma once
+
+#include <cuda_fp8.h>
+
+#include "common.cuh"
+#include "lookat_q8.h"
+
+namespace lookat {
+
+constexpr int kStatusBadPage = 4;           // a page id, a length or a count outside its range was met and left out
+constexpr int kStatusNoPages = 8;           // lookat_pages_extend found too few pages and changed nothing
+
+constexpr float kQ8RangeInt8 = 127.f, kQ8RangeE4m3 = 448.f;
+
+// Where the tokens of the cache are, as the kernels take it.
+struct Q8View {
+    uint8_t *k, *v;
+    float *k_amax, *v_amax;
+    const int32_t *tables;      // [B][max_pages]
+    const int32_t *seq_lens;    // [B]
+    int n_pages, max_pages, page_shift, H_kv, d_k, d_v;
+    int *status;
+};
+
+__device__ __forceinline__ void q8_report(int *status, int bit)
+{
+    if (status) atomicOr(status, bit);
+}
+
+struct Q8AppendArgs {
+    Q8View c;
+    const __half *k_new, *v_new;    // [B][H_kv][n][d]
+    const int32_t *n_new;           // [B] or null
+    int B, n, format;
+};
+lookat_status launch_q8_append(Ctx *ctx, const Q8AppendArgs &a);
+
+struct Q8AttendArgs {
+    Q8View c;
+    const __half *q;                // [B][H_q][L_q][d_k]
+    void *out;                      // [B][H_q][L_q][d_v], fp32 or fp16
+    int out_fp16, B, H_q, g, L_q, format;
+    float scale_log2;               // softmax scale * log2(e)
+};
+lookat_status launch_attend_q8(Ctx *ctx, const Q8AttendArgs &a);
+
+// Scratch of at least `bytes` (zeroed when it is new, if asked).  Grows by allocating anew; the old buffer stays until the
+// context is destroyed, because a captured graph may still name it.  Refuses to allocate while the stream is captured.
+lookat_status workspace(Ctx *ctx, Workspace &w, size_t bytes, bool zeroed, const char *what);
+
+// one 8-bit number nearest to x (ties to even; |x| <= R up to rounding), as its byte
+template <int FORMAT>
+__device__ __forceinline__ uint32_t q8_round(float x)
+{
+    if constexpr (FORMAT == LOOKAT_Q8_INT8) {
+        return (uint32_t)__float2int_rn(fminf(fmaxf(x, -127.f), 127.f)) & 0xffu;
+    } else {
+        return (uint32_t)__nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3);
+    }
+}
+// the number a byte holds
+template <int FORMAT>
+__device__ __forceinline__ float q8_value(uint32_t byte)
+{
+    if constexpr (FORMAT == LOOKAT_Q8_INT8) {
+        return (float)(int)(int8_t)(uint8_t)byte;
+    } else {
+        // sign, 4 exponent and 3 fraction bits moved to the same places of an fp16: the value comes out 2^8 too small
+        // (exponent biases 7 and 15), for subnormals as well
+        const uint32_t h = ((byte & 0x80u) << 8) | ((byte & 0x7fu) << 7);
+        return __half2float(__ushort_as_half((unsigned short)h)) * 256.f;
+    }
+}
+
+}  // namespace lookat
