@@ -201,6 +201,9 @@ def _host(t, dtype, name, shape):
 
 def _on(t, dtype, name, device, shape=None):
     """_dev, and the tensor lies on the context's device."""
+    if isinstance(t, torch.Tensor) and t.device == device and t.is_cuda and t.dtype is dtype and t.is_contiguous() and \
+            (shape is None or t.shape == shape):
+        return t.data_ptr()                                     # (the checks of the lines below, in the order of their cost)
     p = _dev(t, dtype, name, shape)
     if t is not None and t.device != device:
         raise ValueError(f"{name} is on {t.device}, the context on {device}")
@@ -220,8 +223,8 @@ class Q8Cache:
         if v.dim() != 4:
             raise ValueError(f"v must have shape [n_pages][H_kv][page][d_v], got {tuple(v.shape)}")
         self.k, self.k_amax, self.v, self.v_amax = k, k_amax, v, v_amax
-        self.n_pages, self.n_kv_heads, self.page, self.d_k, self.d_v = n_pages, H, page, d_k, v.shape[3]
-        self.device = k.device
+        self.n_pages, self.page, self.device = n_pages, page, k.device
+        self.heads = (H, d_k, v.shape[3])
         self.c = lookat_q8_cache(_dev(k, k.dtype, "k"), _on(k_amax, torch.float32, "k_amax", k.device, (n_pages, H)),
                                  _on(v, k.dtype, "v", k.device, (n_pages, H, page, v.shape[3])),
                                  _on(v_amax, torch.float32, "v_amax", k.device, (n_pages, H)),
@@ -300,6 +303,8 @@ class Lookat:
         if st != 0:
             raise LookatError(st, "lookat_create rejected the configuration or the device")
         self._h = h
+        self._shape = (n_q_heads, n_kv_heads, d_k, d_v)
+        self._raw_stream = stream.cuda_stream
         self.scale = scale if scale > 0 else 1.0 / math.sqrt(d_k)
 
     # -- helpers ---------------------------------------------------------------
@@ -471,10 +476,8 @@ class Lookat:
 
     # -- the 8-bit paged cache (include/lookat_q8.h) --------------------------------
     def _q8(self, cache, tables, seq_lens):
-        c = self.cfg
-        if (cache.n_kv_heads, cache.d_k, cache.d_v) != (c.n_kv_heads, c.d_k, c.d_v):
-            raise ValueError(f"the cache holds {cache.n_kv_heads} heads of {cache.d_k}/{cache.d_v} dims, "
-                             f"the context {c.n_kv_heads} of {c.d_k}/{c.d_v}")
+        if cache.heads != self._shape[1:]:
+            raise ValueError(f"the cache holds (heads, d_k, d_v) = {cache.heads}, the context {self._shape[1:]}")
         if cache.device != self.device:
             raise ValueError(f"the cache is on {cache.device}, the context on {self.device}")
         if tables.dim() != 2:
@@ -484,33 +487,37 @@ class Lookat:
 
     def lookat_q8_append(self, cache, k_new, v_new, tables, seq_lens, n_new=None):
         """Quantises the last n_new[b] (None: n) tokens of every row into its pages; k_new [B][H_kv][n][d_k]."""
-        c = self.cfg
+        _, H, d_k, d_v = self._shape
+        dev = self.device
         B, max_pages, tb, sl = self._q8(cache, tables, seq_lens)
         n = k_new.shape[2] if k_new.dim() == 4 else 0
-        self._check(self._lib.lookat_q8_append(
-            self._h, cache.c, _on(k_new, torch.float16, "k_new", self.device, (B, c.n_kv_heads, n, c.d_k)),
-            _on(v_new, torch.float16, "v_new", self.device, (B, c.n_kv_heads, n, c.d_v)), B, n, tb, max_pages, sl,
-            _on(n_new, torch.int32, "n_new", self.device, (B,))))
+        st = self._lib.lookat_q8_append(
+            self._h, cache.c, _on(k_new, torch.float16, "k_new", dev, (B, H, n, d_k)), _on(v_new, torch.float16, "v_new", dev, (B, H, n, d_v)),
+            B, n, tb, max_pages, sl, None if n_new is None else _on(n_new, torch.int32, "n_new", dev, (B,)))
+        if st:
+            self._check(st)
 
     def lookat_attend_q8(self, cache, q, tables, seq_lens, out=None, out_fp16=False):
         """Attention of the queries at the rows' last positions over the 8-bit cache; q [B][H_q][L_q][d_k] or, for one
         token per row, [B][H_q][d_k]."""
-        c = self.cfg
+        H, _, d_k, d_v = self._shape
+        dev = self.device
         B, max_pages, tb, sl = self._q8(cache, tables, seq_lens)
         one = q.dim() == 3
         L_q = 1 if one else q.shape[2]
+        pq = _on(q, torch.float16, "q", dev, (B, H, d_k) if one else (B, H, L_q, d_k))
         dtype = torch.float16 if out_fp16 else torch.float32
-        shape = (B, c.n_q_heads, c.d_v) if one else (B, c.n_q_heads, L_q, c.d_v)
+        shape = (B, H, d_v) if one else (B, H, L_q, d_v)
         if out is None:
-            out = torch.empty(shape, dtype=dtype, device=self.device)
-            if torch.cuda.current_stream(self.device) != self.stream:
-                out.record_stream(self.stream)
+            out = torch.empty(shape, dtype=dtype, device=dev)
+            if torch._C._cuda_getCurrentRawStream(dev.index) != self._raw_stream:
+                out.record_stream(self.stream)                  # allocated for another stream than the one that writes it
             po = out.data_ptr()
         else:
-            po = _on(out, dtype, "out", self.device, shape)
-        self._check(self._lib.lookat_attend_q8(
-            self._h, cache.c, _on(q, torch.float16, "q", self.device, (B, c.n_q_heads, c.d_k) if one else (B, c.n_q_heads, L_q, c.d_k)),
-            B, L_q, tb, max_pages, sl, po, 1 if out_fp16 else 0))
+            po = _on(out, dtype, "out", dev, shape)
+        st = self._lib.lookat_attend_q8(self._h, cache.c, pq, B, L_q, tb, max_pages, sl, po, 1 if out_fp16 else 0)
+        if st:
+            self._check(st)
         return out
 
     def _pages(self, state, pools):

@@ -29,8 +29,9 @@ namespace {
 
 constexpr int kAqWarps = 4, kAqThreads = kAqWarps * 32;
 constexpr int kAqTile = 16 * kAqWarps;          // tokens of a CTA's step
-constexpr int kAqStages = 4;
+constexpr int kAqStages = 3;                    // tiles in a warp's ring
 constexpr int kAqMinChunk = 4;                  // steps per CTA below which a row is not cut
+constexpr int kAqJoinCells = 1;                 // what joining a unit's results costs, in steps
 constexpr int kAqMaxParts = 128;                // pieces that a unit is cut into at most (one CTA joins them)
 constexpr float kAqSlack = 8.f;                 // how far scores may run ahead of M (base-2 units)
 
@@ -41,11 +42,25 @@ __device__ __forceinline__ void aq_copy(uint32_t dst, const void *src)
     if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
 }
+// the same, or zeros
+template <int BYTES>
+__device__ __forceinline__ void aq_copy_if(uint32_t dst, const void *src, bool there)
+{
+    const int n = there ? BYTES : 0;
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(n) : "memory");
+}
 __device__ __forceinline__ void aq_mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void aq_mma_zero(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t aq_transpose(uint32_t x)
 {
@@ -68,35 +83,87 @@ __device__ __forceinline__ void aq_pairs(uint32_t w, uint32_t &lo, uint32_t &hi)
         lo = *reinterpret_cast<const uint32_t *>(&x);
         hi = *reinterpret_cast<const uint32_t *>(&y);
     } else {
+#ifdef AQ_BITS
         const uint32_t a = __byte_perm(w, 0u, 0x1404), b = __byte_perm(w, 0u, 0x3424);
         lo = ((a >> 1) & 0x3f803f80u) | (a & 0x80008000u);
         hi = ((b >> 1) & 0x3f803f80u) | (b & 0x80008000u);
+#else
+        asm("{\n.reg .b16 x, y;\nmov.b32 {x, y}, %2;\ncvt.rn.f16x2.e4m3x2 %0, x;\ncvt.rn.f16x2.e4m3x2 %1, y;\n}" : "=r"(lo), "=r"(hi) : "r"(w));
+#endif
     }
 }
 template <int FORMAT>
+#ifdef AQ_BITS
 constexpr float kAqUnit = FORMAT == LOOKAT_Q8_INT8 ? 1.f / kQ8RangeInt8 : 256.f / kQ8RangeE4m3;   // value of a fp16 number per amax
+#else
+constexpr float kAqUnit = 1.f / (FORMAT == LOOKAT_Q8_INT8 ? kQ8RangeInt8 : kQ8RangeE4m3);
+#endif
 
-template <int DP, int NT>
+// Where the 16-byte pieces of a tile's rows lie: a row of 64, 128 or 256 bytes after the other as in the cache, the pieces
+// of row r permuted by XOR with aq_turn(r) within their 128 bytes.  The copies are then linear (512 consecutive bytes per
+// warp instruction: reading every other row instead cost a quarter of the bandwidth), and each quarter-warp's reads below
+// touch eight different 16-byte columns: rows r, r + 1 with pieces 0..3 (scores) since the turns of 2i and 2i + 1 differ in
+// bit 2; rows 0, 2, 4, 6 (or 1, 3, 5, 7) with pieces 2i, 2i + 1 (values) since their turns differ above bit 0.
+__device__ __forceinline__ constexpr int aq_turn(int r) { return (r & 6) ^ ((r & 1) << 2); }
+template <int DP>
+__device__ __forceinline__ int aq_piece(int r, int p)           // byte offset of piece p of row r
+{
+    if constexpr (DP == 64) return ((r >> 1) * 8 + (p ^ aq_turn(r))) * 16;
+    else return (r * (DP / 16) + (p & ~7) + ((p ^ aq_turn(r)) & 7)) * 16;
+}
+
+template <int DP, int NT, bool PACK>
 struct AqLayout {
-    static constexpr int kJ = DP / 64;                          // 16-byte pieces per lane and token row of K
+    static constexpr int kJ = DP / 64;                          // 16-byte pieces of a K row per lane
     static constexpr int kVBytes = DP == 64 ? 8 : 16;           // a lane's piece of a V row
     static constexpr int kVPieces = DP / 8 / kVBytes;           // ... and how many of them
-    static constexpr int kTile = 32 * (2 * kJ * 16 + 4 * kVPieces * kVBytes);      // bytes of 16 tokens (padded to DP dims)
-    static constexpr int kStage = kTile + 16;                   // + amax^K, amax^V
+    static constexpr int kOffV = 16 * DP, kTile = 2 * kOffV;    // bytes of 16 tokens (padded to DP dims): K, V
+    static constexpr int kStage = kTile + 16;                   // + amax^K, amax^V, whether the tile is there
     static constexpr int kRing = kAqWarps * kAqStages * kStage;
-    // the warps' results of a unit lie over the drained ring: O [warp][col][DP + 4], M and l [warp][col]
-    static constexpr int kCols = 8 * NT, kPitch = DP + 4;
-    static constexpr int kJoin = kAqWarps * kCols * (kPitch + 2) * 4;
-    static constexpr int kBytes = kRing > kJoin ? kRing : kJoin;
+    // the warps' results of a unit: O [col][DP] of each warp in the stage of its last tile where that is large enough (its
+    // next copy comes after the join), M, l and the factor of M [warp][col], then M and l of the CTA
+    static constexpr int kCols = PACK ? 4 : 8 * NT;
+    static constexpr bool kInRing = kCols * DP * 4 <= kTile;
+    static constexpr int kJoin = ((kInRing ? 0 : kAqWarps * kCols * DP) + kAqWarps * kCols * 3 + 2 * kCols) * 4;
+    // when a CTA joins the pieces of a unit, their factors [col][kAqMaxParts] lie over the drained ring
+    static_assert(kRing >= kCols * kAqMaxParts * 4, "factors of the pieces");
+    static constexpr int kBytes = kRing + kJoin;
     // a piece of a unit in global memory: M [col], l [col], O [col][DP]
     static constexpr int kPart = kCols * (DP + 2);              // floats
 };
 
-template <int FORMAT, int DP, int NT>
-__global__ void __launch_bounds__(kAqThreads, DP == 256 ? 2 : 3)
+// A place in the flat sequence of rows, units and steps.  A unit takes steps + kAqJoinCells cells of it (what precedes its
+// first step stands for the join); an empty row takes none.
+struct AqCursor {
+    int b, unit, step, steps, len;
+    int at;                                                     // cells from the start of the CTA's part
+    __device__ __forceinline__ void row(const Q8View &c, int cap)
+    {
+        len = min(max(__ldg(c.seq_lens + b), 0), cap);
+        steps = (len + kAqTile - 1) / kAqTile;
+    }
+    __device__ __forceinline__ void advance(const Q8View &c, int B, int cap, int units, int end)
+    {
+        ++at;
+        if (++step < steps) return;
+        step = 0;
+        at += kAqJoinCells;
+        if (at < end && ++unit == units) {
+            unit = 0;
+            do {
+                ++b;
+                row(c, cap);
+            } while (steps == 0);                               // (a later row has steps: at < end)
+        }
+    }
+};
+
+// EXACT: d_k = d_v = DP
+template <int FORMAT, int DP, int NT, bool PACK, bool EXACT>
+__global__ void __launch_bounds__(kAqThreads, DP == 256 ? 2 : NT == 2 ? 3 : 4)
 attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict__ tickets)
 {
-    using Lay = AqLayout<DP, NT>;
+    using Lay = AqLayout<DP, NT, PACK>;
     constexpr int KJ = Lay::kJ, VP = Lay::kVPieces, VB = Lay::kVBytes, MT = DP / 16;
     extern __shared__ __align__(16) unsigned char aq_raw[];
     __shared__ long long s_ll[kAqWarps + 2];
@@ -106,22 +173,28 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
     const int page = 1 << c.page_shift, cap = c.max_pages << c.page_shift;
     const int n_cols = a.g * a.L_q, groups = (n_cols + Lay::kCols - 1) / Lay::kCols, units = c.H_kv * groups;
 
-    // ---- this CTA's part of the flat sequence ----
-    auto steps_of = [&](int b) {                                // an empty row has one step, which writes its zeros
-        const int n = min(max(c.seq_lens[b], 0), cap);
-        return max(1, (n + kAqTile - 1) / kAqTile);
-    };
-    long long chunk, pos, end, base;
-    int b;
+    // ---- rows without a token: zeros ----
+    for (int b = blockIdx.x; b < a.B; b += gridDim.x)
+        if (c.seq_lens[b] <= 0) {
+            const size_t n = (size_t)a.H_q * a.L_q * c.d_v * (a.out_fp16 ? 2 : 4) / 16;
+            uint4 *row = static_cast<uint4 *>(a.out) + n * b;
+            for (size_t i = tid; i < n; i += kAqThreads) row[i] = make_uint4(0u, 0u, 0u, 0u);
+        }
+
+    // ---- this CTA's part of the flat sequence: cells pos .. pos + end - 1 ----
+    long long chunk, pos;
+    int end;
+    AqCursor at;                                                // where the products are
     {
         const int per = (a.B + kAqThreads - 1) / kAqThreads, b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
         long long mine = 0;
         int longest = 0;
-        for (int i = b0; i < b1; ++i) {
-            const int len = c.seq_lens[i], n = steps_of(i);
-            if (blockIdx.x == 0 && (len < 0 || len > cap)) q8_report(c.status, kStatusBadPage);
-            mine += n;
-            longest = max(longest, n);
+        AqCursor r;
+        for (r.b = b0; r.b < b1; ++r.b) {
+            r.row(c, cap);
+            if (blockIdx.x == 0 && r.len != c.seq_lens[r.b]) q8_report(c.status, kStatusBadPage);
+            mine += r.steps ? r.steps + kAqJoinCells : 0;
+            longest = max(longest, r.steps);
         }
         long long incl = mine;
 #pragma unroll
@@ -144,142 +217,172 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
         }
         total *= units;
         chunk = (total + gridDim.x - 1) / gridDim.x;
-        chunk = max(chunk, (long long)max(min(kAqMinChunk, longest), (longest + kAqMaxParts - 1) / kAqMaxParts));
+        chunk = max(chunk, (long long)kAqJoinCells + max(min(kAqMinChunk, longest), (longest + kAqMaxParts - 2) / (kAqMaxParts - 1)));
         pos = chunk * blockIdx.x;
-        end = min(pos + chunk, total);
-        if (pos >= end) return;                                 // (the whole CTA)
+        if (pos >= total) return;                               // (the whole CTA)
+        end = (int)min(chunk, total - pos);
         if (pos >= before * units && pos < (before + mine) * units) {
-            int i = b0;
-            for (; pos >= (before + steps_of(i)) * units; ++i) before += steps_of(i);
-            s_i[kAqWarps] = i;
-            s_ll[kAqWarps] = before * units;
+            r.b = b0;
+            for (;; ++r.b) {
+                r.row(c, cap);
+                const int cells = r.steps ? r.steps + kAqJoinCells : 0;
+                if (pos < (before + cells) * units) break;
+                before += cells;
+            }
+            s_i[kAqWarps] = r.b;
+            s_ll[kAqWarps] = pos - before * units;
         }
         __syncthreads();
-        b = s_i[kAqWarps];
-        base = s_ll[kAqWarps];
+        at.b = s_i[kAqWarps];
+        at.row(c, cap);
+        const int cells = at.steps + kAqJoinCells, cell = (int)(s_ll[kAqWarps] % cells);
+        at.unit = (int)(s_ll[kAqWarps] / cells);
+        at.step = max(cell - kAqJoinCells, 0);
+        at.at = max(kAqJoinCells - cell, 0);
+        if (at.at >= end) return;                               // nothing but a unit's join cells: no step of it is here
     }
 
     unsigned char *const ring = aq_raw + warp * (kAqStages * Lay::kStage);
-    const uint32_t ring0 = aq_smem(ring);
-    float *const sO = reinterpret_cast<float *>(aq_raw);                            // [warp][col][kPitch]
-    float *const sM = sO + kAqWarps * Lay::kCols * Lay::kPitch, *const sL = sM + kAqWarps * Lay::kCols;
+    float *const sM = reinterpret_cast<float *>(aq_raw + Lay::kBytes) - kAqWarps * Lay::kCols * 3 - 2 * Lay::kCols, *const sL = sM + kAqWarps * Lay::kCols, *const sK = sL + kAqWarps * Lay::kCols;
+    float *const sTop = sK + kAqWarps * Lay::kCols, *const sSum = sTop + Lay::kCols;
+    const int d_k = EXACT ? DP : c.d_k, d_v = EXACT ? DP : c.d_v;
+    // O of warp w [col][DP], during a join after step n
+    auto results = [&](int w, int n) {
+        return reinterpret_cast<float *>(Lay::kInRing ? aq_raw + (w * kAqStages + n % kAqStages) * Lay::kStage : aq_raw + Lay::kRing + w * (Lay::kCols * DP * 4));
+    };
     const float k_unit = kAqUnit<FORMAT> * a.scale_log2;
 
-    while (pos < end) {
-        const int len = min(max(c.seq_lens[b], 0), cap), steps = max(1, (len + kAqTile - 1) / kAqTile);
-        const int unit = (int)((pos - base) / steps), step0 = (int)((pos - base) % steps);
-        const int n_steps = (int)min((long long)(steps - step0), end - pos);
-        const int h = unit / groups, col0 = unit % groups * Lay::kCols;
-        const int32_t *table = c.tables + (size_t)b * c.max_pages;
-
-        // ---- q as the scores' second operand; the last token each of this lane's result columns sees ----
-        uint32_t qf[NT][KJ * 4][2];
-        int last[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int col = col0 + nt * 8 + g;
-            const bool on = col < n_cols;
-            const __half *qr = a.q + (((size_t)b * a.H_q + h * a.g + (on ? col % a.g : 0)) * a.L_q + (on ? col / a.g : 0)) * c.d_k;
-#pragma unroll
-            for (int j = 0; j < KJ; ++j) {
-                uint4 x = make_uint4(0u, 0u, 0u, 0u), y = x;
-                if (on && 64 * j + 16 * t < c.d_k) {
-                    x = __ldg(reinterpret_cast<const uint4 *>(qr + 64 * j + 16 * t));
-                    y = __ldg(reinterpret_cast<const uint4 *>(qr + 64 * j + 16 * t + 8));
-                }
-                qf[nt][4 * j][0] = x.x, qf[nt][4 * j][1] = x.y;
-                qf[nt][4 * j + 1][0] = x.z, qf[nt][4 * j + 1][1] = x.w;
-                qf[nt][4 * j + 2][0] = y.x, qf[nt][4 * j + 2][1] = y.y;
-                qf[nt][4 * j + 3][0] = y.z, qf[nt][4 * j + 3][1] = y.w;
+    // ---- the ring runs ahead of the products, over the borders of units; this warp's tile of a step holds tokens
+    //      step * 64 + warp * 16 .. + 15 of the row ----
+    AqCursor ahead = at;
+    auto entry_of = [&](const AqCursor &x) {                    // the table's entry, not looked at yet
+        const int tok = x.step * kAqTile + warp * 16;
+        return x.at < end && tok < x.len ? __ldg(c.tables + (size_t)x.b * c.max_pages + (tok >> c.page_shift)) : -1;
+    };
+    auto fetch = [&](int n, int pid) {                          // the tile at `ahead` into stage n % kAqStages
+        unsigned char *const stage = ring + (n % kAqStages) * Lay::kStage;
+        const uint32_t s = aq_smem(stage);
+        if (ahead.at < end) {
+            const int tok = ahead.step * kAqTile + warp * 16;
+            const bool there = tok < ahead.len && pid >= 0 && pid < c.n_pages;
+            if (lane == 0) {
+                *reinterpret_cast<int *>(stage + Lay::kTile + 8) = there;
+                if (!there && tok < ahead.len) q8_report(c.status, kStatusBadPage);
             }
+            if (there) {
+                const size_t block = (size_t)pid * c.H_kv + (groups == 1 ? ahead.unit : ahead.unit / groups), row = block * page + (tok & (page - 1));
+                // lanes over the pieces of a row, then the rows; behind the row's last token zeros for V: a weight of 0
+                // does not mend a NaN that was left there
+                constexpr int kLanes = DP / 16 < 32 ? DP / 16 : 32, kRows = 32 / kLanes;
+                const int r0 = lane / kLanes, p = lane % kLanes;
+                const uint8_t *k = c.k + (row + r0) * d_k + 16 * p, *v = c.v + (row + r0) * d_v + 16 * p;
+                if (EXACT || 16 * p < d_k)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int cc = col0 + nt * 8 + 2 * t + k;
-                last[nt][k] = cc < n_cols ? len - a.L_q + cc / a.g : -1;
-            }
-        }
-
-        // ---- the ring: tile n of this warp holds tokens (step0 + n) * 64 + warp * 16 .. + 15 ----
-        auto token_of = [&](int n) { return (step0 + n) * kAqTile + warp * 16; };
-        auto page_of = [&](int n) {                             // -1: nothing there (beyond the row, or a bad entry)
-            const int tok = token_of(n);
-            if (n >= n_steps || tok >= len) return -1;
-            const int p = __ldg(table + (tok >> c.page_shift));
-            if (p < 0 || p >= c.n_pages) {
-                q8_report(c.status, kStatusBadPage);
-                return -1;
-            }
-            return p;
-        };
-        auto fetch = [&](int n, int pid) {
-            const uint32_t s = ring0 + (n % kAqStages) * Lay::kStage;
-            if (pid >= 0) {
-                const size_t block = (size_t)pid * c.H_kv + h, row = block * page + (token_of(n) & (page - 1));
-                const uint8_t *k = c.k + (row + g) * c.d_k + 16 * t;
+                    for (int i = 0; i < 16 / kRows; ++i) aq_copy<16>(s + aq_piece<DP>(r0 + i * kRows, p), k + i * kRows * d_k);
+                if (EXACT || 16 * p < d_v)
 #pragma unroll
-                for (int j = 0; j < KJ; ++j)
-                    if (DP == 64 ? 16 * t < c.d_k : 64 * j + 16 * t < c.d_k) {
-                        aq_copy<16>(s + (2 * j) * 512 + lane * 16, k + 64 * j);
-                        aq_copy<16>(s + (2 * j + 1) * 512 + lane * 16, k + 8 * c.d_k + 64 * j);
-                    }
-                const uint8_t *v = c.v + (row + 2 * t) * c.d_v + VB * g;
-#pragma unroll
-                for (int j = 0; j < VP; ++j)
-                    if (VB * g + 128 * j < c.d_v) {
-                        const uint32_t sv = s + 2 * KJ * 512 + j * 4 * (32 * VB) + lane * VB;
-                        aq_copy<VB>(sv, v + 128 * j);
-                        aq_copy<VB>(sv + 32 * VB, v + c.d_v + 128 * j);
-                        aq_copy<VB>(sv + 2 * 32 * VB, v + 8 * c.d_v + 128 * j);
-                        aq_copy<VB>(sv + 3 * 32 * VB, v + 9 * c.d_v + 128 * j);
-                    }
+                    for (int i = 0; i < 16 / kRows; ++i)
+                        aq_copy_if<16>(s + Lay::kOffV + aq_piece<DP>(r0 + i * kRows, p), v + i * kRows * d_v, tok + r0 + i * kRows < ahead.len);
                 if (lane == 0) {
                     aq_copy<4>(s + Lay::kTile, c.k_amax + block);
                     aq_copy<4>(s + Lay::kTile + 4, c.v_amax + block);
                 }
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        };
-        int pids[kAqStages];                                    // pages of the tiles in flight and of the next one
-#pragma unroll
-        for (int n = 0; n < kAqStages; ++n) pids[n] = page_of(n);
-#pragma unroll
-        for (int n = 0; n < kAqStages - 1; ++n) fetch(n, pids[n]);
-
-        float o[NT][MT][4], m_ref[NT][2], l_sum[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-            for (int i = 0; i < MT; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
-            m_ref[nt][0] = m_ref[nt][1] = -1e30f;
-            l_sum[nt][0] = l_sum[nt][1] = 0.f;
         }
-
-        for (int n = 0; n < n_steps; ++n) {
-            asm volatile("cp.async.wait_group %0;" ::"n"(kAqStages - 2) : "memory");
-            __syncwarp();                                       // lane 0's amax is there; everyone is done with tile n - 1
-            const int pid = pids[0];
-            fetch(n + kAqStages - 1, pids[kAqStages - 1]);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int entry;
+    {
+        AqCursor x = at;
+        int entries[kAqStages];                                 // asked for together
 #pragma unroll
-            for (int i = 0; i < kAqStages - 1; ++i) pids[i] = pids[i + 1];
-            pids[kAqStages - 1] = page_of(n + kAqStages);
-            if (pid < 0) continue;
-            const unsigned char *s = ring + (n % kAqStages) * Lay::kStage;
-            const float2 amax = *reinterpret_cast<const float2 *>(s + Lay::kTile);
-            const float ks = amax.x * k_unit;
+        for (int n = 0; n < kAqStages; ++n) {
+            entries[n] = entry_of(x);
+            if (x.at < end) x.advance(c, a.B, cap, units, end);
+        }
+#pragma unroll
+        for (int n = 0; n < kAqStages - 1; ++n) {
+            fetch(n, entries[n]);
+            if (ahead.at < end) ahead.advance(c, a.B, cap, units, end);
+        }
+        entry = entries[kAqStages - 1];
+    }
+
+    // pieces of units that other CTAs hold pieces of: the first and the last unit of this CTA's part
+    int split_first[2] = {-1, -1}, split_pieces[2] = {0, 0}, split_b[2] = {0, 0}, split_unit[2] = {0, 0}, n_split = 0;
+    uint32_t qf[NT][KJ * 4][2];
+    int last[NT][2];
+    float o[NT][MT][4], m_ref[NT][2], l_sum[NT][2];
+    const int quads = d_v / 4;
+    auto store = [&](int b, int unit, int col, int quad, float4 x, float l) {       // o = O / (R l); nothing seen: zeros
+        const int cc = unit % groups * Lay::kCols + col;
+        const float r = l != 0.f ? kAqUnit<FORMAT> / l : 0.f;
+        const size_t to = (((size_t)b * a.H_q + unit / groups * a.g + cc % a.g) * a.L_q + cc / a.g) * d_v + quad * 4;
+        x = make_float4(x.x * r, x.y * r, x.z * r, x.w * r);
+        if (a.out_fp16) {
+            const __half2 p = __floats2half2_rn(x.x, x.y), q = __floats2half2_rn(x.z, x.w);
+            *reinterpret_cast<uint2 *>(static_cast<__half *>(a.out) + to) =
+                make_uint2(*reinterpret_cast<const uint32_t *>(&p), *reinterpret_cast<const uint32_t *>(&q));
+        } else {
+            *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + to) = x;
+        }
+    };
+    auto add = [](float4 &x, float k, const float4 &y) {
+        x = make_float4(fmaf(k, y.x, x.x), fmaf(k, y.y, x.y), fmaf(k, y.z, x.z), fmaf(k, y.w, x.w));
+    };
+
+    bool fresh = true;                                          // a unit begins
+    for (int n = 0;; ++n) {
+        if (fresh) {
+            // ---- q as the scores' second operand; the last token each of this lane's result columns sees ----
+            fresh = false;
+            const int h = at.unit / groups, col0 = at.unit % groups * Lay::kCols;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const int col = col0 + (PACK ? g & 3 : nt * 8 + g);
+                const bool on = col < n_cols;
+                const __half *qr = a.q + (((size_t)at.b * a.H_q + h * a.g + (on ? col % a.g : 0)) * a.L_q + (on ? col / a.g : 0)) * d_k;
+#pragma unroll
+                for (int j = 0; j < KJ; ++j) {
+                    uint4 x = make_uint4(0u, 0u, 0u, 0u), y = x;
+                    if (on && 64 * j + 16 * t < d_k) {
+                        x = __ldg(reinterpret_cast<const uint4 *>(qr + 64 * j + 16 * t));
+                        y = __ldg(reinterpret_cast<const uint4 *>(qr + 64 * j + 16 * t + 8));
+                    }
+                    qf[nt][4 * j][0] = x.x, qf[nt][4 * j][1] = x.y;
+                    qf[nt][4 * j + 1][0] = x.z, qf[nt][4 * j + 1][1] = x.w;
+                    qf[nt][4 * j + 2][0] = y.x, qf[nt][4 * j + 2][1] = y.y;
+                    qf[nt][4 * j + 3][0] = y.z, qf[nt][4 * j + 3][1] = y.w;
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int cc = col0 + (PACK ? 2 * (t & 1) : nt * 8 + 2 * t) + k;
+                    last[nt][k] = cc < n_cols ? at.len - a.L_q + cc / a.g : -1;
+                    m_ref[nt][k] = -1e30f;
+                    l_sum[nt][k] = 0.f;
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
+            }
+        }
+        asm volatile("cp.async.wait_group %0;" ::"n"(kAqStages - 2) : "memory");
+        __syncwarp();                                           // lane 0's words are there; everyone is done with step n - 1
+        fetch(n + kAqStages - 1, entry);
+        if (ahead.at < end) ahead.advance(c, a.B, cap, units, end);
+        entry = entry_of(ahead);
+        const unsigned char *s = ring + (n % kAqStages) * Lay::kStage;
+        const float4 meta = *reinterpret_cast<const float4 *>(s + Lay::kTile);
+        if (__float_as_int(meta.z)) {
+            const float ks = meta.x * k_unit;
 
             // scores of tokens g, g + 8 for columns 2t, 2t + 1; two chains of products per column group
             float sc[NT][4], sd[NT][4];
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                sc[nt][0] = sc[nt][1] = sc[nt][2] = sc[nt][3] = 0.f;
-                sd[nt][0] = sd[nt][1] = sd[nt][2] = sd[nt][3] = 0.f;
-            }
-#pragma unroll
             for (int j = 0; j < KJ; ++j) {
                 uint4 x = make_uint4(0u, 0u, 0u, 0u), y = x;
-                if (64 * j + 16 * t < c.d_k) {
-                    x = *reinterpret_cast<const uint4 *>(s + (2 * j) * 512 + lane * 16);
-                    y = *reinterpret_cast<const uint4 *>(s + (2 * j + 1) * 512 + lane * 16);
+                if (EXACT || 64 * j + 16 * t < d_k) {
+                    x = *reinterpret_cast<const uint4 *>(s + aq_piece<DP>(g, t + 4 * j));
+                    y = *reinterpret_cast<const uint4 *>(s + aq_piece<DP>(g + 8, t + 4 * j));
                 }
                 const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
@@ -288,28 +391,31 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
                     aq_pairs<FORMAT>(xw[w], a0, a2);
                     aq_pairs<FORMAT>(yw[w], a1, a3);
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
-                        aq_mma((w & 1) ? sd[nt] : sc[nt], a0, a1, a2, a3, qf[nt][4 * j + w][0], qf[nt][4 * j + w][1]);
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float (&dst)[4] = (w & 1) ? sd[nt] : sc[nt];
+                        if (j == 0 && w < 2) aq_mma_zero(dst, a0, a1, a2, a3, qf[nt][w][0], qf[nt][w][1]);
+                        else aq_mma(dst, a0, a1, a2, a3, qf[nt][4 * j + w][0], qf[nt][4 * j + w][1]);
+                    }
                 }
             }
 
             // weights; amax^V = 2^e f
-            const int vb = __float_as_int(amax.y) >> 23;
+            const int vb = __float_as_int(meta.y) >> 23;
             const float e = vb > 0 ? (float)(vb - 127) : 0.f;
-            const float f = vb > 0 ? __int_as_float((__float_as_int(amax.y) & 0x7fffff) | 0x3f800000) : amax.y;
+            const float f = vb > 0 ? __int_as_float((__float_as_int(meta.y) & 0x7fffff) | 0x3f800000) : meta.y;
             const float inv_e = vb > 0 ? __int_as_float((254 - vb) << 23) : 1.f;
-            const int tok = token_of(n) + g;
+            const int tok = at.step * kAqTile + warp * 16 + g;
             uint32_t ph[NT][2], pl[NT][2];
-            bool ahead = false;
+            bool beyond = false;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float x = fmaf(sc[nt][i] + sd[nt][i], ks, e);
                     sc[nt][i] = tok + 8 * (i >> 1) <= last[nt][i & 1] ? x : -INFINITY;
-                    ahead |= sc[nt][i] > m_ref[nt][i & 1] + kAqSlack;
+                    beyond |= sc[nt][i] > m_ref[nt][i & 1] + kAqSlack;
                 }
-            if (__any_sync(0xffffffffu, ahead)) {               // M moves (seldom): the largest of the tile, per column
+            if (__any_sync(0xffffffffu, beyond)) {              // M moves (seldom): the largest of the tile, per column
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -343,8 +449,9 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
                     const __half2 hi = __floats2half2_rn(w[2 * r], w[2 * r + 1]);
                     const float2 hf = __half22float2(hi);
                     const __half2 lo = __floats2half2_rn(w[2 * r] - hf.x, w[2 * r + 1] - hf.y);
-                    ph[nt][r] = aq_transpose(*reinterpret_cast<const uint32_t *>(&hi));
-                    pl[nt][r] = aq_transpose(*reinterpret_cast<const uint32_t *>(&lo));
+                    const uint32_t hw = *reinterpret_cast<const uint32_t *>(&hi), lw = *reinterpret_cast<const uint32_t *>(&lo);
+                    ph[nt][r] = aq_transpose(PACK && t >= 2 ? lw : hw);
+                    if constexpr (!PACK) pl[nt][r] = aq_transpose(lw);
                 }
             }
 
@@ -354,14 +461,13 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
                 uint32_t r[4][VB / 4];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const unsigned char *sv = s + 2 * KJ * 512 + (j * 4 + k) * (32 * VB) + lane * VB;
+                    const int row = 2 * t + (k & 1) + 8 * (k >> 1);
                     if constexpr (VB == 16) {
                         uint4 u = make_uint4(0u, 0u, 0u, 0u);
-                        if (VB * g + 128 * j < c.d_v) u = *reinterpret_cast<const uint4 *>(sv);
+                        if (EXACT || 16 * g + 128 * j < d_v) u = *reinterpret_cast<const uint4 *>(s + Lay::kOffV + aq_piece<DP>(row, g + 8 * j));
                         r[k][0] = u.x, r[k][1] = u.y, r[k][2] = u.z, r[k][3] = u.w;
                     } else {
-                        uint2 u = make_uint2(0u, 0u);
-                        if (VB * g + 128 * j < c.d_v) u = *reinterpret_cast<const uint2 *>(sv);
+                        const uint2 u = *reinterpret_cast<const uint2 *>(s + Lay::kOffV + aq_piece<DP>(row, g >> 1) + (g & 1) * 8);
                         r[k][0] = u.x, r[k][1] = u.y;
                     }
                 }
@@ -377,22 +483,34 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                         for (int half = 0; half < 2; ++half) {
-                            // the tile's own sum first, from zero, then onto O: the tensor pipe cuts its sums off
-                            float acc[4] = {0.f, 0.f, 0.f, 0.f};
                             const uint32_t a0 = half ? x2 : x0, a1 = half ? x3 : x1, a2 = half ? y2 : y0, a3 = half ? y3 : y1;
-                            aq_mma(acc, a0, a1, a2, a3, pl[nt][0], pl[nt][1]);
-                            aq_mma(acc, a0, a1, a2, a3, ph[nt][0], ph[nt][1]);
                             float (&dst)[4] = o[nt][(j * (VB / 4) + w) * 2 + half];
+                            // the tile's own sum from zero, then onto O: the tensor pipe cuts its sums off, and a chain
+                            // of a hundred tiles through its accumulator tripled the error of the result
+                            float acc[4];
+                            if constexpr (PACK) {
+                                aq_mma_zero(acc, a0, a1, a2, a3, ph[nt][0], ph[nt][1]);
+                            } else {
+                                aq_mma_zero(acc, a0, a1, a2, a3, pl[nt][0], pl[nt][1]);
+                                aq_mma(acc, a0, a1, a2, a3, ph[nt][0], ph[nt][1]);
+                            }
 #pragma unroll
                             for (int i = 0; i < 4; ++i) dst[i] += acc[i];
                         }
                 }
             }
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        const bool done = at.step + 1 == at.steps || at.at + 1 == end;
+        if (!done) {
+            ++at.step;
+            ++at.at;
+            continue;
+        }
 
-        // ---- the four warps' results, then the pieces of the unit ----
-        __syncthreads();                                        // the ring is drained
+        // ---- the unit, or this CTA's piece of it, is done: join the warps (the ring stays full meanwhile) ----
+        fresh = true;
+        float *const mine = results(warp, n);
+        if constexpr (Lay::kInRing) __syncwarp();               // everyone is done with the tile
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -402,91 +520,131 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
                 l += __shfl_xor_sync(0xffffffffu, l, 8);
                 l += __shfl_xor_sync(0xffffffffu, l, 16);
                 const int col = nt * 8 + 2 * t + k;
-                if (g == 0) {
+                if (g == 0 && (!PACK || t < 2)) {
                     sM[warp * Lay::kCols + col] = m_ref[nt][k];
                     sL[warp * Lay::kCols + col] = l;
                 }
-                if (col0 + col < n_cols)
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        // step i of piece j: dims 128 j + VB g + 2 (i % (VB / 2)), + 1
-                        const int dim = i / (VB / 2) * 128 + VB * g + 2 * (i % (VB / 2));
-                        *reinterpret_cast<float2 *>(sO + (warp * Lay::kCols + col) * Lay::kPitch + dim) = make_float2(o[nt][i][k], o[nt][i][k + 2]);
+                for (int i = 0; i < MT; ++i) {
+                    // step i % (VB / 2) of piece j: dims 128 j + VB g + 2 (i % (VB / 2)), + 1
+                    const int dim = i / (VB / 2) * 128 + VB * g + 2 * (i % (VB / 2));
+                    float2 x = make_float2(o[nt][i][k], o[nt][i][k + 2]);
+                    if constexpr (PACK) {                       // columns 4..7 hold the products of the weights' lower halves
+                        x.x += __shfl_xor_sync(0xffffffffu, x.x, 2);
+                        x.y += __shfl_xor_sync(0xffffffffu, x.y, 2);
                     }
+                    if (!PACK || t < 2) *reinterpret_cast<float2 *>(mine + col * DP + dim) = x;
+                }
             }
         __syncthreads();
-        const long long u0 = base + (long long)unit * steps;
-        const int first = (int)(u0 / chunk), pieces = (int)((u0 + steps - 1) / chunk) - first + 1, me = blockIdx.x;
-        const int n_here = min(Lay::kCols, n_cols - col0);
-        float *const part = parts + (size_t)(2 * me + (me == first)) * Lay::kPart;
-        auto store = [&](int col, int dim, float x) {           // o = O / (R l)
-            const int cc = col0 + col;
-            const size_t at = (((size_t)b * a.H_q + h * a.g + cc % a.g) * a.L_q + cc / a.g) * c.d_v + dim;
-            if (a.out_fp16) static_cast<__half *>(a.out)[at] = __float2half_rn(x);
-            else static_cast<float *>(a.out)[at] = x;
-        };
-        for (int i = tid; i < n_here * c.d_v; i += kAqThreads) {
-            const int col = i / c.d_v, dim = i % c.d_v;
-            float top = sM[col], l = 0.f, x = 0.f;
+        if (tid < Lay::kCols) {
+            float top = sM[tid], l = 0.f;
 #pragma unroll
-            for (int w = 1; w < kAqWarps; ++w) top = fmaxf(top, sM[w * Lay::kCols + col]);
+            for (int w = 1; w < kAqWarps; ++w) top = fmaxf(top, sM[w * Lay::kCols + tid]);
 #pragma unroll
             for (int w = 0; w < kAqWarps; ++w) {
-                const float k = ex2_approx(sM[w * Lay::kCols + col] - top);
-                l = fmaf(k, sL[w * Lay::kCols + col], l);
-                x = fmaf(k, sO[(w * Lay::kCols + col) * Lay::kPitch + dim], x);
+                const float k = ex2_approx(sM[w * Lay::kCols + tid] - top);
+                sK[w * Lay::kCols + tid] = k;
+                l = fmaf(k, sL[w * Lay::kCols + tid], l);
             }
-            if (pieces == 1) {
-                store(col, dim, l != 0.f ? x * kAqUnit<FORMAT> / l : 0.f);
-            } else {
-                if (dim == 0) {
-                    __stcg(part + col, top);
-                    __stcg(part + Lay::kCols + col, l);
-                }
-                __stcg(part + 2 * Lay::kCols + col * DP + dim, x);
-            }
+            sTop[tid] = top;
+            sSum[tid] = l;
+        }
+        __syncthreads();
+        const long long u0 = pos + at.at - at.step;             // the unit's first step
+        const int first = (int)(u0 / chunk), pieces = (int)((u0 + at.steps - 1) / chunk) - first + 1, me = blockIdx.x;
+        const int n_here = min(Lay::kCols, n_cols - at.unit % groups * Lay::kCols) * quads;     // groups of 4 dims, of all columns
+        float *const part = parts + (size_t)(2 * me + (me == first)) * Lay::kPart;
+        for (int i = tid; i < n_here; i += kAqThreads) {
+            const int col = i / quads, quad = i % quads;
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < kAqWarps; ++w)
+                add(x, sK[w * Lay::kCols + col], *reinterpret_cast<const float4 *>(results(w, n) + col * DP + quad * 4));
+            if (pieces == 1) store(at.b, at.unit, col, quad, x, sSum[col]);
+            else __stcg(reinterpret_cast<float4 *>(part + 2 * Lay::kCols + col * DP + quad * 4), x);
         }
         if (pieces > 1) {
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) {
-                const unsigned seen = atomicAdd(tickets + first, 1u);
-                s_i[kAqWarps + 1] = seen == (unsigned)pieces - 1;
-                if (seen == (unsigned)pieces - 1) tickets[first] = 0u;      // all pieces are in: ready for the next launch
+            if (tid < Lay::kCols) {
+                __stcg(part + tid, sTop[tid]);
+                __stcg(part + Lay::kCols + tid, sSum[tid]);
             }
-            __syncthreads();
-            if (s_i[kAqWarps + 1]) {
-                __threadfence();
-                for (int i = tid; i < n_here * c.d_v; i += kAqThreads) {
-                    const int col = i / c.d_v, dim = i % c.d_v;
-                    float top = -1e30f, l = 0.f, x = 0.f;
-                    for (int p = 0; p < pieces; ++p) {
-                        const float *q = parts + (size_t)(p == 0 ? 2 * first + 1 : 2 * (first + p)) * Lay::kPart;
-                        const float m = __ldcg(q + col), lp = __ldcg(q + Lay::kCols + col), xp = __ldcg(q + 2 * Lay::kCols + col * DP + dim);
-                        const float now = fmaxf(top, m), k0 = ex2_approx(top - now), k1 = ex2_approx(m - now);
-                        top = now;
-                        l = l * k0 + lp * k1;
-                        x = x * k0 + xp * k1;
-                    }
-                    store(col, dim, l != 0.f ? x * kAqUnit<FORMAT> / l : 0.f);
-                }
-            }
+            split_first[n_split] = first;
+            split_pieces[n_split] = pieces;
+            split_b[n_split] = at.b;
+            split_unit[n_split] = at.unit;
+            ++n_split;
         }
-        __syncthreads();                                        // the ring's memory may be written again
+        at.advance(c, a.B, cap, units, end);
+        if (at.at >= end) break;
+        __syncthreads();                                        // the results have been read
+    }
+    if (n_split == 0) return;
 
-        pos += n_steps;
-        if (pos == base + (long long)units * steps) {
-            base = pos;
-            ++b;
+    // ---- units of several CTAs: whoever brings the last piece joins them, in the order of the pieces ----
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    float *const sF = reinterpret_cast<float *>(aq_raw);        // [col][kAqMaxParts]
+    __threadfence();
+    __syncthreads();
+    if (tid < n_split) {
+        const int first = tid ? split_first[1] : split_first[0], pieces = tid ? split_pieces[1] : split_pieces[0];
+        const unsigned seen = atomicAdd(tickets + first, 1u);
+        s_i[tid] = seen == (unsigned)pieces - 1;
+        if (seen == (unsigned)pieces - 1) tickets[first] = 0u;  // all pieces are in: ready for the next launch
+    }
+    __syncthreads();
+    for (int u = 0; u < n_split; ++u) {
+        if (!s_i[u]) continue;
+        __threadfence();
+        const int first = u ? split_first[1] : split_first[0], pieces = u ? split_pieces[1] : split_pieces[0];
+        const int b = u ? split_b[1] : split_b[0], unit = u ? split_unit[1] : split_unit[0];
+        const float *const head = parts + (size_t)(2 * first + 1) * Lay::kPart, *const rest = parts + (size_t)2 * first * Lay::kPart;
+        auto piece = [&](int p) { return p == 0 ? head : rest + (size_t)2 * p * Lay::kPart; };
+        __syncthreads();
+        for (int col = warp; col < Lay::kCols; col += kAqWarps) {           // a warp's lanes over the pieces of a column
+            float m[kAqMaxParts / 32], l = 0.f, top = -1e30f;
+#pragma unroll
+            for (int i = 0; i < kAqMaxParts / 32; ++i) {
+                m[i] = lane + 32 * i < pieces ? __ldcg(piece(lane + 32 * i) + col) : -1e30f;
+                top = fmaxf(top, m[i]);
+            }
+#pragma unroll
+            for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
+#pragma unroll
+            for (int i = 0; i < kAqMaxParts / 32; ++i)
+                if (lane + 32 * i < pieces) {
+                    const float k = ex2_approx(m[i] - top);
+                    sF[col * kAqMaxParts + lane + 32 * i] = k;
+                    l = fmaf(k, __ldcg(piece(lane + 32 * i) + Lay::kCols + col), l);
+                }
+#pragma unroll
+            for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
+            if (lane == 0) sSum[col] = l;
+        }
+        __syncthreads();
+        const int n_here = min(Lay::kCols, n_cols - unit % groups * Lay::kCols) * quads;
+        for (int i = tid; i < n_here; i += kAqThreads) {
+            const int col = i / quads, quad = i % quads, off = 2 * Lay::kCols + col * DP + quad * 4;
+            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int p0 = 0; p0 < pieces; p0 += 4) {
+                float4 y[4];
+#pragma unroll
+                for (int p = 0; p < 4; ++p)
+                    if (p0 + p < pieces) y[p] = __ldcg(reinterpret_cast<const float4 *>(piece(p0 + p) + off));
+#pragma unroll
+                for (int p = 0; p < 4; ++p)
+                    if (p0 + p < pieces) add(x, sF[col * kAqMaxParts + p0 + p], y[p]);
+            }
+            store(b, unit, col, quad, x, sSum[col]);
         }
     }
 }
 
-template <int FORMAT, int DP, int NT>
+template <int FORMAT, int DP, int NT, bool PACK, bool EXACT>
 lookat_status launch_aq(Ctx *ctx, const Q8AttendArgs &a)
 {
-    using Lay = AqLayout<DP, NT>;
-    auto kern = attend_q8_kernel<FORMAT, DP, NT>;
+    using Lay = AqLayout<DP, NT, PACK>;
+    auto kern = attend_q8_kernel<FORMAT, DP, NT, PACK, EXACT>;
     static int resident[64];                                    // CTAs per SM, by device (0: not asked yet)
     int &per_sm = resident[ctx->device & 63];
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kBytes) != cudaSuccess)
@@ -501,6 +659,7 @@ lookat_status launch_aq(Ctx *ctx, const Q8AttendArgs &a)
     const long long most = (long long)a.B * a.c.H_kv * ((n_cols + Lay::kCols - 1) / Lay::kCols) *
                            ((((long long)a.c.max_pages << a.c.page_shift) + kAqTile - 1) / kAqTile);
     const long long full = (long long)ctx->sm_count * per_sm;
+    if (most / full > (1ll << 29)) return set_error(ctx, LOOKAT_ERR_UNSUPPORTED, "attend_q8: too many tokens for one call");
     const unsigned grid = (unsigned)(most < full ? most : full);
     lookat_status st = workspace(ctx, ctx->q8_partials, (size_t)full * 2 * Lay::kPart * sizeof(float), false, "attend_q8");
     if (st == LOOKAT_OK) st = workspace(ctx, ctx->q8_tickets, (size_t)ctx->sm_count * 16 * sizeof(unsigned), true, "attend_q8");
@@ -509,14 +668,26 @@ lookat_status launch_aq(Ctx *ctx, const Q8AttendArgs &a)
     return check_launch(ctx, "attend_q8_kernel");
 }
 
+// columns of a unit: 4 where that is all there are (the two halves of the weights then share the 8 columns of a product),
+// 8, or 16
+template <int FORMAT, int DP, bool EXACT>
+lookat_status launch_aq_cols(Ctx *ctx, const Q8AttendArgs &a)
+{
+    const long long n = (long long)a.g * a.L_q;
+    if (n <= 4) return launch_aq<FORMAT, DP, 1, true, EXACT>(ctx, a);
+    if constexpr (DP <= 128)
+        if (n > 8) return launch_aq<FORMAT, DP, 2, false, EXACT>(ctx, a);
+    return launch_aq<FORMAT, DP, 1, false, EXACT>(ctx, a);
+}
+
+// head dims: 64 and 128 as they are, others padded to 128 or 256
 template <int FORMAT>
 lookat_status launch_aq_dims(Ctx *ctx, const Q8AttendArgs &a)
 {
-    const int d = a.c.d_k > a.c.d_v ? a.c.d_k : a.c.d_v;
-    const bool wide = (long long)a.g * a.L_q > 8;
-    if (d <= 64) return wide ? launch_aq<FORMAT, 64, 2>(ctx, a) : launch_aq<FORMAT, 64, 1>(ctx, a);
-    if (d <= 128) return wide ? launch_aq<FORMAT, 128, 2>(ctx, a) : launch_aq<FORMAT, 128, 1>(ctx, a);
-    return launch_aq<FORMAT, 256, 1>(ctx, a);
+    const int dk = a.c.d_k, dv = a.c.d_v;
+    if (dk == 64 && dv == 64) return launch_aq_cols<FORMAT, 64, true>(ctx, a);
+    if (dk == 128 && dv == 128) return launch_aq_cols<FORMAT, 128, true>(ctx, a);
+    return dk <= 128 && dv <= 128 ? launch_aq_cols<FORMAT, 128, false>(ctx, a) : launch_aq_cols<FORMAT, 256, false>(ctx, a);
 }
 
 }  // namespace
