@@ -69,36 +69,6 @@ __device__ __forceinline__ uint32_t aq_transpose(uint32_t x)
     return y;
 }
 
-// Four stored numbers as two pairs of fp16 numbers.  int8: with the sign bit flipped a byte u stands for u - 128, and the
-// half 0x6400 + u is 1024 + u, so one exact subtraction gives n.  e4m3: the bits moved into an fp16's places (2^8 too
-// small; kAqUnit makes up for it).
-template <int FORMAT>
-__device__ __forceinline__ void aq_pairs(uint32_t w, uint32_t &lo, uint32_t &hi)       // bytes 0,1 and 2,3
-{
-    if constexpr (FORMAT == LOOKAT_Q8_INT8) {
-        const uint32_t u = w ^ 0x80808080u;
-        const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
-        const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));   // 1152
-        const __half2 x = __hsub2(*reinterpret_cast<const __half2 *>(&a), off), y = __hsub2(*reinterpret_cast<const __half2 *>(&b), off);
-        lo = *reinterpret_cast<const uint32_t *>(&x);
-        hi = *reinterpret_cast<const uint32_t *>(&y);
-    } else {
-#ifdef AQ_BITS
-        const uint32_t a = __byte_perm(w, 0u, 0x1404), b = __byte_perm(w, 0u, 0x3424);
-        lo = ((a >> 1) & 0x3f803f80u) | (a & 0x80008000u);
-        hi = ((b >> 1) & 0x3f803f80u) | (b & 0x80008000u);
-#else
-        asm("{\n.reg .b16 x, y;\nmov.b32 {x, y}, %2;\ncvt.rn.f16x2.e4m3x2 %0, x;\ncvt.rn.f16x2.e4m3x2 %1, y;\n}" : "=r"(lo), "=r"(hi) : "r"(w));
-#endif
-    }
-}
-template <int FORMAT>
-#ifdef AQ_BITS
-constexpr float kAqUnit = FORMAT == LOOKAT_Q8_INT8 ? 1.f / kQ8RangeInt8 : 256.f / kQ8RangeE4m3;   // value of a fp16 number per amax
-#else
-constexpr float kAqUnit = 1.f / (FORMAT == LOOKAT_Q8_INT8 ? kQ8RangeInt8 : kQ8RangeE4m3);
-#endif
-
 // Where the 16-byte pieces of a tile's rows lie: a row of 64, 128 or 256 bytes after the other as in the cache, the pieces
 // of row r permuted by XOR with aq_turn(r) within their 128 bytes.  The copies are then linear (512 consecutive bytes per
 // warp instruction: reading every other row instead cost a quarter of the bandwidth), and each quarter-warp's reads below
@@ -250,7 +220,7 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
     auto results = [&](int w, int n) {
         return reinterpret_cast<float *>(Lay::kInRing ? aq_raw + (w * kAqStages + n % kAqStages) * Lay::kStage : aq_raw + Lay::kRing + w * (Lay::kCols * DP * 4));
     };
-    const float k_unit = kAqUnit<FORMAT> * a.scale_log2;
+    const float k_unit = kQ8Unit<FORMAT> * a.scale_log2;
 
     // ---- the ring runs ahead of the products, over the borders of units; this warp's tile of a step holds tokens
     //      step * 64 + warp * 16 .. + 15 of the row ----
@@ -316,7 +286,7 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
     const int quads = d_v / 4;
     auto store = [&](int b, int unit, int col, int quad, float4 x, float l) {       // o = O / (R l); nothing seen: zeros
         const int cc = unit % groups * Lay::kCols + col;
-        const float r = l != 0.f ? kAqUnit<FORMAT> / l : 0.f;
+        const float r = l != 0.f ? kQ8Unit<FORMAT> / l : 0.f;
         const size_t to = (((size_t)b * a.H_q + unit / groups * a.g + cc % a.g) * a.L_q + cc / a.g) * d_v + quad * 4;
         x = make_float4(x.x * r, x.y * r, x.z * r, x.w * r);
         if (a.out_fp16) {
@@ -388,8 +358,8 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     uint32_t a0, a1, a2, a3;
-                    aq_pairs<FORMAT>(xw[w], a0, a2);
-                    aq_pairs<FORMAT>(yw[w], a1, a3);
+                    q8_pairs<FORMAT>(xw[w], a0, a2);
+                    q8_pairs<FORMAT>(yw[w], a1, a3);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         float (&dst)[4] = (w & 1) ? sd[nt] : sc[nt];
@@ -475,10 +445,10 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
                 for (int w = 0; w < VB / 4; ++w) {
                     // bytes of two tokens side by side: dims 4w, 4w + 1 and dims 4w + 2, 4w + 3
                     uint32_t x0, x1, x2, x3, y0, y1, y2, y3;
-                    aq_pairs<FORMAT>(__byte_perm(r[0][w], r[1][w], 0x5140), x0, x1);        // tokens 2t, 2t + 1
-                    aq_pairs<FORMAT>(__byte_perm(r[0][w], r[1][w], 0x7362), x2, x3);
-                    aq_pairs<FORMAT>(__byte_perm(r[2][w], r[3][w], 0x5140), y0, y1);        // tokens 2t + 8, 2t + 9
-                    aq_pairs<FORMAT>(__byte_perm(r[2][w], r[3][w], 0x7362), y2, y3);
+                    q8_pairs<FORMAT>(__byte_perm(r[0][w], r[1][w], 0x5140), x0, x1);        // tokens 2t, 2t + 1
+                    q8_pairs<FORMAT>(__byte_perm(r[0][w], r[1][w], 0x7362), x2, x3);
+                    q8_pairs<FORMAT>(__byte_perm(r[2][w], r[3][w], 0x5140), y0, y1);        // tokens 2t + 8, 2t + 9
+                    q8_pairs<FORMAT>(__byte_perm(r[2][w], r[3][w], 0x7362), y2, y3);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -647,9 +617,9 @@ lookat_status launch_aq(Ctx *ctx, const Q8AttendArgs &a)
     auto kern = attend_q8_kernel<FORMAT, DP, NT, PACK, EXACT>;
     static int resident[64];                                    // CTAs per SM, by device (0: not asked yet)
     int &per_sm = resident[ctx->device & 63];
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kBytes) != cudaSuccess)
-        return check_launch(ctx, "attend_q8: shared-memory opt-in");
     if (!per_sm) {
+        if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kBytes) != cudaSuccess)
+            return check_launch(ctx, "attend_q8: shared-memory opt-in");
         int n = 0;
         if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kern, kAqThreads, Lay::kBytes) != cudaSuccess || n < 1)
             return check_launch(ctx, "attend_q8: occupancy");
@@ -695,6 +665,7 @@ lookat_status launch_aq_dims(Ctx *ctx, const Q8AttendArgs &a)
 lookat_status launch_attend_q8(Ctx *ctx, const Q8AttendArgs &a)
 {
     if ((long long)a.H_q * a.L_q > (1ll << 30)) return set_error(ctx, LOOKAT_ERR_UNSUPPORTED, "attend_q8: more than 2^30 queries per row");
+    if (attend_q8_umma_covers(ctx, a)) return launch_attend_q8_umma(ctx, a);
     return a.format == LOOKAT_Q8_INT8 ? launch_aq_dims<LOOKAT_Q8_INT8>(ctx, a) : launch_aq_dims<LOOKAT_Q8_E4M3>(ctx, a);
 }
 

@@ -45,6 +45,9 @@ struct Q8AttendArgs {
     float scale_log2;               // softmax scale * log2(e)
 };
 lookat_status launch_attend_q8(Ctx *ctx, const Q8AttendArgs &a);
+// prompts and pieces of them, on tcgen05 (attend_q8_umma.cu)
+bool attend_q8_umma_covers(const Ctx *ctx, const Q8AttendArgs &a);
+lookat_status launch_attend_q8_umma(Ctx *ctx, const Q8AttendArgs &a);
 
 // Scratch of at least `bytes` (zeroed when it is new, if asked).  Grows by allocating anew; the old buffer stays until the
 // context is destroyed, because a captured graph may still name it.  Refuses to allocate while the stream is captured.
@@ -73,5 +76,26 @@ __device__ __forceinline__ float q8_value(uint32_t byte)
         return __half2float(__ushort_as_half((unsigned short)h)) * 256.f;
     }
 }
+
+// Four stored numbers as two pairs of fp16 numbers, in order.  int8: with the sign bit flipped a byte u stands for u - 128,
+// and the half 0x6400 + u is 1024 + u, so one exact subtraction gives n (5 instructions per 4 numbers).  e4m3: the
+// conversion instruction (moving the bits into an fp16's places by hand takes 8 instructions; the attention kernel ran
+// 3 % slower with it).  A NaN stays one.
+template <int FORMAT>
+__device__ __forceinline__ void q8_pairs(uint32_t w, uint32_t &lo, uint32_t &hi)       // bytes 0, 1 and 2, 3
+{
+    if constexpr (FORMAT == LOOKAT_Q8_INT8) {
+        const uint32_t u = w ^ 0x80808080u;
+        const uint32_t a = __byte_perm(u, 0x64646464u, 0x4140), b = __byte_perm(u, 0x64646464u, 0x4342);
+        const __half2 off = __halves2half2(__ushort_as_half(0x6480), __ushort_as_half(0x6480));   // 1152
+        const __half2 x = __hsub2(*reinterpret_cast<const __half2 *>(&a), off), y = __hsub2(*reinterpret_cast<const __half2 *>(&b), off);
+        lo = *reinterpret_cast<const uint32_t *>(&x);
+        hi = *reinterpret_cast<const uint32_t *>(&y);
+    } else {
+        asm("{\n.reg .b16 x, y;\nmov.b32 {x, y}, %2;\ncvt.rn.f16x2.e4m3x2 %0, x;\ncvt.rn.f16x2.e4m3x2 %1, y;\n}" : "=r"(lo), "=r"(hi) : "r"(w));
+    }
+}
+template <int FORMAT>
+constexpr float kQ8Unit = 1.f / (FORMAT == LOOKAT_Q8_INT8 ? kQ8RangeInt8 : kQ8RangeE4m3);      // value of a number per amax
 
 }  // namespace lookat

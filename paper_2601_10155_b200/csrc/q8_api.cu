@@ -161,6 +161,10 @@ lookat_status lookat_attend_q8(lookat_ctx *handle, const lookat_q8_cache *cache,
     Q8AttendArgs a;
     memset(&a, 0, sizeof(a));
     Q8_TRY(view_of(ctx, cache, B, tables, max_pages, seq_lens, &a.c));
+    if (ctx->timeout_flag && *(volatile int *)ctx->timeout_flag) {
+        *(volatile int *)ctx->timeout_flag = 0;
+        return set_error(ctx, LOOKAT_ERR_TIMEOUT, "an earlier attention kernel gave up a bounded barrier wait; its output is not valid");
+    }
     if (L_q < 1 || L_q > (1 << 20)) return set_error(ctx, LOOKAT_ERR_INVALID_ARG, "L_q=%d out of range 1..2^20", (int)L_q);
     if (out_fp16 != 0 && out_fp16 != 1) return set_error(ctx, LOOKAT_ERR_INVALID_ARG, "out_fp16=%d is not 0 or 1", (int)out_fp16);
     Q8_TRY(need(ctx, q, "q"));
