@@ -310,7 +310,7 @@ void lookat_destroy(lookat_ctx *handle)
                     ctx->step_q,  ctx->step_k,  ctx->step_out};
     for (void *p : bufs)
         if (p) cudaFree(p);
-    for (Workspace *w : {&ctx->q8_partials, &ctx->q8_tickets, &ctx->page_lists, &ctx->page_marks}) {
+    for (Workspace *w : {&ctx->q8_partials, &ctx->q8_tickets, &ctx->q8_pieces, &ctx->page_lists, &ctx->page_marks}) {
         if (w->ptr) cudaFree(w->ptr);
         for (int i = 0; i < w->n_outgrown; ++i) cudaFree(w->outgrown[i]);
     }

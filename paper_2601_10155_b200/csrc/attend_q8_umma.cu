@@ -10,13 +10,16 @@
 // lie in the scores' second half of tensor memory, and move O out of tensor memory every 16 chunks: the tensor pipe cuts
 // its sums off, and a chain of 16 chunks stays below 2^-20.
 //
-// A CTA works on two tiles of 128 rows against the same chunks of 64 tokens: while the softmax threads of one tile work,
-// the tensor pipe has the other tile's products.  Roles (13 warps, one CTA per SM by tensor memory):
+// A CTA works on two tiles of 128 rows against the same chunks of 64 tokens.  The scores of a tile have two buffers in
+// tensor memory, so the tensor pipe makes the next chunk's while the softmax threads work on this one's.  Roles (14 warps,
+// one CTA per SM by tensor memory):
 //   warps 0-3 / 4-7  softmax of tile 0 / 1: thread r owns row r of its tile = tensor-memory lane r;
 //   warps 8-11  producers: the next chunk's keys and values from the pages to fp16 operand rows in shared memory (128-byte
 //               swizzle), a chunk's loads issued before the wait for its buffer;
-//   warp 12     one thread issues every MMA and commits them to mbarriers.
-// Tensor memory (512 columns): per tile S (64; the weights overwrite it), O (d_v), Q (d_k / 2).
+//   warps 12, 13  one thread each issues the MMAs of tile 0 / 1 and commits them to mbarriers.
+// Tensor memory (512 columns): per tile S (2 x 64; the weights overwrite it) and O (d_v).  Q lies in shared memory.
+//   Few rows over a long cache are cut along the tokens (blockIdx), every piece leaves O, M and l in the workspace and
+// attend_q8_join_kernel joins them in order.
 // Every mbarrier wait gives up after a bounded number of polls, raises the context's time-out flag and lets the CTA drain
 // and free its tensor memory.
 #include "q8.cuh"
@@ -26,10 +29,11 @@ namespace lookat {
 
 namespace {
 
-constexpr int kPqRows = 128, kPqChunk = 64, kPqTiles = 2;
-constexpr int kPqSoftmax = kPqTiles * kPqRows, kPqProducers = 128, kPqThreads = kPqSoftmax + kPqProducers + 32;
+constexpr int kPqRows = 128, kPqChunk = 64, kPqTiles = 2, kPqBoth = kPqTiles * kPqRows;
+constexpr int kPqSoftmax = kPqBoth, kPqProducers = 128, kPqThreads = kPqSoftmax + kPqProducers + 32 * kPqTiles;
 constexpr int kPqGroups = kPqChunk / 16;        // groups of 16 tokens: a page holds whole ones
 constexpr int kPqFlush = 16;                    // chunks that O stays in tensor memory for fp32 results
+constexpr int kPqMinPiece = 8;                  // chunks below which a row's tokens are not cut further
 constexpr float kPqSlack = 8.f;
 
 struct PqMeta {                                 // of 16 tokens: y = s * ks + le - M, l += w * inv
@@ -39,20 +43,48 @@ struct PqMeta {                                 // of 16 tokens: y = s * ks + le
 template <int DK, int DV>
 struct PqLayout {
     static constexpr int kKb = DK / 64, kNb = DV / 64;
-    static constexpr int kKeys = kKb * kPqChunk * 128, kV = kNb * kPqChunk * 128;   // [64 dims each][token][128 B]
-    static constexpr int kOffKeys = 0, kOffV = 2 * kKeys, kOffMeta = kOffV + 2 * kV;
+    static constexpr int kKeys = kKb * kPqChunk * 128, kV = kNb * kPqChunk * 128, kQ = kKb * kPqRows * 128;     // [64 dims each][row][128 B]
+    static constexpr int kOffKeys = 0, kOffV = 2 * kKeys, kOffQ = kOffV + 2 * kV, kOffMeta = kOffQ + kPqTiles * kQ;
     static constexpr int kOffBars = kOffMeta + 4 * kPqGroups * (int)sizeof(PqMeta);
     static constexpr int kBytes = kOffBars + 256;
-    static constexpr int kColO = kPqTiles * kPqChunk, kColQ = kColO + kPqTiles * DV;
-    static constexpr int kTmemCols = kColQ + kPqTiles * (DK / 2) <= 256 ? 256 : 512;
-    static_assert(kColQ + kPqTiles * (DK / 2) <= 512, "tensor memory");
+    static constexpr int kColO = kPqTiles * 2 * kPqChunk;
+    static_assert(kColO + kPqTiles * DV <= 512, "tensor memory");
     // instruction descriptors: fp32 accumulate, fp16 operands, N >> 3 at bit 17, M >> 4 at bit 24; bit 16: B is MN-major
     static constexpr uint32_t kIdescS = (1u << 4) | ((uint32_t)(kPqChunk >> 3) << 17) | ((uint32_t)(kPqRows >> 4) << 24);
     static constexpr uint32_t kIdescO = (1u << 4) | (1u << 16) | ((uint32_t)(DV >> 3) << 17) | ((uint32_t)(kPqRows >> 4) << 24);
+    static constexpr int kPart = kPqBoth * (DV + 2);            // floats of a piece: O [row][DV], then M [row], l [row]
 };
 
+__device__ __forceinline__ float2 pq_fma2(float2 a, float b, float c)           // a * b + c, both halves in one instruction
+{
+    float2 d;
+    asm("{\n.reg .b64 u, v, w, r;\nmov.b64 u, {%2, %3};\nmov.b64 v, {%4, %4};\nmov.b64 w, {%5, %5};\nfma.rn.f32x2 r, u, v, w;\nmov.b64 {%0, %1}, r;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float2 pq_add2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n.reg .b64 u, v, r;\nmov.b64 u, {%2, %3};\nmov.b64 v, {%4, %5};\nadd.rn.f32x2 r, u, v;\nmov.b64 {%0, %1}, r;\n}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+__device__ __forceinline__ float pq_max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
+// Where row `row` of KV head h of batch row b stands in q and in the result.
+__device__ __forceinline__ size_t pq_out_row(const Q8AttendArgs &a, int b, int h, int row)
+{
+    return ((size_t)b * a.H_q + h * a.g + row % a.g) * a.L_q + row / a.g;
+}
+
 template <int FORMAT, int DK, int DV, bool FULL>      // FULL: fp32 results
-__global__ void __launch_bounds__(kPqThreads, 1) attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag)
+__global__ void __launch_bounds__(kPqThreads, 1)
+attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_super, int pieces, float *__restrict__ parts)
 {
     using Lay = PqLayout<DK, DV>;
     extern __shared__ __align__(1024) unsigned char pq_raw[];
@@ -61,26 +93,35 @@ __global__ void __launch_bounds__(kPqThreads, 1) attend_q8_umma_kernel(Q8AttendA
     PqMeta *const meta = reinterpret_cast<PqMeta *>(sm + Lay::kOffMeta);             // [chunk & 3][group]
     uint64_t *const bars = reinterpret_cast<uint64_t *>(sm + Lay::kOffBars);
     uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(bars + 24);
-    // k_ready[buf], v_ready[buf]; per tile s_full[t][buf] (scores done), pv_done[t][buf] (value MMA done), p_ready[t];
-    // meta_ready[chunk & 3]
+    // k_ready[buf], v_ready[buf]; per tile s_full[t][buf] (scores done), pv_done[t][buf] (value MMA done), p_ready[t][buf]
+    // (weights stored); meta_ready[chunk & 3].  A phase of each can only end after every waiter of the one before has
+    // moved on, so waits by parity are safe.
     const uint32_t bar0 = um_smem(bars);
-    const uint32_t bar_k = bar0, bar_v = bar0 + 16, bar_s = bar0 + 32, bar_pv = bar0 + 64, bar_p = bar0 + 96, bar_m = bar0 + 112;
+    const uint32_t bar_k = bar0, bar_v = bar0 + 16, bar_s = bar0 + 32, bar_pv = bar0 + 64, bar_p = bar0 + 96, bar_m = bar0 + 128;
 
     const Q8View &c = a.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int n_rows = a.g * a.L_q, h = blockIdx.y, b = blockIdx.z;
-    const int row0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * (kPqTiles * kPqRows);  // longest first
+    const int n_rows = a.g * a.L_q;
+    // heads and batch rows first, then the pieces, then the row tiles, longest first: the last CTAs to start are short ones
+    const int h = blockIdx.x % c.H_kv, b = blockIdx.x / c.H_kv % a.B, piece = blockIdx.x / (c.H_kv * a.B) % pieces;
+    const int super = n_super - 1 - blockIdx.x / (c.H_kv * a.B * pieces), row0 = super * kPqBoth;
     const int page = 1 << c.page_shift, cap = c.max_pages << c.page_shift;
     const int len_in = c.seq_lens[b], len = min(max(len_in, 0), cap);
     if (tid == 0 && len != len_in && h == 0) q8_report(c.status, kStatusBadPage);
-    const int t_end = len - a.L_q + (min(row0 + kPqTiles * kPqRows, n_rows) - 1) / a.g + 1;      // tokens the CTA's last row sees
-    const int n_chunks = (t_end + kPqChunk - 1) / kPqChunk;
-    auto out_row = [&](int row) { return (((size_t)b * a.H_q + h * a.g + row % a.g) * a.L_q + row / a.g); };
+    const int t_end = len - a.L_q + (min(row0 + kPqBoth, n_rows) - 1) / a.g + 1;     // tokens the CTA's last row sees
+    const int all_chunks = max(0, (t_end + kPqChunk - 1) / kPqChunk), per_piece = (all_chunks + pieces - 1) / pieces;
+    const int chunk0 = piece * per_piece, n_chunks = max(0, min(per_piece, all_chunks - chunk0));
+    float *const part = parts + (pieces > 1 ? (((size_t)super * a.B + b) * c.H_kv + h) * pieces + piece : 0) * Lay::kPart;
 
-    if (t_end <= 0) {                                          // nothing to see for any row here
+    if (n_chunks == 0) {                                       // nothing to see for any row here
+        if (pieces > 1) {
+            for (int i = tid; i < kPqBoth; i += kPqThreads) part[kPqBoth * (DV + 1) + i] = 0.f;
+            return;
+        }
         const int quads = DV * (a.out_fp16 ? 2 : 4) / 16;
-        for (int i = tid; i < min(kPqTiles * kPqRows, n_rows - row0) * quads; i += kPqThreads)
-            *reinterpret_cast<uint4 *>(static_cast<char *>(a.out) + (out_row(row0 + i / quads) * quads + i % quads) * 16) = make_uint4(0u, 0u, 0u, 0u);
+        for (int i = tid; i < min(kPqBoth, n_rows - row0) * quads; i += kPqThreads)
+            *reinterpret_cast<uint4 *>(static_cast<char *>(a.out) + (pq_out_row(a, b, h, row0 + i / quads) * quads + i % quads) * 16) =
+                make_uint4(0u, 0u, 0u, 0u);
         return;
     }
 
@@ -91,15 +132,24 @@ __global__ void __launch_bounds__(kPqThreads, 1) attend_q8_umma_kernel(Q8AttendA
             for (int t = 0; t < kPqTiles; ++t) {
                 um_bar_init(bar_s + 16 * t + 8 * i, 1);
                 um_bar_init(bar_pv + 16 * t + 8 * i, 1);
+                um_bar_init(bar_p + 16 * t + 8 * i, kPqRows);
             }
-            um_bar_init(bar_p + 8 * i, kPqRows);               // i as the tile index here
         }
         for (int i = 0; i < 4; ++i) um_bar_init(bar_m + 8 * i, kPqGroups);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(um_smem(tmem_slot)), "n"(Lay::kTmemCols) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(um_smem(tmem_slot)), "n"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    // ---- the query rows, A operand of the scores: row r of a tile, 64 dims each, 128-byte swizzle ----
+    if (warp < kPqSoftmax / 32) {
+        const int t = warp >> 2, r = (warp & 3) * 32 + lane, row = min(row0 + t * kPqRows + r, n_rows - 1);  // rows beyond the last repeat it
+        const uint4 *src = reinterpret_cast<const uint4 *>(a.q + pq_out_row(a, b, h, row) * DK);
+#pragma unroll
+        for (int i = 0; i < DK / 8; ++i)
+            *reinterpret_cast<uint4 *>(sm + Lay::kOffQ + t * Lay::kQ + (i >> 3) * (kPqRows * 128) + r * 128 + (((i & 7) ^ (r & 7)) << 4)) = __ldg(src + i);
+        um_fence_async_smem();
     }
     um_fence_before();
     __syncthreads();
@@ -107,95 +157,60 @@ __global__ void __launch_bounds__(kPqThreads, 1) attend_q8_umma_kernel(Q8AttendA
     const uint32_t tmem = *tmem_slot;
     bool dead = (sm0 & 1023u) != 0;                            // a wait ran out (or the base is misaligned): leave, free, return
 
-    // ---- the query rows to tensor memory, the A operand of the scores: lane r = row r, two halves per column ----
-    if (warp < kPqSoftmax / 32) {
-        const int t = warp >> 2, row = min(row0 + t * kPqRows + (warp & 3) * 32 + lane, n_rows - 1);     // rows beyond the last repeat it
-        const uint4 *src = reinterpret_cast<const uint4 *>(a.q + out_row(row) * DK);
-#pragma unroll
-        for (int part = 0; part < DK / 64; ++part) {
-            uint32_t w[32];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint4 x = __ldg(src + part * 8 + i);
-                w[4 * i] = x.x;
-                w[4 * i + 1] = x.y;
-                w[4 * i + 2] = x.z;
-                w[4 * i + 3] = x.w;
-            }
-            um_st32(tmem + Lay::kColQ + t * (DK / 2) + part * 32 + ((uint32_t)((warp & 3) * 32) << 16), w);
-        }
-        um_wait_st();
-    }
-    um_fence_before();
-    __syncthreads();
-    um_fence_after();
-
     if (dead) {
         // misaligned shared-memory base: nothing runs
-    } else if (warp == (kPqSoftmax + kPqProducers) / 32) {
-        // =================== the MMA thread ===================
+    } else if (warp >= (kPqSoftmax + kPqProducers) / 32) {
+        // =================== the MMA thread of a tile ===================
         if (lane == 0) {
+            const int t = warp - (kPqSoftmax + kPqProducers) / 32;
             // descriptors: stride 1024 B, version 1, 128-byte swizzle in the high word; start address and leading offset in
             // the low word
             const uint32_t desc_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
             const uint32_t keys_lo = ((sm0 + Lay::kOffKeys) >> 4) | (1u << 16);                    // leading offset unused (16 B)
+            const uint32_t q_lo = ((sm0 + Lay::kOffQ + t * Lay::kQ) >> 4) | (1u << 16);
             const uint32_t v_lo = ((sm0 + Lay::kOffV) >> 4) | ((uint32_t)(kPqChunk * 128 / 16) << 16);   // between 64-column blocks
-            auto score_mma = [&](int t, int ch) {
+            const uint32_t tm_s = tmem + t * 2 * kPqChunk, tm_o = tmem + Lay::kColO + t * DV;
+            auto score_mma = [&](int ch) {                     // into the buffer that the weights of chunk ch - 2 lay in
                 const int buf = ch & 1;
-                const uint32_t lo = keys_lo + buf * (Lay::kKeys >> 4), d = tmem + t * kPqChunk, q = tmem + Lay::kColQ + t * (DK / 2);
+                if (!um_bar_wait(bar_k + 8 * buf, (ch >> 1) & 1)) return false;
+                um_fence_after();
+                const uint32_t lo = keys_lo + buf * (Lay::kKeys >> 4), d = tm_s + buf * kPqChunk;
 #pragma unroll
                 for (int ks = 0; ks < DK / 16; ++ks) {
-                    const uint32_t off = ((ks >> 2) * (kPqChunk * 128) + (ks & 3) * 32) >> 4;
-                    if (ks == 0) um_mma_ts<false>(d, q + ks * 8, lo + off, desc_hi, Lay::kIdescS);
-                    else um_mma_ts<true>(d, q + ks * 8, lo + off, desc_hi, Lay::kIdescS);
+                    const uint32_t qo = ((ks >> 2) * (kPqRows * 128) + (ks & 3) * 32) >> 4, ko = ((ks >> 2) * (kPqChunk * 128) + (ks & 3) * 32) >> 4;
+                    if (ks == 0) um_mma_ss<false>(d, q_lo + qo, desc_hi, lo + ko, desc_hi, Lay::kIdescS);
+                    else um_mma_ss<true>(d, q_lo + qo, desc_hi, lo + ko, desc_hi, Lay::kIdescS);
                 }
                 um_commit(bar_s + 16 * t + 8 * buf);
+                return true;
             };
-            auto value_mma = [&](int t, int ch) {              // the weights lie over S(t): first halves, then (FULL) second ones
+            auto value_mma = [&](int ch) {                     // weights over the scores: first halves, then (FULL) second ones
                 const int buf = ch & 1;
-                const uint32_t lo = v_lo + buf * (Lay::kV >> 4), pa = tmem + t * kPqChunk, d = tmem + Lay::kColO + t * DV;
+                if (!um_bar_wait(bar_p + 16 * t + 8 * buf, (ch >> 1) & 1) || !um_bar_wait(bar_v + 8 * buf, (ch >> 1) & 1)) return false;
+                um_fence_after();
+                const uint32_t lo = v_lo + buf * (Lay::kV >> 4), pa = tm_s + buf * kPqChunk;
                 const bool first = FULL ? ch % kPqFlush == 0 : ch == 0;
 #pragma unroll
-                for (int part = 0; part < (FULL ? 2 : 1); ++part)
+                for (int half = 0; half < (FULL ? 2 : 1); ++half)
 #pragma unroll
                     for (int kt = 0; kt < kPqChunk / 16; ++kt) {
-                        if (part == 0 && kt == 0 && first) um_mma_ts<false>(d, pa, lo, desc_hi, Lay::kIdescO);
-                        else um_mma_ts<true>(d, pa + part * 32 + kt * 8, lo + kt * (2048 >> 4), desc_hi, Lay::kIdescO);
+                        if (half == 0 && kt == 0 && first) um_mma_ts<false>(tm_o, pa, lo, desc_hi, Lay::kIdescO);
+                        else um_mma_ts<true>(tm_o, pa + half * 32 + kt * 8, lo + kt * (2048 >> 4), desc_hi, Lay::kIdescO);
                     }
                 um_commit(bar_pv + 16 * t + 8 * buf);
+                return true;
             };
-            // Per tile strictly scores(c) -> [softmax] -> value(c) -> scores(c + 1); the two tiles take turns.
-            int next_qk[kPqTiles] = {0, 0}, next_pv[kPqTiles] = {0, 0};
-            int polls = 0;
-            while (next_pv[0] < n_chunks || next_pv[1] < n_chunks) {
-                bool progress = false;
-#pragma unroll
-                for (int t = 0; t < kPqTiles; ++t) {
-                    const int cp = next_pv[t];
-                    if (cp < next_qk[t] && um_bar_test(bar_p + 8 * t, cp & 1) && um_bar_test(bar_v + 8 * (cp & 1), (cp >> 1) & 1)) {
-                        um_fence_after();
-                        value_mma(t, cp);
-                        next_pv[t] = cp + 1;
-                        progress = true;
-                    }
-                    const int cq = next_qk[t];
-                    if (cq < n_chunks && next_pv[t] == cq && um_bar_test(bar_k + 8 * (cq & 1), (cq >> 1) & 1)) {
-                        um_fence_after();
-                        score_mma(t, cq);
-                        next_qk[t] = cq + 1;
-                        progress = true;
-                    }
-                }
-                if (progress) polls = 0;
-                else if (++polls > kUmPolls) { dead = true; break; }
-            }
+            bool ok = score_mma(0);
+            if (n_chunks > 1) ok = ok && score_mma(1);
+            for (int ch = 0; ok && ch < n_chunks; ++ch) ok = value_mma(ch) && (ch + 2 >= n_chunks || score_mma(ch + 2));
+            dead = !ok;
         }
     } else if (warp >= kPqSoftmax / 32) {
         // =================== producers ===================
         // A warp's item: 8 tokens (an octet; it lies in one page) by 64 dims; lane: token lane & 7, 16 dims lane >> 3.  The
         // stores of 8 lanes then go to 8 different columns of the swizzle.
         const int ptid = tid - kPqSoftmax, pw = ptid >> 5, tl = lane & 7, pl = lane >> 3;
-        constexpr int kItemsK = 8 * Lay::kKb / 4, kItemsV = 8 * Lay::kNb / 4;       // per warp and chunk
+        constexpr int kItemsK = 2 * Lay::kKb, kItemsV = 2 * Lay::kNb;                // per warp and chunk
         const int32_t *table = c.tables + (size_t)b * c.max_pages;
         auto entry_of = [&](int tok) { return tok < len ? __ldg(table + (tok >> c.page_shift)) : -1; };
         auto held = [&](int tok, int p) {                      // reports a bad entry
@@ -209,14 +224,16 @@ __global__ void __launch_bounds__(kPqThreads, 1) attend_q8_umma_kernel(Q8AttendA
         float am_k = 0.f, am_v = 0.f;
         bool meta_there = false;
         auto ask_entries = [&](int ch) {
+            const int tok0 = (chunk0 + ch) * kPqChunk;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) ent[i] = entry_of(ch * kPqChunk + (pw + 4 * i) * 8);
-            ent_meta = entry_of(ch * kPqChunk + (ptid & 3) * 16);
+            for (int i = 0; i < 2; ++i) ent[i] = entry_of(tok0 + (pw + 4 * i) * 8);
+            ent_meta = entry_of(tok0 + (ptid & 3) * 16);
         };
         auto ask_rows = [&](int ch) {                          // zeros behind the row's last token and for bad entries
+            const int tok0 = (chunk0 + ch) * kPqChunk;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const int oct = pw + 4 * i, tok = ch * kPqChunk + oct * 8;
+                const int tok = tok0 + (pw + 4 * i) * 8;
                 const bool ok = held(tok, ent[i]) && tok + tl < len;
                 const size_t row = ok ? ((size_t)ent[i] * c.H_kv + h) * page + ((tok + tl) & (page - 1)) : 0;
 #pragma unroll
@@ -227,7 +244,7 @@ __global__ void __launch_bounds__(kPqThreads, 1) attend_q8_umma_kernel(Q8AttendA
                     rv[i * Lay::kNb + nb] = ok ? __ldg(reinterpret_cast<const uint4 *>(c.v + row * DV + nb * 64 + pl * 16)) : make_uint4(0u, 0u, 0u, 0u);
             }
             if (ptid < kPqGroups) {
-                meta_there = ch * kPqChunk + ptid * 16 < len && ent_meta >= 0 && ent_meta < c.n_pages;
+                meta_there = tok0 + ptid * 16 < len && ent_meta >= 0 && ent_meta < c.n_pages;
                 const size_t block = meta_there ? (size_t)ent_meta * c.H_kv + h : 0;
                 am_k = meta_there ? __ldg(c.k_amax + block) : 0.f;
                 am_v = meta_there ? __ldg(c.v_amax + block) : 0.f;
@@ -255,7 +272,7 @@ __global__ void __launch_bounds__(kPqThreads, 1) attend_q8_umma_kernel(Q8AttendA
                     ok = um_group_wait<1, kPqProducers>(ptid == 0, bar_s + 16 * t + 8 * buf, ((ch - 2) >> 1) & 1) && ok;
                 if (!ok) { dead = true; break; }
             }
-            // (the softmax of chunk ch - 2 may still run, that of ch - 4 is over: its slot is free)
+            // (scores ch - 2 were issued after the value MMA of ch - 4, so the softmax of ch - 4 is over: its slot is free)
             if (ptid < kPqGroups) {
                 PqMeta m;
                 m.ks = am_k * (kQ8Unit<FORMAT> * a.scale_log2);
@@ -290,22 +307,23 @@ __global__ void __launch_bounds__(kPqThreads, 1) attend_q8_umma_kernel(Q8AttendA
         }
     } else {
         // =================== softmax: thread r owns row r of tile t ===================
-        const int t = warp >> 2, rq = warp & 3, row = row0 + t * kPqRows + rq * 32 + lane;
+        const int t = warp >> 2, rq = warp & 3, r = t * kPqRows + rq * 32 + lane, row = row0 + r;
         const bool on = row < n_rows;
         const int vis_end = len - a.L_q + (on ? row : n_rows - 1) / a.g + 1;       // tokens this row sees (may be <= 0)
         const uint32_t lane_base = (uint32_t)(rq * 32) << 16;
-        const uint32_t tm_s = tmem + t * kPqChunk + lane_base, tm_o = tmem + Lay::kColO + t * DV + lane_base;
-        float m_run = 0.f, l_run = 0.f, m_out = 0.f;           // M; m_out: M at the time of what lies in `out`
+        const uint32_t tm_s = tmem + t * 2 * kPqChunk + lane_base, tm_o = tmem + Lay::kColO + t * DV + lane_base;
+        float m_run = 0.f, l_run = 0.f, m_out = 0.f;           // M; m_out: M at the time of what was moved out of tensor memory
         bool set = false;                                      // the row has seen a token
-        // O in tensor memory, and what was moved out before, times `mul`, to the result's row
+        float *const acc = pieces > 1 ? part + (size_t)r * DV : FULL ? static_cast<float *>(a.out) + (on ? pq_out_row(a, b, h, row) * DV : 0) : nullptr;
+        // O in tensor memory, and what was moved out before, times `mul`, to acc
         auto move_out = [&](float mul, bool again) {
             const float old = ex2_approx(m_out - m_run) * mul;
 #pragma unroll 1
-            for (int part = 0; part < DV / 32; ++part) {
+            for (int p = 0; p < DV / 32; ++p) {
                 uint32_t o[32];
-                um_ld32(o, tm_o + part * 32);
+                um_ld32(o, tm_o + p * 32);
                 um_wait_ld();
-                float4 *dst = reinterpret_cast<float4 *>(static_cast<float *>(a.out) + (on ? out_row(row) * DV : 0) + part * 32);
+                float4 *dst = reinterpret_cast<float4 *>(acc + p * 32);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     if (!on) break;
@@ -321,41 +339,53 @@ __global__ void __launch_bounds__(kPqThreads, 1) attend_q8_umma_kernel(Q8AttendA
             }
             m_out = set ? m_run : -1e30f;
         };
+        auto values_done = [&](int ch) {                       // the tile's value MMAs up to chunk ch (warp-uniform)
+            const bool ok = __all_sync(0xffffffffu, um_bar_wait(bar_pv + 16 * t + 8 * (ch & 1), (ch >> 1) & 1));
+            um_fence_after();
+            return ok;
+        };
         for (int ch = 0; ch < n_chunks; ++ch) {
-            const int buf = ch & 1, tok0 = ch * kPqChunk;
+            const int buf = ch & 1, tok0 = (chunk0 + ch) * kPqChunk;
+            const uint32_t tm_sb = tm_s + buf * kPqChunk;
             const bool ok = um_bar_wait(bar_s + 16 * t + 8 * buf, (ch >> 1) & 1) && um_bar_wait(bar_m + 8 * (ch & 3), (ch >> 2) & 1);
             if (!__all_sync(0xffffffffu, ok)) { dead = true; break; }              // warp-uniform
             um_fence_after();
-            // The tile's previous value MMA is complete: the commit behind s_full covers every MMA its thread issued before.
-            if (FULL && ch > 0 && ch % kPqFlush == 0) move_out(1.f, ch > kPqFlush);     // the next value MMA starts from zero
-            float y[kPqChunk];
+            float2 y[kPqChunk / 2];
             {
                 uint32_t s0[32], s1[32];
-                um_ld32(s0, tm_s);
-                um_ld32(s1, tm_s + 32);
+                um_ld32(s0, tm_sb);
+                um_ld32(s1, tm_sb + 32);
                 um_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    y[i] = __uint_as_float(s0[i]);
-                    y[32 + i] = __uint_as_float(s1[i]);
+                for (int i = 0; i < 16; ++i) {
+                    y[i] = make_float2(__uint_as_float(s0[2 * i]), __uint_as_float(s0[2 * i + 1]));
+                    y[16 + i] = make_float2(__uint_as_float(s1[2 * i]), __uint_as_float(s1[2 * i + 1]));
                 }
             }
-            float inv[kPqGroups], top = -INFINITY;
+            if (FULL && ch > 0 && ch % kPqFlush == 0) {        // the next value MMA starts from zero
+                if (!values_done(ch - 1)) { dead = true; break; }
+                move_out(1.f, ch > kPqFlush);
+            }
+            float inv[kPqGroups];
 #pragma unroll
             for (int gr = 0; gr < kPqGroups; ++gr) {
                 const PqMeta m = meta[(ch & 3) * kPqGroups + gr];
                 const float off = m.le - m_run;
                 inv[gr] = m.inv;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) y[gr * 16 + i] = fmaf(y[gr * 16 + i], m.ks, off);
+                for (int i = gr * 8; i < gr * 8 + 8; ++i) y[i] = pq_fma2(y[i], m.ks, off);
             }
             if (tok0 + kPqChunk > vis_end) {                   // the chunk crosses (or lies beyond) this row's causal limit
 #pragma unroll
-                for (int i = 0; i < kPqChunk; ++i)
-                    if (tok0 + i >= vis_end) y[i] = -INFINITY;
+                for (int i = 0; i < kPqChunk / 2; ++i) {
+                    if (tok0 + 2 * i >= vis_end) y[i].x = -INFINITY;
+                    if (tok0 + 2 * i + 1 >= vis_end) y[i].y = -INFINITY;
+                }
             }
+            float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int i = 0; i < kPqChunk; ++i) top = fmaxf(top, y[i]);
+            for (int i = 0; i < kPqChunk / 2; ++i) tops[i & 3] = pq_max3(tops[i & 3], y[i].x, y[i].y);
+            const float top = fmaxf(pq_max3(tops[0], tops[1], tops[2]), tops[3]);
             // M moves only when the scores run ahead of it by more than kPqSlack (base-2 units), or to the first score
             const bool move = top > kPqSlack || (!set && top > -INFINITY);
             float alpha = 1.f;
@@ -364,58 +394,63 @@ __global__ void __launch_bounds__(kPqThreads, 1) attend_q8_umma_kernel(Q8AttendA
                 alpha = set ? ex2_approx(-d) : 1.f;            // (no score so far: O and l are zero)
                 set |= move;
                 m_run += d;
+                const float2 nd = make_float2(-d, -d);
 #pragma unroll
-                for (int i = 0; i < kPqChunk; ++i) y[i] -= d;
+                for (int i = 0; i < kPqChunk / 2; ++i) y[i] = pq_add2(y[i], nd);
             }
             uint32_t pk[32], pl[FULL ? 32 : 1];
             float l = 0.f;
 #pragma unroll
             for (int gr = 0; gr < kPqGroups; ++gr) {
-                float sum = 0.f;
+                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                 for (int i = gr * 8; i < gr * 8 + 8; ++i) {
-                    const float w0 = ex2_approx(y[2 * i]), w1 = ex2_approx(y[2 * i + 1]);
-                    sum += w0 + w1;
-                    const __half2 hi = __floats2half2_rn(w0, w1);
+                    const float2 w = make_float2(ex2_approx(y[i].x), ex2_approx(y[i].y));
+                    sum[i & 1] = pq_add2(sum[i & 1], w);
+                    const __half2 hi = __floats2half2_rn(w.x, w.y);
                     pk[i] = *reinterpret_cast<const uint32_t *>(&hi);
                     if constexpr (FULL) {
                         const float2 hf = __half22float2(hi);
-                        const __half2 lo = __floats2half2_rn(w0 - hf.x, w1 - hf.y);
+                        const __half2 lo = __floats2half2_rn(w.x - hf.x, w.y - hf.y);
                         pl[i] = *reinterpret_cast<const uint32_t *>(&lo);
                     }
                 }
-                l = fmaf(sum, inv[gr], l);
+                l = fmaf((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y), inv[gr], l);
             }
             l_run = fmaf(l_run, alpha, l);
+            um_st32(tm_sb, pk);
+            if constexpr (FULL) um_st32(tm_sb + 32, pl);
             if (ch >= 1 && !(FULL && ch % kPqFlush == 0) && __any_sync(0xffffffffu, alpha != 1.f)) {
+                if (!values_done(ch - 1)) { dead = true; break; }
 #pragma unroll 1
-                for (int part = 0; part < DV / 32; ++part) {
+                for (int p = 0; p < DV / 32; ++p) {
                     uint32_t o[32];
-                    um_ld32(o, tm_o + part * 32);
+                    um_ld32(o, tm_o + p * 32);
                     um_wait_ld();
 #pragma unroll
                     for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                    um_st32(tm_o + part * 32, o);
+                    um_st32(tm_o + p * 32, o);
                 }
             }
-            um_st32(tm_s, pk);
-            if constexpr (FULL) um_st32(tm_s + 32, pl);
             um_wait_st();
             um_fence_before();
-            um_bar_arrive(bar_p + 8 * t);
+            um_bar_arrive(bar_p + 16 * t + 8 * buf);
         }
-        if (!dead && __all_sync(0xffffffffu, um_bar_wait(bar_pv + 16 * t + 8 * ((n_chunks - 1) & 1), ((n_chunks - 1) >> 1) & 1))) {
-            um_fence_after();
-            const float mul = l_run != 0.f ? kQ8Unit<FORMAT> / l_run : 0.f;
-            if constexpr (FULL) {
-                move_out(mul, n_chunks > kPqFlush);
+        if (!dead && values_done(n_chunks - 1)) {
+            const float mul = pieces > 1 ? 1.f : l_run != 0.f ? kQ8Unit<FORMAT> / l_run : 0.f;
+            if (FULL || pieces > 1) {
+                move_out(mul, FULL && n_chunks > kPqFlush);
+                if (pieces > 1) {
+                    part[kPqBoth * DV + r] = m_run;
+                    part[kPqBoth * (DV + 1) + r] = l_run;
+                }
             } else {
 #pragma unroll 1
-                for (int part = 0; part < DV / 32; ++part) {
+                for (int p = 0; p < DV / 32; ++p) {
                     uint32_t o[32];
-                    um_ld32(o, tm_o + part * 32);
+                    um_ld32(o, tm_o + p * 32);
                     um_wait_ld();
-                    uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__half *>(a.out) + (on ? out_row(row) * DV : 0) + part * 32);
+                    uint4 *dst = reinterpret_cast<uint4 *>(static_cast<__half *>(a.out) + (on ? pq_out_row(a, b, h, row) * DV : 0) + p * 32);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         if (!on) break;
@@ -438,21 +473,77 @@ __global__ void __launch_bounds__(kPqThreads, 1) attend_q8_umma_kernel(Q8AttendA
     if (dead) atomicExch(timeout_flag, 1);
     um_fence_before();
     __syncthreads();
-    if (warp == 0)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(Lay::kTmemCols) : "memory");
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(512) : "memory");
+}
+
+// The pieces of rows that were cut along the tokens, one warp per row; a piece without a token for the row has l = 0.
+template <int FORMAT, int DV>
+__global__ void __launch_bounds__(256) attend_q8_join_kernel(Q8AttendArgs a, int n_super, int pieces, const float *__restrict__ parts)
+{
+    constexpr int kPart = kPqBoth * (DV + 2), kEach = DV / 32;
+    const int lane = threadIdx.x & 31;
+    const long long item = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);           // [super][b][h][row of the tiles]
+    const int r = (int)(item % kPqBoth), h = (int)(item / kPqBoth % a.c.H_kv), b = (int)(item / kPqBoth / a.c.H_kv % a.B);
+    const int super = (int)(item / kPqBoth / a.c.H_kv / a.B), row = super * kPqBoth + r;
+    if (super >= n_super || row >= a.g * a.L_q) return;
+    const float *p0 = parts + (((size_t)super * a.B + b) * a.c.H_kv + h) * pieces * kPart;
+    float top = -INFINITY, l = 0.f, o[kEach] = {};
+    for (int p = 0; p < pieces; ++p) {
+        const float lp = p0[(size_t)p * kPart + kPqBoth * (DV + 1) + r];
+        if (lp != 0.f) top = fmaxf(top, p0[(size_t)p * kPart + kPqBoth * DV + r]);
+    }
+    for (int p = 0; p < pieces; ++p) {
+        const float *q = p0 + (size_t)p * kPart;
+        const float lp = q[kPqBoth * (DV + 1) + r];
+        if (lp == 0.f) continue;                               // (nothing was written for it)
+        const float k = ex2_approx(q[kPqBoth * DV + r] - top);
+        l = fmaf(k, lp, l);
+        if constexpr (kEach == 4) {
+            const float4 x = *reinterpret_cast<const float4 *>(q + (size_t)r * DV + lane * 4);
+            o[0] = fmaf(k, x.x, o[0]), o[1] = fmaf(k, x.y, o[1]), o[2] = fmaf(k, x.z, o[2]), o[3] = fmaf(k, x.w, o[3]);
+        } else {
+            const float2 x = *reinterpret_cast<const float2 *>(q + (size_t)r * DV + lane * 2);
+            o[0] = fmaf(k, x.x, o[0]), o[1] = fmaf(k, x.y, o[1]);
+        }
+    }
+    const float mul = l != 0.f ? kQ8Unit<FORMAT> / l : 0.f;
+    const size_t at = pq_out_row(a, b, h, row) * DV + lane * kEach;
+#pragma unroll
+    for (int i = 0; i < kEach; i += 2) {
+        if (a.out_fp16) *reinterpret_cast<__half2 *>(static_cast<__half *>(a.out) + at + i) = __floats2half2_rn(o[i] * mul, o[i + 1] * mul);
+        else *reinterpret_cast<float2 *>(static_cast<float *>(a.out) + at + i) = make_float2(o[i] * mul, o[i + 1] * mul);
+    }
 }
 
 template <int FORMAT, int DK, int DV, bool FULL>
 lookat_status launch_pq(Ctx *ctx, const Q8AttendArgs &a)
 {
+    using Lay = PqLayout<DK, DV>;
     auto kern = attend_q8_umma_kernel<FORMAT, DK, DV, FULL>;
-    constexpr int smem = PqLayout<DK, DV>::kBytes;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kBytes) != cudaSuccess)
         return check_launch(ctx, "attend_q8 (tcgen05 form): shared-memory opt-in");
-    const int rows = a.g * a.L_q, per = kPqTiles * kPqRows;
-    dim3 grid((unsigned)((rows + per - 1) / per), (unsigned)a.c.H_kv, (unsigned)a.B);
-    kern<<<grid, kPqThreads, smem, ctx->stream>>>(a, ctx->timeout_flag);
-    return check_launch(ctx, "attend_q8_umma_kernel");
+    const int n_super = (a.g * a.L_q + kPqBoth - 1) / kPqBoth;
+    const long long ctas = (long long)n_super * a.c.H_kv * a.B;
+    // Few row tiles: cut the tokens so that one wave of CTAs fills the GPU (the host knows the longest length only)
+    const long long chunks = (((long long)a.c.max_pages << a.c.page_shift) + kPqChunk - 1) / kPqChunk;
+    int pieces = 1;
+    if (ctas * 2 <= ctx->sm_count) {
+        const long long fill = ctx->sm_count / ctas, most = chunks / kPqMinPiece;
+        pieces = (int)(fill < most ? fill : most);
+        if (pieces < 1) pieces = 1;
+    }
+    if (ctas > 0x7fffffffll / kPqBoth) return set_error(ctx, LOOKAT_ERR_UNSUPPORTED, "attend_q8: too many queries for one call");
+    float *parts = nullptr;
+    if (pieces > 1) {
+        lookat_status st = workspace(ctx, ctx->q8_pieces, (size_t)ctas * pieces * Lay::kPart * sizeof(float), false, "attend_q8");
+        if (st != LOOKAT_OK) return st;
+        parts = static_cast<float *>(ctx->q8_pieces.ptr);
+    }
+    kern<<<(unsigned)(ctas * pieces), kPqThreads, Lay::kBytes, ctx->stream>>>(a, ctx->timeout_flag, n_super, pieces, parts);
+    lookat_status st = check_launch(ctx, "attend_q8_umma_kernel");
+    if (st != LOOKAT_OK || pieces == 1) return st;
+    attend_q8_join_kernel<FORMAT, DV><<<(unsigned)(ctas * kPqBoth / 8), 256, 0, ctx->stream>>>(a, n_super, pieces, parts);
+    return check_launch(ctx, "attend_q8_join_kernel");
 }
 
 template <int FORMAT, bool FULL>

@@ -55,7 +55,7 @@ struct Ctx {
     float *step_out;
     size_t step_q_cap, step_k_cap, step_out_cap;   // bytes
     // 8-bit paged cache: partial results and arrival counters of the attention; lists of pages, tables being rewritten
-    Workspace q8_partials, q8_tickets, page_lists, page_marks;
+    Workspace q8_partials, q8_tickets, q8_pieces, page_lists, page_marks;
 
     // per-launch timing of the attend kernel: an event pair per timed launch, read only after the timed run
     int timing;

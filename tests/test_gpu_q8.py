@@ -111,6 +111,13 @@ def test_attend_prompt(fmt, fp16, P, H_q, H_kv, d, L_q, lens):
     check_attend(np.random.default_rng(P + L_q), lens, L_q, P, H_q, H_kv, d, d, fmt, fp16=fp16)
 
 
+@pytest.mark.parametrize("fmt,fp16", [("int8", False), ("e4m3", True)])
+@pytest.mark.parametrize("P,H_q,H_kv,d_k,d_v,L_q,lens", [(64, 4, 1, 128, 128, 70, [3000, 70, 0, 1200]), (16, 2, 2, 64, 64, 300, [2500]), (32, 2, 1, 64, 128, 65, [1100, 64])])
+def test_attend_prompt_pieces_over_a_long_cache(fmt, fp16, P, H_q, H_kv, d_k, d_v, L_q, lens):
+    """Few queries over many tokens: the tokens are cut among CTAs and joined; fp32 sums move out of tensor memory."""
+    check_attend(np.random.default_rng(P + L_q), lens, L_q, P, H_q, H_kv, d_k, d_v, fmt, fp16=fp16)
+
+
 def test_attend_large_and_small_numbers():
     """Blocks of very different sizes, peaked scores, and a scale of the caller's."""
     for peak in (1e-4, 30.0):
