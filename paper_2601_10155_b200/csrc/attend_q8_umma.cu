@@ -11,17 +11,21 @@
 // its sums off, and a chain of 16 chunks stays below 2^-20.
 //
 // A CTA works on two tiles of 128 rows against the same chunks of 64 tokens.  The scores of a tile have two buffers in
-// tensor memory, so the tensor pipe makes the next chunk's while the softmax threads work on this one's.  Roles (14 warps,
+// tensor memory, so the tensor pipe makes the next chunk's while the softmax threads work on this one's.  Roles (16 warps,
 // one CTA per SM by tensor memory):
 //   warps 0-3 / 4-7  softmax of tile 0 / 1: thread r owns row r of its tile = tensor-memory lane r;
-//   warps 8-11  producers: the next chunk's keys and values from the pages to fp16 operand rows in shared memory (128-byte
-//               swizzle), a chunk's loads issued before the wait for its buffer;
-//   warps 12, 13  one thread each issues the MMAs of tile 0 / 1 and commits them to mbarriers.
+//   warps 8, 9 / 10, 11  producers of the keys / values: from 8-bit rows to fp16 operand rows (128-byte swizzle), both in
+//               shared memory;
+//   warps 12, 13  one thread each issues the MMAs of tile 0 / 1 and commits them to mbarriers;
+//   warp 14     fetches 8-bit rows: a bulk copy per 16 tokens (a page holds whole ones) of K and of V, kPqRaw chunks ahead;
+//   warp 15     the scales of each chunk's blocks.
 // Tensor memory (512 columns): per tile S (2 x 64; the weights overwrite it) and O (d_v).  Q lies in shared memory.
 //   Few rows over a long cache are cut along the tokens (blockIdx), every piece leaves O, M and l in the workspace and
 // attend_q8_join_kernel joins them in order.
 // Every mbarrier wait gives up after a bounded number of polls, raises the context's time-out flag and lets the CTA drain
 // and free its tensor memory.
+#include <type_traits>
+
 #include "q8.cuh"
 #include "umma.cuh"
 
@@ -30,8 +34,9 @@ namespace lookat {
 namespace {
 
 constexpr int kPqRows = 128, kPqChunk = 64, kPqTiles = 2, kPqBoth = kPqTiles * kPqRows;
-constexpr int kPqSoftmax = kPqBoth, kPqProducers = 128, kPqThreads = kPqSoftmax + kPqProducers + 32 * kPqTiles;
+constexpr int kPqSoftmax = kPqBoth, kPqProducers = 128, kPqOperand = kPqProducers / 2, kPqThreads = kPqSoftmax + kPqProducers + 32 * kPqTiles + 64;
 constexpr int kPqGroups = kPqChunk / 16;        // groups of 16 tokens: a page holds whole ones
+constexpr int kPqRaw = 3;                       // chunks of 8-bit rows in shared memory
 constexpr int kPqFlush = 16;                    // chunks that O stays in tensor memory for fp32 results
 constexpr int kPqMinPiece = 8;                  // chunks below which a row's tokens are not cut further
 constexpr float kPqSlack = 8.f;
@@ -45,7 +50,10 @@ struct PqLayout {
     static constexpr int kKb = DK / 64, kNb = DV / 64;
     static constexpr int kKeys = kKb * kPqChunk * 128, kV = kNb * kPqChunk * 128, kQ = kKb * kPqRows * 128;     // [64 dims each][row][128 B]
     static constexpr int kOffKeys = 0, kOffV = 2 * kKeys, kOffQ = kOffV + 2 * kV, kOffMeta = kOffQ + kPqTiles * kQ;
-    static constexpr int kOffBars = kOffMeta + 4 * kPqGroups * (int)sizeof(PqMeta);
+    static constexpr int kOffRaw = kOffMeta + 2 * kPqGroups * (int)sizeof(PqMeta);
+    static constexpr int kRawK = kPqChunk * DK, kRaw = kRawK + kPqChunk * DV;
+    static constexpr int kOffThere = kOffRaw + kPqRaw * kRaw;                        // int [stage][group]: the group's page is there
+    static constexpr int kOffBars = kOffThere + 64;
     static constexpr int kBytes = kOffBars + 256;
     static constexpr int kColO = kPqTiles * 2 * kPqChunk;
     static_assert(kColO + kPqTiles * DV <= 512, "tensor memory");
@@ -90,14 +98,17 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
     extern __shared__ __align__(1024) unsigned char pq_raw[];
     unsigned char *const sm = pq_raw;
     const uint32_t sm0 = um_smem(sm);
-    PqMeta *const meta = reinterpret_cast<PqMeta *>(sm + Lay::kOffMeta);             // [chunk & 3][group]
+    PqMeta *const meta = reinterpret_cast<PqMeta *>(sm + Lay::kOffMeta);             // [buf][group]
     uint64_t *const bars = reinterpret_cast<uint64_t *>(sm + Lay::kOffBars);
-    uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(bars + 24);
+    uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(bars + 30);
     // k_ready[buf], v_ready[buf]; per tile s_full[t][buf] (scores done), pv_done[t][buf] (value MMA done), p_ready[t][buf]
-    // (weights stored); meta_ready[chunk & 3].  A phase of each can only end after every waiter of the one before has
+    // (weights stored); meta_ready[buf]; k_free[buf], v_free[buf] (both tiles' MMAs are done with it);
+    // raw_full[stage], raw_free[stage].  A phase of each can only end after every waiter of the one before has
     // moved on, so waits by parity are safe.
     const uint32_t bar0 = um_smem(bars);
     const uint32_t bar_k = bar0, bar_v = bar0 + 16, bar_s = bar0 + 32, bar_pv = bar0 + 64, bar_p = bar0 + 96, bar_m = bar0 + 128;
+    const uint32_t bar_kf = bar0 + 144, bar_vf = bar0 + 160, bar_raw = bar0 + 176, bar_rawf = bar0 + 200;
+    int *const there_s = reinterpret_cast<int *>(sm + Lay::kOffThere);
 
     const Q8View &c = a.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -127,15 +138,21 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
 
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
-            um_bar_init(bar_k + 8 * i, kPqProducers);
-            um_bar_init(bar_v + 8 * i, kPqProducers);
+            um_bar_init(bar_k + 8 * i, kPqOperand);
+            um_bar_init(bar_v + 8 * i, kPqOperand);
+            um_bar_init(bar_kf + 8 * i, kPqTiles);
+            um_bar_init(bar_vf + 8 * i, kPqTiles);
             for (int t = 0; t < kPqTiles; ++t) {
                 um_bar_init(bar_s + 16 * t + 8 * i, 1);
                 um_bar_init(bar_pv + 16 * t + 8 * i, 1);
                 um_bar_init(bar_p + 16 * t + 8 * i, kPqRows);
             }
         }
-        for (int i = 0; i < 4; ++i) um_bar_init(bar_m + 8 * i, kPqGroups);
+        for (int i = 0; i < 2; ++i) um_bar_init(bar_m + 8 * i, kPqGroups);
+        for (int i = 0; i < kPqRaw; ++i) {
+            um_bar_init(bar_raw + 8 * i, kPqGroups);
+            um_bar_init(bar_rawf + 8 * i, kPqProducers / 32);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
@@ -159,6 +176,65 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
 
     if (dead) {
         // misaligned shared-memory base: nothing runs
+    } else if (warp == kPqThreads / 32 - 2) {
+        // =================== the fetcher: a thread per group of 16 tokens ===================
+        if (lane < kPqGroups) {
+            const int32_t *table = c.tables + (size_t)b * c.max_pages;
+            auto entry_of = [&](int ch) {
+                const int tok = (chunk0 + ch) * kPqChunk + lane * 16;
+                return ch < n_chunks && tok < len ? __ldg(table + (tok >> c.page_shift)) : -1;
+            };
+            int entry = entry_of(0), ch = 0;
+            for (; ch < n_chunks; ++ch) {
+                const int stage = ch % kPqRaw, tok = (chunk0 + ch) * kPqChunk + lane * 16;
+                const bool there = entry >= 0 && entry < c.n_pages;
+                if (tok < len && !there) q8_report(c.status, kStatusBadPage);
+                const size_t row = there ? ((size_t)entry * c.H_kv + h) * page + (tok & (page - 1)) : 0;
+                entry = entry_of(ch + 1);
+                if (ch >= kPqRaw && !um_bar_wait(bar_rawf + 8 * stage, (ch / kPqRaw - 1) & 1)) { dead = true; break; }
+                there_s[stage * kPqGroups + lane] = there;
+                const uint32_t bar = bar_raw + 8 * stage, dst = sm0 + Lay::kOffRaw + stage * Lay::kRaw + lane * 16 * DK;
+                if (!there) {
+                    um_bar_arrive(bar);
+                    continue;
+                }
+                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(16 * (DK + DV)) : "memory");
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+                             "l"(c.k + row * DK), "r"(16 * DK), "r"(bar)
+                             : "memory");
+                asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                                 sm0 + Lay::kOffRaw + stage * Lay::kRaw + Lay::kRawK + lane * 16 * DV),
+                             "l"(c.v + row * DV), "r"(16 * DV), "r"(bar)
+                             : "memory");
+            }
+            for (int i = max(0, ch - kPqRaw); i < ch; ++i) um_bar_wait(bar_raw + 8 * (i % kPqRaw), (i / kPqRaw) & 1);     // copies in flight end first
+        }
+    } else if (warp == kPqThreads / 32 - 1) {
+        // =================== the scales: a thread per group of 16 tokens ===================
+        if (lane < kPqGroups) {
+            const int32_t *table = c.tables + (size_t)b * c.max_pages;
+            auto entry_of = [&](int ch) {
+                const int tok = (chunk0 + ch) * kPqChunk + lane * 16;
+                return ch < n_chunks && tok < len ? __ldg(table + (tok >> c.page_shift)) : -1;
+            };
+            int entry = entry_of(0);
+            for (int ch = 0; ch < n_chunks; ++ch) {
+                const bool there = entry >= 0 && entry < c.n_pages;
+                const size_t block = there ? (size_t)entry * c.H_kv + h : 0;
+                const float ak = there ? __ldg(c.k_amax + block) : 0.f, av = there ? __ldg(c.v_amax + block) : 0.f;
+                entry = entry_of(ch + 1);
+                PqMeta m;
+                m.ks = ak * (kQ8Unit<FORMAT> * a.scale_log2);
+                m.le = !there ? -INFINITY : av > 0.f ? log2f(av) : 0.f;            // (amax 0: the numbers are 0, the weights count)
+                m.inv = av > 0.f ? 1.f / av : 1.f;
+                m.pad = 0.f;
+                // the slot's last reader was the softmax of chunk ch - 2, over when the value MMAs of that chunk are done (and
+                // those of chunk ch, the barrier's next phase, wait for these scales)
+                if (ch >= 2 && !um_bar_wait(bar_vf + 8 * (ch & 1), ((ch - 2) >> 1) & 1)) { dead = true; break; }
+                meta[(ch & 1) * kPqGroups + lane] = m;
+                um_bar_arrive(bar_m + 8 * (ch & 1));
+            }
+        }
     } else if (warp >= (kPqSoftmax + kPqProducers) / 32) {
         // =================== the MMA thread of a tile ===================
         if (lane == 0) {
@@ -182,6 +258,7 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
                     else um_mma_ss<true>(d, q_lo + qo, desc_hi, lo + ko, desc_hi, Lay::kIdescS);
                 }
                 um_commit(bar_s + 16 * t + 8 * buf);
+                um_commit(bar_kf + 8 * buf);
                 return true;
             };
             auto value_mma = [&](int ch) {                     // weights over the scores: first halves, then (FULL) second ones
@@ -198,6 +275,7 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
                         else um_mma_ts<true>(tm_o, pa + half * 32 + kt * 8, lo + kt * (2048 >> 4), desc_hi, Lay::kIdescO);
                     }
                 um_commit(bar_pv + 16 * t + 8 * buf);
+                um_commit(bar_vf + 8 * buf);
                 return true;
             };
             bool ok = score_mma(0);
@@ -206,105 +284,50 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
             dead = !ok;
         }
     } else if (warp >= kPqSoftmax / 32) {
-        // =================== producers ===================
-        // A warp's item: 8 tokens (an octet; it lies in one page) by 64 dims; lane: token lane & 7, 16 dims lane >> 3.  The
-        // stores of 8 lanes then go to 8 different columns of the swizzle.
-        const int ptid = tid - kPqSoftmax, pw = ptid >> 5, tl = lane & 7, pl = lane >> 3;
-        constexpr int kItemsK = 2 * Lay::kKb, kItemsV = 2 * Lay::kNb;                // per warp and chunk
-        const int32_t *table = c.tables + (size_t)b * c.max_pages;
-        auto entry_of = [&](int tok) { return tok < len ? __ldg(table + (tok >> c.page_shift)) : -1; };
-        auto held = [&](int tok, int p) {                      // reports a bad entry
-            const bool ok = p >= 0 && p < c.n_pages;
-            if (tok < len && !ok) q8_report(c.status, kStatusBadPage);
-            return ok;
+        // =================== producers: two warps for the keys, two for the values ===================
+        // An item: 8 tokens by 64 dims; lane: token lane >> 2, 16 dims lane & 3.  Odd tokens take the other 64 dims than even
+        // ones, so that 8 lanes read 128 different bytes (of two rows) and store to 8 different columns of the swizzle.
+        auto produce = [&](auto values) {
+            constexpr bool V = decltype(values)::value;
+            constexpr int D = V ? DV : DK, kBlocks = D / 64, kItems = 4 * kBlocks;   // per warp and chunk
+            const int pw = (warp - kPqSoftmax / 32) & 1, tl = lane >> 2, pl = lane & 3;
+            const uint32_t bar_full = V ? bar_v : bar_k, bar_free = V ? bar_vf : bar_kf;
+            const unsigned char *const raw0 = sm + Lay::kOffRaw + (V ? Lay::kRawK : 0) + (pw * 32 + tl) * D + pl * 16;
+            unsigned char *const rows0 = sm + (V ? Lay::kOffV : Lay::kOffKeys) + (pw * 32 + tl) * 128;
+            for (int ch = 0; ch < n_chunks; ++ch) {
+                const int buf = ch & 1, stage = ch % kPqRaw, tok = (chunk0 + ch) * kPqChunk + pw * 32 + tl;
+                if (!__all_sync(0xffffffffu, um_bar_wait(bar_raw + 8 * stage, (ch / kPqRaw) & 1))) return false;
+                const unsigned char *const raw = raw0 + stage * Lay::kRaw;
+                uint4 u[kItems];
+#pragma unroll
+                for (int i = 0; i < kItems; ++i) {             // zeros behind the row's last token and for bad entries
+                    const int octet = i / kBlocks, block = kBlocks == 2 ? (i & 1) ^ (tl & 1) : 0;
+                    u[i] = *reinterpret_cast<const uint4 *>(raw + octet * 8 * D + block * 64);
+                    if (tok + octet * 8 >= len || !there_s[stage * kPqGroups + pw * 2 + (octet >> 1)]) u[i] = make_uint4(0u, 0u, 0u, 0u);
+                }
+                __syncwarp();
+                if (lane == 0) um_bar_arrive(bar_rawf + 8 * stage);
+                if (ch >= 2 && !__all_sync(0xffffffffu, um_bar_wait(bar_free + 8 * buf, ((ch - 2) >> 1) & 1))) return false;
+                unsigned char *const rows = rows0 + buf * (V ? Lay::kV : Lay::kKeys);
+#pragma unroll
+                for (int i = 0; i < kItems; ++i) {             // 16 numbers as two 16-byte pieces of a row
+                    const int octet = i / kBlocks, block = kBlocks == 2 ? (i & 1) ^ (tl & 1) : 0;
+                    unsigned char *const row = rows + block * (kPqChunk * 128) + octet * (8 * 128);
+                    uint4 x, y;
+                    q8_pairs<FORMAT>(u[i].x, x.x, x.y);
+                    q8_pairs<FORMAT>(u[i].y, x.z, x.w);
+                    q8_pairs<FORMAT>(u[i].z, y.x, y.y);
+                    q8_pairs<FORMAT>(u[i].w, y.z, y.w);
+                    *reinterpret_cast<uint4 *>(row + (((2 * pl) ^ tl) << 4)) = x;
+                    *reinterpret_cast<uint4 *>(row + (((2 * pl + 1) ^ tl) << 4)) = y;
+                }
+                um_fence_async_smem();                         // generic-proxy writes before the MMA's reads
+                um_bar_arrive(bar_full + 8 * buf);
+            }
+            return true;
         };
-        // warp w takes the octets w and w + 4 (for every 64 dims): two table entries a chunk
-        uint4 rk[kItemsK], rv[kItemsV];
-        int ent[2], ent_meta;
-        float am_k = 0.f, am_v = 0.f;
-        bool meta_there = false;
-        auto ask_entries = [&](int ch) {
-            const int tok0 = (chunk0 + ch) * kPqChunk;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) ent[i] = entry_of(tok0 + (pw + 4 * i) * 8);
-            ent_meta = entry_of(tok0 + (ptid & 3) * 16);
-        };
-        auto ask_rows = [&](int ch) {                          // zeros behind the row's last token and for bad entries
-            const int tok0 = (chunk0 + ch) * kPqChunk;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int tok = tok0 + (pw + 4 * i) * 8;
-                const bool ok = held(tok, ent[i]) && tok + tl < len;
-                const size_t row = ok ? ((size_t)ent[i] * c.H_kv + h) * page + ((tok + tl) & (page - 1)) : 0;
-#pragma unroll
-                for (int kb = 0; kb < Lay::kKb; ++kb)
-                    rk[i * Lay::kKb + kb] = ok ? __ldg(reinterpret_cast<const uint4 *>(c.k + row * DK + kb * 64 + pl * 16)) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-                for (int nb = 0; nb < Lay::kNb; ++nb)
-                    rv[i * Lay::kNb + nb] = ok ? __ldg(reinterpret_cast<const uint4 *>(c.v + row * DV + nb * 64 + pl * 16)) : make_uint4(0u, 0u, 0u, 0u);
-            }
-            if (ptid < kPqGroups) {
-                meta_there = tok0 + ptid * 16 < len && ent_meta >= 0 && ent_meta < c.n_pages;
-                const size_t block = meta_there ? (size_t)ent_meta * c.H_kv + h : 0;
-                am_k = meta_there ? __ldg(c.k_amax + block) : 0.f;
-                am_v = meta_there ? __ldg(c.v_amax + block) : 0.f;
-            }
-        };
-        auto widen = [&](unsigned char *block, int oct, const uint4 &u) {          // 16 numbers as two 16-byte pieces of a row
-            const int r = oct * 8 + tl;
-            uint4 x, y;
-            q8_pairs<FORMAT>(u.x, x.x, x.y);
-            q8_pairs<FORMAT>(u.y, x.z, x.w);
-            q8_pairs<FORMAT>(u.z, y.x, y.y);
-            q8_pairs<FORMAT>(u.w, y.z, y.w);
-            *reinterpret_cast<uint4 *>(block + r * 128 + (((2 * pl) ^ tl) << 4)) = x;
-            *reinterpret_cast<uint4 *>(block + r * 128 + (((2 * pl + 1) ^ tl) << 4)) = y;
-        };
-        ask_entries(0);
-        ask_rows(0);
-        ask_entries(1);
-        for (int ch = 0; ch < n_chunks; ++ch) {
-            const int buf = ch & 1;
-            bool ok = true;
-            if (ch >= 2) {                                     // both tiles' scores of chunk ch - 2 are done with the buffer
-#pragma unroll
-                for (int t = 0; t < kPqTiles; ++t)
-                    ok = um_group_wait<1, kPqProducers>(ptid == 0, bar_s + 16 * t + 8 * buf, ((ch - 2) >> 1) & 1) && ok;
-                if (!ok) { dead = true; break; }
-            }
-            // (scores ch - 2 were issued after the value MMA of ch - 4, so the softmax of ch - 4 is over: its slot is free)
-            if (ptid < kPqGroups) {
-                PqMeta m;
-                m.ks = am_k * (kQ8Unit<FORMAT> * a.scale_log2);
-                m.le = !meta_there ? -INFINITY : am_v > 0.f ? log2f(am_v) : 0.f;   // (amax 0: the numbers are 0, the weights count)
-                m.inv = am_v > 0.f ? 1.f / am_v : 1.f;
-                m.pad = 0.f;
-                meta[(ch & 3) * kPqGroups + ptid] = m;
-                um_bar_arrive(bar_m + 8 * (ch & 3));
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int kb = 0; kb < Lay::kKb; ++kb)
-                    widen(sm + Lay::kOffKeys + buf * Lay::kKeys + kb * (kPqChunk * 128), pw + 4 * i, rk[i * Lay::kKb + kb]);
-            um_fence_async_smem();                             // generic-proxy writes before the MMA's reads
-            um_bar_arrive(bar_k + 8 * buf);
-            if (ch >= 2) {                                     // ... and their value MMAs with the V buffer
-#pragma unroll
-                for (int t = 0; t < kPqTiles; ++t)
-                    ok = um_group_wait<1, kPqProducers>(ptid == 0, bar_pv + 16 * t + 8 * buf, ((ch - 2) >> 1) & 1) && ok;
-                if (!ok) { dead = true; break; }
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int nb = 0; nb < Lay::kNb; ++nb)
-                    widen(sm + Lay::kOffV + buf * Lay::kV + nb * (kPqChunk * 128), pw + 4 * i, rv[i * Lay::kNb + nb]);
-            um_fence_async_smem();
-            um_bar_arrive(bar_v + 8 * buf);
-            ask_rows(ch + 1);                                  // in flight while the next buffer is waited for
-            ask_entries(ch + 2);
-        }
+        const bool ok = warp < kPqSoftmax / 32 + 2 ? produce(std::false_type{}) : produce(std::true_type{});
+        dead = !ok;
     } else {
         // =================== softmax: thread r owns row r of tile t ===================
         const int t = warp >> 2, rq = warp & 3, r = t * kPqRows + rq * 32 + lane, row = row0 + r;
@@ -347,7 +370,7 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
         for (int ch = 0; ch < n_chunks; ++ch) {
             const int buf = ch & 1, tok0 = (chunk0 + ch) * kPqChunk;
             const uint32_t tm_sb = tm_s + buf * kPqChunk;
-            const bool ok = um_bar_wait(bar_s + 16 * t + 8 * buf, (ch >> 1) & 1) && um_bar_wait(bar_m + 8 * (ch & 3), (ch >> 2) & 1);
+            const bool ok = um_bar_wait(bar_s + 16 * t + 8 * buf, (ch >> 1) & 1) && um_bar_wait(bar_m + 8 * buf, (ch >> 1) & 1);
             if (!__all_sync(0xffffffffu, ok)) { dead = true; break; }              // warp-uniform
             um_fence_after();
             float2 y[kPqChunk / 2];
@@ -369,7 +392,7 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
             float inv[kPqGroups];
 #pragma unroll
             for (int gr = 0; gr < kPqGroups; ++gr) {
-                const PqMeta m = meta[(ch & 3) * kPqGroups + gr];
+                const PqMeta m = meta[buf * kPqGroups + gr];
                 const float off = m.le - m_run;
                 inv[gr] = m.inv;
 #pragma unroll
