@@ -580,8 +580,12 @@ lookat_status launch_pq_dims(Ctx *ctx, const Q8AttendArgs &a)
 
 bool attend_q8_umma_covers(const Ctx *ctx, const Q8AttendArgs &a)
 {
+    // Rows of a KV head (queries times heads of its group) above which this form is the faster one.  Up to 32 the streaming
+    // kernel reads the cache once or twice: 16 rows of 4096 tokens, 20 and 32 rows per head, fp32 results 102 us there and
+    // 118 us here (fp16 102 and 87); from 33 on it reads it three times: 48 rows 33 and 23 us for one row of tokens, 64 rows
+    // 181 and 87 us for 16 (fp16).
     const bool dims = (a.c.d_k == 64 || a.c.d_k == 128) && (a.c.d_v == 64 || a.c.d_v == 128);
-    return dims && (long long)a.g * a.L_q >= 64 && ctx->timeout_flag;
+    return dims && (long long)a.g * a.L_q > 32 && ctx->timeout_flag;
 }
 
 lookat_status launch_attend_q8_umma(Ctx *ctx, const Q8AttendArgs &a)
