@@ -90,11 +90,11 @@ struct AqLayout {
     static constexpr int kOffV = 16 * DP, kTile = 2 * kOffV;    // bytes of 16 tokens (padded to DP dims): K, V
     static constexpr int kStage = kTile + 16;                   // + amax^K, amax^V, whether the tile is there
     static constexpr int kRing = kAqWarps * kAqStages * kStage;
-    // the warps' results of a unit: O [col][DP] of each warp in the stage of its last tile where that is large enough (its
-    // next copy comes after the join), M, l and the factor of M [warp][col], then M and l of the CTA
-    static constexpr int kCols = PACK ? 4 : 8 * NT;
-    static constexpr bool kInRing = kCols * DP * 4 <= kTile;
-    static constexpr int kJoin = ((kInRing ? 0 : kAqWarps * kCols * DP) + kAqWarps * kCols * 3 + 2 * kCols) * 4;
+    // the warps' results of 8 (or 4) columns at a time: O [col][DP] of each warp in the stage of its last tile, whose next
+    // copy comes after the join; M, l and the factor of M [warp][col], then M and l of the CTA
+    static constexpr int kCols = PACK ? 4 : 8 * NT, kJoinCols = PACK ? 4 : 8;
+    static_assert(kJoinCols * DP * 4 <= kTile, "O of a warp lies in a stage of the ring");
+    static constexpr int kJoin = (kAqWarps * kJoinCols * 3 + 2 * kCols) * 4;
     // when a CTA joins the pieces of a unit, their factors [col][kAqMaxParts] lie over the drained ring
     static_assert(kRing >= kCols * kAqMaxParts * 4, "factors of the pieces");
     static constexpr int kBytes = kRing + kJoin;
@@ -213,13 +213,12 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
     }
 
     unsigned char *const ring = aq_raw + warp * (kAqStages * Lay::kStage);
-    float *const sM = reinterpret_cast<float *>(aq_raw + Lay::kBytes) - kAqWarps * Lay::kCols * 3 - 2 * Lay::kCols, *const sL = sM + kAqWarps * Lay::kCols, *const sK = sL + kAqWarps * Lay::kCols;
-    float *const sTop = sK + kAqWarps * Lay::kCols, *const sSum = sTop + Lay::kCols;
+    constexpr int JC = Lay::kJoinCols;
+    float *const sM = reinterpret_cast<float *>(aq_raw + Lay::kRing), *const sL = sM + kAqWarps * JC, *const sK = sL + kAqWarps * JC;
+    float *const sTop = sK + kAqWarps * JC, *const sSum = sTop + Lay::kCols;
     const int d_k = EXACT ? DP : c.d_k, d_v = EXACT ? DP : c.d_v;
     // O of warp w [col][DP], during a join after step n
-    auto results = [&](int w, int n) {
-        return reinterpret_cast<float *>(Lay::kInRing ? aq_raw + (w * kAqStages + n % kAqStages) * Lay::kStage : aq_raw + Lay::kRing + w * (Lay::kCols * DP * 4));
-    };
+    auto results = [&](int w, int n) { return reinterpret_cast<float *>(aq_raw + (w * kAqStages + n % kAqStages) * Lay::kStage); };
     const float k_unit = kQ8Unit<FORMAT> * a.scale_log2;
 
     // ---- the ring runs ahead of the products, over the borders of units; this warp's tile of a step holds tokens
@@ -479,20 +478,26 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
 
         // ---- the unit, or this CTA's piece of it, is done: join the warps (the ring stays full meanwhile) ----
         fresh = true;
+        const long long u0 = pos + at.at - at.step;             // the unit's first step
+        const int first = (int)(u0 / chunk), pieces = (int)((u0 + at.steps - 1) / chunk) - first + 1, me = blockIdx.x;
+        const int left = n_cols - at.unit % groups * Lay::kCols;                    // columns of the unit and beyond
+        float *const part = parts + (size_t)(2 * me + (me == first)) * Lay::kPart;
         float *const mine = results(warp, n);
-        if constexpr (Lay::kInRing) __syncwarp();               // everyone is done with the tile
+        __syncwarp();                                           // everyone is done with the tile
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
+            if (nt > 0 && nt * 8 >= left) break;
+            if (nt > 0) __syncthreads();                        // the results of the columns before have been read
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 float l = l_sum[nt][k];
                 l += __shfl_xor_sync(0xffffffffu, l, 4);
                 l += __shfl_xor_sync(0xffffffffu, l, 8);
                 l += __shfl_xor_sync(0xffffffffu, l, 16);
-                const int col = nt * 8 + 2 * t + k;
+                const int col = 2 * t + k;
                 if (g == 0 && (!PACK || t < 2)) {
-                    sM[warp * Lay::kCols + col] = m_ref[nt][k];
-                    sL[warp * Lay::kCols + col] = l;
+                    sM[warp * JC + col] = m_ref[nt][k];
+                    sL[warp * JC + col] = l;
                 }
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
@@ -506,36 +511,34 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
                     if (!PACK || t < 2) *reinterpret_cast<float2 *>(mine + col * DP + dim) = x;
                 }
             }
-        __syncthreads();
-        if (tid < Lay::kCols) {
-            float top = sM[tid], l = 0.f;
+            __syncthreads();
+            if (tid < JC) {
+                float top = sM[tid], l = 0.f;
 #pragma unroll
-            for (int w = 1; w < kAqWarps; ++w) top = fmaxf(top, sM[w * Lay::kCols + tid]);
+                for (int w = 1; w < kAqWarps; ++w) top = fmaxf(top, sM[w * JC + tid]);
 #pragma unroll
-            for (int w = 0; w < kAqWarps; ++w) {
-                const float k = ex2_approx(sM[w * Lay::kCols + tid] - top);
-                sK[w * Lay::kCols + tid] = k;
-                l = fmaf(k, sL[w * Lay::kCols + tid], l);
+                for (int w = 0; w < kAqWarps; ++w) {
+                    const float k = ex2_approx(sM[w * JC + tid] - top);
+                    sK[w * JC + tid] = k;
+                    l = fmaf(k, sL[w * JC + tid], l);
+                }
+                sTop[nt * 8 + tid] = top;
+                sSum[nt * 8 + tid] = l;
             }
-            sTop[tid] = top;
-            sSum[tid] = l;
-        }
-        __syncthreads();
-        const long long u0 = pos + at.at - at.step;             // the unit's first step
-        const int first = (int)(u0 / chunk), pieces = (int)((u0 + at.steps - 1) / chunk) - first + 1, me = blockIdx.x;
-        const int n_here = min(Lay::kCols, n_cols - at.unit % groups * Lay::kCols) * quads;     // groups of 4 dims, of all columns
-        float *const part = parts + (size_t)(2 * me + (me == first)) * Lay::kPart;
-        for (int i = tid; i < n_here; i += kAqThreads) {
-            const int col = i / quads, quad = i % quads;
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+            __syncthreads();
+            const int n_here = min(JC, left - nt * 8) * quads;  // groups of 4 dims, of all columns
+            for (int i = tid; i < n_here; i += kAqThreads) {
+                const int col = i / quads, quad = i % quads;
+                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int w = 0; w < kAqWarps; ++w)
-                add(x, sK[w * Lay::kCols + col], *reinterpret_cast<const float4 *>(results(w, n) + col * DP + quad * 4));
-            if (pieces == 1) store(at.b, at.unit, col, quad, x, sSum[col]);
-            else __stcg(reinterpret_cast<float4 *>(part + 2 * Lay::kCols + col * DP + quad * 4), x);
+                for (int w = 0; w < kAqWarps; ++w)
+                    add(x, sK[w * JC + col], *reinterpret_cast<const float4 *>(results(w, n) + col * DP + quad * 4));
+                if (pieces == 1) store(at.b, at.unit, nt * 8 + col, quad, x, sSum[nt * 8 + col]);
+                else __stcg(reinterpret_cast<float4 *>(part + 2 * Lay::kCols + (nt * 8 + col) * DP + quad * 4), x);
+            }
         }
         if (pieces > 1) {
-            if (tid < Lay::kCols) {
+            if (tid < min(Lay::kCols, left)) {
                 __stcg(part + tid, sTop[tid]);
                 __stcg(part + Lay::kCols + tid, sSum[tid]);
             }
@@ -571,7 +574,7 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
         const float *const head = parts + (size_t)(2 * first + 1) * Lay::kPart, *const rest = parts + (size_t)2 * first * Lay::kPart;
         auto piece = [&](int p) { return p == 0 ? head : rest + (size_t)2 * p * Lay::kPart; };
         __syncthreads();
-        for (int col = warp; col < Lay::kCols; col += kAqWarps) {           // a warp's lanes over the pieces of a column
+        for (int col = warp; col < min(Lay::kCols, n_cols - unit % groups * Lay::kCols); col += kAqWarps) {           // a warp's lanes over the pieces of a column
             float m[kAqMaxParts / 32], l = 0.f, top = -1e30f;
 #pragma unroll
             for (int i = 0; i < kAqMaxParts / 32; ++i) {
