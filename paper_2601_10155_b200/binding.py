@@ -303,7 +303,7 @@ class Lookat:
         if st != 0:
             raise LookatError(st, "lookat_create rejected the configuration or the device")
         self._h = h
-        self._shape = (n_q_heads, n_kv_heads, d_k, d_v)
+        self._shape, self._kv_shape = (n_q_heads, n_kv_heads, d_k, d_v), (n_kv_heads, d_k, d_v)
         self._raw_stream = stream.cuda_stream
         self.scale = scale if scale > 0 else 1.0 / math.sqrt(d_k)
 
@@ -476,8 +476,8 @@ class Lookat:
 
     # -- the 8-bit paged cache (include/lookat_q8.h) --------------------------------
     def _q8(self, cache, tables, seq_lens):
-        if cache.heads != self._shape[1:]:
-            raise ValueError(f"the cache holds (heads, d_k, d_v) = {cache.heads}, the context {self._shape[1:]}")
+        if cache.heads != self._kv_shape:
+            raise ValueError(f"the cache holds (heads, d_k, d_v) = {cache.heads}, the context {self._kv_shape}")
         if cache.device != self.device:
             raise ValueError(f"the cache is on {cache.device}, the context on {self.device}")
         if tables.dim() != 2:
@@ -509,7 +509,7 @@ class Lookat:
         dtype = torch.float16 if out_fp16 else torch.float32
         shape = (B, H, d_v) if one else (B, H, L_q, d_v)
         if out is None:
-            out = torch.empty(shape, dtype=dtype, device=dev)
+            out = q.new_empty(shape, dtype=dtype)
             if torch._C._cuda_getCurrentRawStream(dev.index) != self._raw_stream:
                 out.record_stream(self.stream)                  # allocated for another stream than the one that writes it
             po = out.data_ptr()

@@ -110,6 +110,7 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
     const uint32_t bar_kf = bar0 + 144, bar_vf = bar0 + 160, bar_raw = bar0 + 176, bar_rawf = bar0 + 200;
     int *const there_s = reinterpret_cast<int *>(sm + Lay::kOffThere);
 
+    if (pieces > 1) pdl_release();
     const Q8View &c = a.c;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int n_rows = a.g * a.L_q;
@@ -504,6 +505,7 @@ template <int FORMAT, int DV>
 __global__ void __launch_bounds__(256) attend_q8_join_kernel(Q8AttendArgs a, int n_super, int pieces, const float *__restrict__ parts)
 {
     constexpr int kPart = kPqBoth * (DV + 2), kEach = DV / 32;
+    pdl_wait();
     const int lane = threadIdx.x & 31;
     const long long item = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);           // [super][b][h][row of the tiles]
     const int r = (int)(item % kPqBoth), h = (int)(item / kPqBoth % a.c.H_kv), b = (int)(item / kPqBoth / a.c.H_kv % a.B);
@@ -565,7 +567,7 @@ lookat_status launch_pq(Ctx *ctx, const Q8AttendArgs &a)
     kern<<<(unsigned)(ctas * pieces), kPqThreads, Lay::kBytes, ctx->stream>>>(a, ctx->timeout_flag, n_super, pieces, parts);
     lookat_status st = check_launch(ctx, "attend_q8_umma_kernel");
     if (st != LOOKAT_OK || pieces == 1) return st;
-    attend_q8_join_kernel<FORMAT, DV><<<(unsigned)(ctas * kPqBoth / 8), 256, 0, ctx->stream>>>(a, n_super, pieces, parts);
+    launch_after(ctx, attend_q8_join_kernel<FORMAT, DV>, (unsigned)(ctas * kPqBoth / 8), 256, 0, a, n_super, pieces, parts);
     return check_launch(ctx, "attend_q8_join_kernel");
 }
 

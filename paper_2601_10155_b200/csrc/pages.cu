@@ -58,6 +58,7 @@ __global__ void __launch_bounds__(kPgThreads) pages_extend_kernel(PageState s, i
     int *const len_s = start_s + s.B, *const n_s = len_s + s.B; // tokens held and coming
     __shared__ long long sums[32];
     __shared__ int pair_count;
+    pdl_release();
     const int tid = threadIdx.x, page = 1 << s.page_shift;
     const long long cap = (long long)s.max_pages << s.page_shift;
     const int nf = *s.n_free;
@@ -173,6 +174,7 @@ __device__ __forceinline__ void pg_move(const PagePools &pools, const int2 *pair
 __global__ void __launch_bounds__(256) pages_move_kernel(const __grid_constant__ PagePools pools, const int2 *__restrict__ pairs,
                                                          const int *__restrict__ n_pairs, int n_pages)
 {
+    pdl_wait();
     pg_move(pools, pairs, *n_pairs, n_pages);
 }
 
@@ -181,6 +183,7 @@ __global__ void __launch_bounds__(256) pages_move_kernel(const __grid_constant__
 __global__ void __launch_bounds__(256) pages_fork_count_kernel(PageState s, const int32_t *__restrict__ parents, int32_t *__restrict__ rows,
                                                                int32_t *__restrict__ lens, unsigned *__restrict__ marks)
 {
+    pdl_release();
     const int b = blockIdx.x, p = parents[b];
     const bool alive = p >= 0 && p < s.B;
     const int cap = s.max_pages << s.page_shift;
@@ -215,6 +218,7 @@ pages_fork_write_kernel(PageState s, const int32_t *__restrict__ parents, const 
                         unsigned *__restrict__ marks)
 {
     const int tid = threadIdx.x, rank = blockIdx.x % kPgCluster;
+    pdl_wait();
     if (blockIdx.x >= kPgCluster) {
         for (int b = blockIdx.x - kPgCluster; b < s.B; b += gridDim.x - kPgCluster) {
             if (parents[b] == b) continue;
@@ -281,6 +285,7 @@ __global__ void __launch_bounds__(kPgThreads) pages_compact_plan_kernel(PageStat
                                                                         int32_t *__restrict__ map, int32_t *__restrict__ remap)
 {
     extern __shared__ unsigned bits[];                          // [2 * duos], then int below[duos]
+    pdl_release();
     __shared__ long long sums[32];
     const int tid = threadIdx.x, lane = tid & 31, duos = (s.n_pages + 63) / 64;
     int *below = reinterpret_cast<int *>(bits + 2 * duos);
@@ -337,6 +342,7 @@ __global__ void __launch_bounds__(256) pages_compact_move_kernel(const __grid_co
                                                                  const int32_t *__restrict__ map)
 {
     const int cap = s.max_pages << s.page_shift;
+    pdl_wait();
     for (int b = blockIdx.x; b < s.B; b += gridDim.x) {
         const int n = pg_blocks(min(max(s.seq_lens[b], 0), cap), s.page_shift);
         int32_t *row = s.tables + (size_t)b * s.max_pages;
@@ -384,7 +390,7 @@ lookat_status launch_pages_extend(Ctx *ctx, const PageState &s, int32_t *n_new, 
     pages_extend_kernel<<<1, kPgThreads, smem, ctx->stream>>>(s, n_new, pairs, count);
     st = check_launch(ctx, "pages_extend_kernel");
     if (st != LOOKAT_OK || pools.n == 0) return st;
-    pages_move_kernel<<<move_grid(ctx, (long long)s.B * pools.items), 256, 0, ctx->stream>>>(pools, pairs, count, s.n_pages);
+    launch_after(ctx, pages_move_kernel, move_grid(ctx, (long long)s.B * pools.items), 256, 0, pools, pairs, count, s.n_pages);
     return check_launch(ctx, "pages_move_kernel");
 }
 
@@ -402,7 +408,7 @@ lookat_status launch_pages_fork(Ctx *ctx, const PageState &s, const int32_t *par
     st = check_launch(ctx, "pages_fork_count_kernel");
     if (st != LOOKAT_OK) return st;
     const int writers = ((s.B < 512 ? s.B : 512) + kPgCluster - 1) / kPgCluster * kPgCluster;
-    pages_fork_write_kernel<<<kPgCluster + writers, kPgThreads, 0, ctx->stream>>>(s, parents, rows, lens, marks);
+    launch_after(ctx, pages_fork_write_kernel, kPgCluster + writers, kPgThreads, 0, s, parents, rows, lens, marks);
     return check_launch(ctx, "pages_fork_write_kernel");
 }
 
@@ -420,7 +426,7 @@ lookat_status launch_pages_compact(Ctx *ctx, const PageState &s, const PagePools
     pages_compact_plan_kernel<<<1, kPgThreads, smem, ctx->stream>>>(s, pairs, count, map, remap);
     st = check_launch(ctx, "pages_compact_plan_kernel");
     if (st != LOOKAT_OK) return st;
-    pages_compact_move_kernel<<<move_grid(ctx, (long long)s.n_pages * pools.items), 256, 0, ctx->stream>>>(pools, s, pairs, count, map);
+    launch_after(ctx, pages_compact_move_kernel, move_grid(ctx, (long long)s.n_pages * pools.items), 256, 0, pools, s, pairs, count, map);
     return check_launch(ctx, "pages_compact_move_kernel");
 }
 

@@ -53,6 +53,27 @@ lookat_status launch_attend_q8_umma(Ctx *ctx, const Q8AttendArgs &a);
 // context is destroyed, because a captured graph may still name it.  Refuses to allocate while the stream is captured.
 lookat_status workspace(Ctx *ctx, Workspace &w, size_t bytes, bool zeroed, const char *what);
 
+// Launches a kernel that may start while the one before it on the stream still runs: that one has called pdl_release() and
+// this one calls pdl_wait() before it touches anything the other writes.  Saves the launch latency between the two halves
+// of a call (1 to 2 us).
+template <class... P, class... A>
+cudaError_t launch_after(Ctx *ctx, void (*kernel)(P...), unsigned grid, unsigned block, size_t smem, A &&...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = ctx->stream;
+    cudaLaunchAttribute early = {};
+    early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    early.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &early;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+__device__ __forceinline__ void pdl_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // one 8-bit number nearest to x (ties to even; |x| <= R up to rounding), as its byte
 template <int FORMAT>
 __device__ __forceinline__ uint32_t q8_round(float x)

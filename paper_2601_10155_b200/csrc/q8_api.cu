@@ -10,15 +10,16 @@ namespace {
 
 struct Q8DeviceGuard {
     int prev = -1;
-    bool ok = false;
+    bool ok = false, moved = false;
     explicit Q8DeviceGuard(int dev)
     {
         if (cudaGetDevice(&prev) != cudaSuccess) return;
-        ok = prev == dev || cudaSetDevice(dev) == cudaSuccess;
+        moved = prev != dev;
+        ok = !moved || cudaSetDevice(dev) == cudaSuccess;
     }
     ~Q8DeviceGuard()
     {
-        if (ok && prev >= 0) cudaSetDevice(prev);
+        if (ok && moved) cudaSetDevice(prev);
     }
 };
 
