@@ -49,8 +49,10 @@ __device__ __forceinline__ int pg_blocks(long long len, int shift) { return (int
 // ---- extend: who needs which pages ----
 // Rows in order.  Row b's place on the stack is the sum of what the rows before it take; whether it takes a copy of its
 // begun last page depends on how many rows before it (of this call) left that page: refs - rank > 1.
-__global__ void __launch_bounds__(kPgThreads) pages_extend_kernel(PageState s, int32_t *__restrict__ n_new, int2 *__restrict__ pairs,
-                                                                  int *__restrict__ n_pairs)
+// taken: per row what pages_extend_apply_kernel does, {first page off the stack, pages, table place of the first, the page that
+// a copy replaces or -1}.
+__global__ void __launch_bounds__(kPgThreads) pages_extend_plan_kernel(PageState s, int32_t *__restrict__ n_new, int2 *__restrict__ pairs,
+                                                                       int *__restrict__ n_pairs, int4 *__restrict__ taken)
 {
     extern __shared__ int rows_s[];                             // per row:
     int *const last_s = rows_s;                                 // the begun page it appends to, -1 if it has none
@@ -104,30 +106,22 @@ __global__ void __launch_bounds__(kPgThreads) pages_extend_kernel(PageState s, i
     }
     __syncthreads();
     if (bad) {                                                  // (the same for every thread)
-        for (int b = tid; b < s.B; b += kPgThreads) n_new[b] = 0;
+        for (int b = tid; b < s.B; b += kPgThreads) {
+            n_new[b] = 0;
+            taken[b] = make_int4(0, 0, 0, -1);
+        }
         if (tid == 0) {
             *n_pairs = 0;
             q8_report(s.status, kStatusNoPages);
         }
         return;
     }
-    // 8 threads per row: the pages it takes
-    for (int b = tid >> 3; b < s.B; b += kPgThreads / 8) {
+    for (int b = tid; b < s.B; b += kPgThreads) {
         const int n = n_s[b], L = len_s[b];
         const int copy = start_s[b] & 1, start = start_s[b] >> 1, have = pg_blocks(L, s.page_shift);
-        const int take = pg_blocks((long long)L + n, s.page_shift) - have + copy;
-        int32_t *row = s.tables + (size_t)b * s.max_pages;
-#pragma unroll 4
-        for (int k = tid & 7; k < take; k += 8) {
-            const int p = s.free_list[nf - 1 - start - k];
-            if (pg_valid(p, s)) s.refs[p] = 1;
-            row[have - copy + k] = p;
-            if (copy && k == 0) {
-                atomicSub(s.refs + last_s[b], 1);
-                pairs[atomicAdd(&pair_count, 1)] = make_int2(last_s[b], p);
-            }
-        }
-        if ((tid & 7) == 0 && n > 0) s.seq_lens[b] = L + n;
+        taken[b] = make_int4(nf - 1 - start, pg_blocks((long long)L + n, s.page_shift) - have + copy, have - copy, copy ? last_s[b] : -1);
+        if (copy) pairs[atomicAdd(&pair_count, 1)] = make_int2(last_s[b], s.free_list[nf - 1 - start]);
+        if (n > 0) s.seq_lens[b] = L + n;
     }
     __syncthreads();
     if (tid == 0) {
@@ -171,11 +165,23 @@ __device__ __forceinline__ void pg_move(const PagePools &pools, const int2 *pair
     }
 }
 
-__global__ void __launch_bounds__(256) pages_move_kernel(const __grid_constant__ PagePools pools, const int2 *__restrict__ pairs,
-                                                         const int *__restrict__ n_pairs, int n_pages)
+// the plan of an extend: tables and refs, 8 threads per row (one CTA's stores for 11,000 pages took 6 us), and the copies
+__global__ void __launch_bounds__(256) pages_extend_apply_kernel(const __grid_constant__ PagePools pools, PageState s, const int2 *__restrict__ pairs,
+                                                                 const int *__restrict__ n_pairs, const int4 *__restrict__ taken)
 {
     pdl_wait();
-    pg_move(pools, pairs, *n_pairs, n_pages);
+    for (int b = blockIdx.x * 32 + (threadIdx.x >> 3); b < s.B; b += gridDim.x * 32) {
+        const int4 t = taken[b];
+        int32_t *row = s.tables + (size_t)b * s.max_pages + t.z;
+#pragma unroll 4
+        for (int k = threadIdx.x & 7; k < t.y; k += 8) {
+            const int p = s.free_list[t.x - k];
+            if (pg_valid(p, s)) s.refs[p] = 1;
+            row[k] = p;
+        }
+        if ((threadIdx.x & 7) == 0 && t.w >= 0) atomicSub(s.refs + t.w, 1);
+    }
+    pg_move(pools, pairs, *n_pairs, s.n_pages);
 }
 
 // ---- fork: references and the new rows ----
@@ -234,15 +240,16 @@ pages_fork_write_kernel(PageState s, const int32_t *__restrict__ parents, const 
     const int words = (s.n_pages + 31) / 32, per = (words + kPgCluster - 1) / kPgCluster, w0 = min(rank * per, words), mine = min(per, words - w0);
     const int lane = tid & 31, warp = tid >> 5, nf = *s.n_free;
     // a word per warp: lane i looks at page i of it
-    for (int k0 = warp; k0 < mine; k0 += 32 * 4) {
-        unsigned bits[4];
-        bool dead[4];
+    constexpr int kAtOnce = 16;
+    for (int k0 = warp; k0 < mine; k0 += 32 * kAtOnce) {
+        unsigned bits[kAtOnce];
+        bool dead[kAtOnce];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) bits[j] = k0 + 32 * j < mine ? marks[w0 + k0 + 32 * j] : 0u;
+        for (int j = 0; j < kAtOnce; ++j) bits[j] = k0 + 32 * j < mine ? marks[w0 + k0 + 32 * j] : 0u;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) dead[j] = (bits[j] >> lane & 1) && s.refs[(w0 + k0 + 32 * j) * 32 + lane] == 0;
+        for (int j = 0; j < kAtOnce; ++j) dead[j] = (bits[j] >> lane & 1) && s.refs[(w0 + k0 + 32 * j) * 32 + lane] == 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < kAtOnce; ++j) {
             const unsigned m = __ballot_sync(0xffffffffu, dead[j]);
             if (k0 + 32 * j < mine && lane == 0) {
                 dead_s[k0 + 32 * j] = m;
@@ -382,16 +389,19 @@ lookat_status launch_pages_extend(Ctx *ctx, const PageState &s, int32_t *n_new, 
     int *count;
     int2 *pairs;
     int32_t *map;
-    lookat_status st = lists(ctx, s.B, 0, &count, &pairs, &map, "pages_extend");
+    const int even = (s.B + 1) / 2 * 2;                         // (what follows the pairs is 16-byte aligned)
+    lookat_status st = lists(ctx, even, (size_t)s.B * 4, &count, &pairs, &map, "pages_extend");
     if (st != LOOKAT_OK) return st;
+    int4 *taken = reinterpret_cast<int4 *>(map);
     const int smem = s.B * 16;                                  // 64 KB at most
-    if (smem > 40 * 1024 && cudaFuncSetAttribute(pages_extend_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+    if (smem > 40 * 1024 && cudaFuncSetAttribute(pages_extend_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
         return check_launch(ctx, "pages_extend: shared-memory opt-in");
-    pages_extend_kernel<<<1, kPgThreads, smem, ctx->stream>>>(s, n_new, pairs, count);
-    st = check_launch(ctx, "pages_extend_kernel");
-    if (st != LOOKAT_OK || pools.n == 0) return st;
-    launch_after(ctx, pages_move_kernel, move_grid(ctx, (long long)s.B * pools.items), 256, 0, pools, pairs, count, s.n_pages);
-    return check_launch(ctx, "pages_move_kernel");
+    pages_extend_plan_kernel<<<1, kPgThreads, smem, ctx->stream>>>(s, n_new, pairs, count, taken);
+    st = check_launch(ctx, "pages_extend_plan_kernel");
+    if (st != LOOKAT_OK) return st;
+    const unsigned movers = move_grid(ctx, (long long)s.B * pools.items), rows = (unsigned)(s.B + 31) / 32;
+    launch_after(ctx, pages_extend_apply_kernel, movers > rows ? movers : rows, 256, 0, pools, s, pairs, count, taken);
+    return check_launch(ctx, "pages_extend_apply_kernel");
 }
 
 lookat_status launch_pages_fork(Ctx *ctx, const PageState &s, const int32_t *parents)
