@@ -30,7 +30,10 @@ namespace {
 constexpr int kAqWarps = 4, kAqThreads = kAqWarps * 32;
 constexpr int kAqTile = 16 * kAqWarps;          // tokens of a CTA's step
 constexpr int kAqStages = 3;                    // tiles in a warp's ring
-constexpr int kAqMinChunk = 4;                  // steps per CTA below which a row is not cut
+// Cutting a unit costs about 5 us (pieces through global memory, a counter, the join), a step of a lone CTA 0.7 us: units of
+// up to kAqWhole steps stay whole (23 rows of 500 tokens, 8 KV heads: 12.7 us whole, 17 cut in two), pieces have at least
+// kAqMinChunk steps (one row of 1024 tokens, 12 heads: 11.4 us in pieces of 4, 14.2 of 8, 14.8 whole).
+constexpr int kAqWhole = 10, kAqMinChunk = 4;
 constexpr int kAqJoinCells = 1;                 // what joining a unit's results costs, in steps
 constexpr int kAqMaxParts = 128;                // pieces that a unit is cut into at most (one CTA joins them)
 constexpr float kAqSlack = 8.f;                 // how far scores may run ahead of M (base-2 units)
@@ -187,7 +190,7 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
         }
         total *= units;
         chunk = (total + gridDim.x - 1) / gridDim.x;
-        chunk = max(chunk, (long long)kAqJoinCells + max(min(kAqMinChunk, longest), (longest + kAqMaxParts - 2) / (kAqMaxParts - 1)));
+        chunk = max(chunk, (long long)kAqJoinCells + max(longest <= kAqWhole ? longest : kAqMinChunk, (longest + kAqMaxParts - 2) / (kAqMaxParts - 1)));
         pos = chunk * blockIdx.x;
         if (pos >= total) return;                               // (the whole CTA)
         end = (int)min(chunk, total - pos);
@@ -557,56 +560,58 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
     // ---- units of several CTAs: whoever brings the last piece joins them, in the order of the pieces ----
     asm volatile("cp.async.wait_group 0;" ::: "memory");
     float *const sF = reinterpret_cast<float *>(aq_raw);        // [col][kAqMaxParts]
-    __threadfence();
     __syncthreads();
     if (tid < n_split) {
         const int first = tid ? split_first[1] : split_first[0], pieces = tid ? split_pieces[1] : split_pieces[0];
+        __threadfence();                                        // the CTA's pieces (ordered before by the barrier), then the count
         const unsigned seen = atomicAdd(tickets + first, 1u);
+        __threadfence();                                        // the count, then what the others wrote
         s_i[tid] = seen == (unsigned)pieces - 1;
         if (seen == (unsigned)pieces - 1) tickets[first] = 0u;  // all pieces are in: ready for the next launch
     }
     __syncthreads();
     for (int u = 0; u < n_split; ++u) {
         if (!s_i[u]) continue;
-        __threadfence();
         const int first = u ? split_first[1] : split_first[0], pieces = u ? split_pieces[1] : split_pieces[0];
         const int b = u ? split_b[1] : split_b[0], unit = u ? split_unit[1] : split_unit[0];
         const float *const head = parts + (size_t)(2 * first + 1) * Lay::kPart, *const rest = parts + (size_t)2 * first * Lay::kPart;
         auto piece = [&](int p) { return p == 0 ? head : rest + (size_t)2 * p * Lay::kPart; };
+        const int n_here = min(Lay::kCols, n_cols - unit % groups * Lay::kCols) * quads;
         __syncthreads();
-        for (int col = warp; col < min(Lay::kCols, n_cols - unit % groups * Lay::kCols); col += kAqWarps) {           // a warp's lanes over the pieces of a column
-            float m[kAqMaxParts / 32], l = 0.f, top = -1e30f;
+        for (int col = warp; col < min(Lay::kCols, n_cols - unit % groups * Lay::kCols); col += kAqWarps) {    // a warp's lanes over the pieces
+            float m[kAqMaxParts / 32], lp[kAqMaxParts / 32], l = 0.f, top = -1e30f;
 #pragma unroll
             for (int i = 0; i < kAqMaxParts / 32; ++i) {
-                m[i] = lane + 32 * i < pieces ? __ldcg(piece(lane + 32 * i) + col) : -1e30f;
-                top = fmaxf(top, m[i]);
+                const bool on = lane + 32 * i < pieces;
+                m[i] = on ? __ldcg(piece(lane + 32 * i) + col) : -1e30f;
+                lp[i] = on ? __ldcg(piece(lane + 32 * i) + Lay::kCols + col) : 0.f;
             }
+#pragma unroll
+            for (int i = 0; i < kAqMaxParts / 32; ++i) top = fmaxf(top, m[i]);
 #pragma unroll
             for (int s = 16; s; s >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, s));
 #pragma unroll
-            for (int i = 0; i < kAqMaxParts / 32; ++i)
-                if (lane + 32 * i < pieces) {
-                    const float k = ex2_approx(m[i] - top);
-                    sF[col * kAqMaxParts + lane + 32 * i] = k;
-                    l = fmaf(k, __ldcg(piece(lane + 32 * i) + Lay::kCols + col), l);
-                }
+            for (int i = 0; i < kAqMaxParts / 32; ++i) {
+                const float k = ex2_approx(m[i] - top);
+                if (lane + 32 * i < pieces) sF[col * kAqMaxParts + lane + 32 * i] = k;
+                l = fmaf(k, lp[i], l);
+            }
 #pragma unroll
             for (int s = 16; s; s >>= 1) l += __shfl_xor_sync(0xffffffffu, l, s);
             if (lane == 0) sSum[col] = l;
         }
         __syncthreads();
-        const int n_here = min(Lay::kCols, n_cols - unit % groups * Lay::kCols) * quads;
         for (int i = tid; i < n_here; i += kAqThreads) {
-            const int col = i / quads, quad = i % quads, off = 2 * Lay::kCols + col * DP + quad * 4;
+            const int col = i / quads, quad = i % quads;
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int p0 = 0; p0 < pieces; p0 += 4) {
-                float4 y[4];
+            const int off = 2 * Lay::kCols + col * DP + quad * 4;
+            for (int p0 = 0; p0 < pieces; p0 += 16) {           // 16 loads in flight
+                float4 y[16];
 #pragma unroll
-                for (int p = 0; p < 4; ++p)
-                    if (p0 + p < pieces) y[p] = __ldcg(reinterpret_cast<const float4 *>(piece(p0 + p) + off));
+                for (int p = 0; p < 16; ++p)
+                    y[p] = p0 + p < pieces ? __ldcg(reinterpret_cast<const float4 *>(piece(p0 + p) + off)) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int p = 0; p < 4; ++p)
-                    if (p0 + p < pieces) add(x, sF[col * kAqMaxParts + p0 + p], y[p]);
+                for (int p = 0; p < 16; ++p) add(x, p0 + p < pieces ? sF[col * kAqMaxParts + p0 + p] : 0.f, y[p]);
             }
             store(b, unit, col, quad, x, sSum[col]);
         }
