@@ -18,6 +18,7 @@
 #define LOOKAT_GPT2_H
 
 #include "lookat.h"
+#include "lookat_q8.h"
 
 #ifdef __cplusplus
 extern "C" {
@@ -66,8 +67,26 @@ lookat_status lookat_gpt2_prefill(lookat_gpt2 *model, const int32_t *ids, int32_
  * next_ids int32 [B] (first index of the largest logit). */
 lookat_status lookat_gpt2_decode(lookat_gpt2 *model, const int32_t *ids, float *hidden_out, float *logits, int32_t *next_ids);
 
+/*
+ * The same model over the 8-bit paged cache (lookat_q8.h) instead of codes and fp16 values: the paper's scalar-quantised
+ * comparison, in a form that beams can share.  lookat_gpt2_use_q8_cache is called once, before the first prompt; it
+ * allocates B * ceil(capacity / page) pages per layer, which suffice however the rows share them.  From then on
+ * lookat_gpt2_prefill quantises the prompt's keys and values (no codebooks are fitted) and lookat_gpt2_decode makes room
+ * (lookat_pages_extend over the pools of all layers), appends and attends (lookat_q8_append, lookat_attend_q8) in every layer.
+ *
+ * lookat_gpt2_fork: every row continues from row parents[b] (device int32 [B], each in 0..B-1), as a beam search does
+ * between steps (lookat_pages_fork; the pages are shared until a row writes to one).
+ *
+ * lookat_gpt2_q8_state: a layer's cache and the page state of the batch (device pointers, for checks); either out pointer
+ * may be NULL.  All three return LOOKAT_ERR_INVALID_ARG where the model does not use (or already uses) that cache.
+ */
+lookat_status lookat_gpt2_use_q8_cache(lookat_gpt2 *model, int32_t page, int32_t format);
+lookat_status lookat_gpt2_fork(lookat_gpt2 *model, const int32_t *parents);
+lookat_status lookat_gpt2_q8_state(lookat_gpt2 *model, int32_t layer, lookat_q8_cache *cache, lookat_page_state *state);
+
 /* Device pointers to a layer's state (for checks): codebooks fp32 [H][m][K][64/m], codes uint8 [B][H][capacity][m],
- * values fp16 [B][H][capacity][64], prompt_keys fp16 [B][H][T][64] (NULL unless kept).  Any out pointer may be NULL. */
+ * values fp16 [B][H][capacity][64], prompt_keys fp16 [B][H][T][64] (NULL unless kept).  Any out pointer may be NULL.  With
+ * the 8-bit cache the first three are not written. */
 lookat_status lookat_gpt2_layer_state(lookat_gpt2 *model, int32_t layer, const float **codebooks, const uint8_t **codes,
                                       const void **values, const void **prompt_keys);
 

@@ -25,7 +25,7 @@ EXPORTS = [
     # include/lookat_gpt2.h
     "lookat_gpt2_create", "lookat_gpt2_destroy", "lookat_gpt2_last_error", "lookat_gpt2_set_weights", "lookat_gpt2_prefill",
     "lookat_gpt2_decode", "lookat_gpt2_layer_state", "lookat_gpt2_position", "lookat_gpt2_kernel_launches",
-    "lookat_gpt2_set_profile", "lookat_gpt2_profile",
+    "lookat_gpt2_set_profile", "lookat_gpt2_profile", "lookat_gpt2_use_q8_cache", "lookat_gpt2_fork", "lookat_gpt2_q8_state",
     "lookat_linear", "lookat_linear_qkv", "lookat_layernorm", "lookat_embed", "lookat_causal_attention", "lookat_argmax",
     # include/lookat_q8.h
     "lookat_q8_append", "lookat_attend_q8", "lookat_pages_extend", "lookat_pages_fork", "lookat_pages_compact",
@@ -148,6 +148,12 @@ def load_library(debug: bool = False) -> ctypes.CDLL:
     lib.lookat_gpt2_set_profile.restype = None
     lib.lookat_gpt2_profile.argtypes = [vp, ctypes.POINTER(ctypes.c_double)]
     lib.lookat_gpt2_profile.restype = i32
+    lib.lookat_gpt2_use_q8_cache.argtypes = [vp, i32, i32]
+    lib.lookat_gpt2_use_q8_cache.restype = i32
+    lib.lookat_gpt2_fork.argtypes = [vp, vp]
+    lib.lookat_gpt2_fork.restype = i32
+    lib.lookat_gpt2_q8_state.argtypes = [vp, i32, ctypes.POINTER(lookat_q8_cache), ctypes.POINTER(lookat_page_state)]
+    lib.lookat_gpt2_q8_state.restype = i32
     lib.lookat_linear.argtypes = [vp, vp, i32, vp, vp, i64, i32, i32, i32, vp, vp, i32]
     lib.lookat_linear.restype = i32
     lib.lookat_linear_qkv.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, i64, i64, vp, i64, i64, vp, i64, i64]
@@ -720,6 +726,28 @@ class LookatGpt2:
         return (view(ptrs[0], (H, c.m, c.K, 64 // c.m), torch.float32), view(ptrs[1], (self.B, H, cap, c.m), torch.uint8),
                 view(ptrs[2], (self.B, H, cap, 64), torch.float16),
                 view(ptrs[3], (self.B, H, T, 64), torch.float16) if T else None)
+
+    def lookat_gpt2_use_q8_cache(self, page=16, dtype=torch.int8):
+        """The 8-bit paged cache in place of codes and fp16 values; before the first prompt."""
+        if dtype not in (torch.int8, torch.float8_e4m3fn):
+            raise TypeError("dtype must be int8 or float8_e4m3fn")
+        self._check(self._lib.lookat_gpt2_use_q8_cache(self._h, page, 0 if dtype == torch.int8 else 1))
+
+    def lookat_gpt2_fork(self, parents):
+        """Row b continues from row parents[b] (int32 [B], each in 0..B-1)."""
+        self._check(self._lib.lookat_gpt2_fork(self._h, _on(parents, torch.int32, "parents", self.device, (self.B,))))
+
+    def lookat_gpt2_q8_state(self, layer):
+        """(k, k_amax, v, v_amax, tables, seq_lens, refs, free_list, n_free) of a layer's 8-bit cache and the batch's pages,
+        copied; k and v as bytes."""
+        q, ps, c = lookat_q8_cache(), lookat_page_state(), self.cfg
+        self._check(self._lib.lookat_gpt2_q8_state(self._h, layer, ctypes.byref(q), ctypes.byref(ps)))
+        self.stream.synchronize()
+        view = lambda ptr, shape, t: torch.as_tensor(_RawDeviceArray(ptr, shape, t), device=self.device).clone()  # noqa: E731
+        rows = (q.n_pages, c.n_head, q.page, 64)
+        return (view(q.k, rows, "|u1"), view(q.k_amax, rows[:2], "<f4"), view(q.v, rows, "|u1"), view(q.v_amax, rows[:2], "<f4"),
+                view(ps.tables, (ps.B, ps.max_pages), "<i4"), view(ps.seq_lens, (ps.B,), "<i4"), view(ps.refs, (ps.n_pages,), "<i4"),
+                view(ps.free_list, (ps.n_pages,), "<i4"), view(ps.n_free, (1,), "<i4"))
 
     def lookat_gpt2_set_profile(self, enabled: bool):
         self._lib.lookat_gpt2_set_profile(self._h, 1 if enabled else 0)

@@ -37,6 +37,13 @@ struct Gpt2 {
     std::vector<__half *> values;           // [B][H][capacity][64]
     std::vector<__half *> prompt_keys;      // [B][H][T][64], kept on request (tests)
     int pos;                                // tokens in the cache
+    // the 8-bit paged cache in place of codes and values (lookat_gpt2_use_q8_cache)
+    bool q8;
+    std::vector<lookat_q8_cache> q8_layers;
+    std::vector<lookat_page_pool> q8_pools; // k, k_amax, v, v_amax of every layer
+    lookat_page_state pages;
+    int32_t *page_ints, *ones, *counts;     // the page state's arrays; 1 per row (a step's tokens); the prompt's tokens per row, or -1
+    __half *v16, *vd;                       // [B][H][T][64] of the layer being processed (prompt pass), [B][H][64] of a step
     // optional per-category device timing of a decode step (events between the launches of one step)
     bool profile;
     std::vector<cudaEvent_t> prof_ev;       // boundaries, in launch order
@@ -65,6 +72,11 @@ bool dev_alloc(T **p, size_t n)
         return false;
     }
     return true;
+}
+
+__global__ void fill_ints_kernel(int32_t *p, int n, int value)
+{
+    for (int i = threadIdx.x; i < n; i += blockDim.x) p[i] = value;
 }
 
 #define G_TRY(expr)                                                                              \
@@ -185,7 +197,9 @@ void lookat_gpt2_destroy(lookat_gpt2 *handle)
     cudaGetDevice(&prev);
     cudaSetDevice(g->device);
     cudaStreamSynchronize(g->stream);
-    void *bufs[] = {g->x, g->a16, g->att16, g->fc16, g->q16, g->k16, g->qd, g->kd, g->attn_out, g->logits};
+    void *bufs[] = {g->x, g->a16, g->att16, g->fc16, g->q16, g->k16, g->qd, g->kd, g->attn_out, g->logits, g->v16, g->vd, g->page_ints};
+    for (const lookat_page_pool &p : g->q8_pools)
+        if (p.base) cudaFree(p.base);
     for (void *p : bufs)
         if (p) cudaFree(p);
     for (size_t l = 0; l < g->books.size(); ++l) {
@@ -251,6 +265,14 @@ lookat_status lookat_gpt2_prefill(lookat_gpt2 *handle, const int32_t *ids, int32
     const int d = c.d_model, H = c.n_head, B = g->B;
     const long long rows = (long long)B * T;
     G_TRY(launch_embed(ctx, ids, g->wte, g->wpe, g->x, rows, T, 0, d, c.vocab));
+    if (g->q8) {                                             // whatever the rows held is freed, then room for the prompt
+        for (int value : {-1, (int)T}) {
+            fill_ints_kernel<<<1, 32, 0, g->stream>>>(g->counts, B, value);
+            G_TRY(check_launch(ctx, "fill_ints_kernel"));
+            if (value < 0) G_TRY(lookat_pages_fork(g->attn, &g->pages, g->counts));
+            else G_TRY(lookat_pages_extend(g->attn, &g->pages, g->counts, nullptr, 0));
+        }
+    }
     for (int l = 0; l < c.n_layer; ++l) {
         const lookat_gpt2_layer &w = g->layers[l];
         G_TRY(launch_layernorm(ctx, g->x, (const __half *)w.ln1_g, (const __half *)w.ln1_b, g->a16, rows, d));
@@ -261,15 +283,19 @@ lookat_status lookat_gpt2_prefill(lookat_gpt2 *handle, const int32_t *ids, int32
         p.n_head = H;
         p.dst[0] = g->q16; p.cap[0] = T; p.off[0] = 0;
         p.dst[1] = g->k16; p.cap[1] = T; p.off[1] = 0;
-        p.dst[2] = g->values[l]; p.cap[2] = g->capacity; p.off[2] = 0;
+        p.dst[2] = g->q8 ? g->v16 : g->values[l]; p.cap[2] = g->q8 ? T : g->capacity; p.off[2] = 0;
         G_TRY(launch_linear(ctx, g->a16, 0, (const __half *)w.w_qkv, p));
         // the prompt attends exactly (Section 3.1): the codebooks do not exist yet
-        G_TRY(launch_causal_attention(ctx, g->q16, g->k16, g->values[l], g->att16, B, H, T, g->capacity));
+        G_TRY(launch_causal_attention(ctx, g->q16, g->k16, p.dst[2], g->att16, B, H, T, p.cap[2]));
         G_TRY(launch_linear(ctx, g->att16, 0, (const __half *)w.w_o, plain((const __half *)w.b_o, rows, d, d, 0, g->x, g->x, 0)));
         G_TRY(mlp(g, w, rows));
-        // Section 3.4: codebooks from the prompt's keys of every head, then the prompt's codes
-        G_TRY(lookat_fit_codebooks(g->attn, g->k16, B, T, c.fit_iters, seed + (uint64_t)l, nullptr, g->books[l], nullptr));
-        G_TRY(lookat_encode_keys(g->attn, g->k16, B, T, g->books[l], g->codes[l], g->capacity, 0, nullptr));
+        if (g->q8) {
+            G_TRY(lookat_q8_append(g->attn, &g->q8_layers[l], g->k16, g->v16, B, T, g->pages.tables, g->pages.max_pages, g->pages.seq_lens, nullptr));
+        } else {
+            // Section 3.4: codebooks from the prompt's keys of every head, then the prompt's codes
+            G_TRY(lookat_fit_codebooks(g->attn, g->k16, B, T, c.fit_iters, seed + (uint64_t)l, nullptr, g->books[l], nullptr));
+            G_TRY(lookat_encode_keys(g->attn, g->k16, B, T, g->books[l], g->codes[l], g->capacity, 0, nullptr));
+        }
         if (g->prompt_keys[l] &&
             cudaMemcpyAsync(g->prompt_keys[l], g->k16, (size_t)rows * d * sizeof(__half), cudaMemcpyDeviceToDevice, g->stream) != cudaSuccess)
             return g_fail(g, LOOKAT_ERR_CUDA, "copy of the prompt keys failed");
@@ -299,6 +325,10 @@ lookat_status lookat_gpt2_decode(lookat_gpt2 *handle, const int32_t *ids, float 
     mark(g, -1);                                             // opens the step
     G_TRY(launch_embed(ctx, ids, g->wte, g->wpe, g->x, B, 1, pos, d, c.vocab));
     mark(g, LOOKAT_GPT2_CAT_EMBED);
+    if (g->q8) {
+        G_TRY(lookat_pages_extend(g->attn, &g->pages, g->ones, g->q8_pools.data(), (int32_t)g->q8_pools.size()));
+        mark(g, LOOKAT_GPT2_CAT_ATTENTION);
+    }
     for (int l = 0; l < c.n_layer; ++l) {
         const lookat_gpt2_layer &w = g->layers[l];
         G_TRY(launch_layernorm(ctx, g->x, (const __half *)w.ln1_g, (const __half *)w.ln1_b, g->a16, B, d));
@@ -310,10 +340,17 @@ lookat_status lookat_gpt2_decode(lookat_gpt2 *handle, const int32_t *ids, float 
         p.dst[0] = g->qd; p.cap[0] = 1; p.off[0] = 0;
         p.dst[1] = g->kd; p.cap[1] = 1; p.off[1] = 0;
         p.dst[2] = g->values[l]; p.cap[2] = g->capacity; p.off[2] = pos;       // the value row goes straight into the cache
+        if (g->q8) { p.dst[2] = g->vd; p.cap[2] = 1; p.off[2] = 0; }
         G_TRY(launch_linear(ctx, g->a16, 0, (const __half *)w.w_qkv, p));
         mark(g, LOOKAT_GPT2_CAT_QKV);
-        // append (Section 3.4 "Encoding") and Algorithm 1 over tokens 0..pos, one launch
-        G_TRY(lookat_decode_step(g->attn, g->qd, g->kd, g->books[l], g->codes[l], g->values[l], B, g->capacity, pos, 0, g->attn_out));
+        if (g->q8) {
+            const lookat_page_state &ps = g->pages;
+            G_TRY(lookat_q8_append(g->attn, &g->q8_layers[l], g->kd, g->vd, B, 1, ps.tables, ps.max_pages, ps.seq_lens, nullptr));
+            G_TRY(lookat_attend_q8(g->attn, &g->q8_layers[l], g->qd, B, 1, ps.tables, ps.max_pages, ps.seq_lens, g->attn_out, 0));
+        } else {
+            // append (Section 3.4 "Encoding") and Algorithm 1 over tokens 0..pos, one launch
+            G_TRY(lookat_decode_step(g->attn, g->qd, g->kd, g->books[l], g->codes[l], g->values[l], B, g->capacity, pos, 0, g->attn_out));
+        }
         mark(g, LOOKAT_GPT2_CAT_ATTENTION);
         G_TRY(launch_linear(ctx, g->attn_out, 1, (const __half *)w.w_o, plain((const __half *)w.b_o, B, d, d, 0, g->x, g->x, 0)));
         mark(g, LOOKAT_GPT2_CAT_OUT_PROJ);
@@ -329,6 +366,87 @@ lookat_status lookat_gpt2_decode(lookat_gpt2 *handle, const int32_t *ids, float 
         mark(g, LOOKAT_GPT2_CAT_LM_HEAD);
     }
     g->pos = pos + 1;
+    return LOOKAT_OK;
+}
+
+lookat_status lookat_gpt2_use_q8_cache(lookat_gpt2 *handle, int32_t page, int32_t format)
+{
+    if (!handle) return LOOKAT_ERR_INVALID_ARG;
+    Gpt2 *g = reinterpret_cast<Gpt2 *>(handle);
+    g->err[0] = 0;
+    if (g->q8 || g->pos) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "use_q8_cache: call it once, before the first prompt");
+    if (page != 16 && page != 32 && page != 64 && page != 128) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "use_q8_cache: page=%d is not 16, 32, 64 or 128", page);
+    if (format != LOOKAT_Q8_INT8 && format != LOOKAT_Q8_E4M3) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "use_q8_cache: unknown 8-bit format %d", format);
+    const lookat_gpt2_config &c = g->cfg;
+    const size_t B = g->B, W = ((size_t)g->capacity + page - 1) / page, n_pages = B * W, d = c.d_model, H = c.n_head;
+    if (n_pages > (1u << 20) || 4 * c.n_layer > LOOKAT_MAX_POOLS)
+        return g_fail(g, LOOKAT_ERR_UNSUPPORTED, "use_q8_cache: %zu pages in %d arrays are more than a page state holds", n_pages, 4 * c.n_layer);
+    int prev = -1;
+    cudaGetDevice(&prev);
+    cudaSetDevice(g->device);
+    struct Restore { int d; ~Restore() { if (d >= 0) cudaSetDevice(d); } } restore{prev};
+    // [tables | seq_lens | refs | free_list | n_free | ones | counts], parts of a multiple of 4 ints
+    const size_t row_ints = (B + 3) / 4 * 4, page_ints = (n_pages + 3) / 4 * 4, table_ints = page_ints, total = table_ints + 3 * row_ints + 2 * page_ints + 4;
+    std::vector<int32_t> ints(total, 0);
+    int32_t *const free_list = ints.data() + table_ints + row_ints + page_ints, *const n_free = free_list + page_ints;
+    for (size_t i = 0; i < n_pages; ++i) ints[i] = -1, free_list[i] = (int32_t)(n_pages - 1 - i);
+    n_free[0] = (int32_t)n_pages;
+    for (size_t i = 0; i < B; ++i) n_free[4 + i] = 1;
+    bool ok = dev_alloc(&g->page_ints, total) && dev_alloc(&g->v16, B * g->capacity * d) && dev_alloc(&g->vd, B * d);
+    for (int l = 0; ok && l < c.n_layer; ++l) {
+        lookat_q8_cache q = {nullptr, nullptr, nullptr, nullptr, (int32_t)n_pages, page, format};
+        for (int i = 0; ok && i < 4; ++i) {
+            const size_t bytes = (i & 1) ? H * sizeof(float) : d * page;
+            unsigned char *p = nullptr;
+            ok = dev_alloc(&p, n_pages * bytes) && cudaMemsetAsync(p, 0, n_pages * bytes, g->stream) == cudaSuccess;
+            g->q8_pools.push_back({p, (int64_t)bytes});
+            (i == 0 ? q.k : i == 2 ? q.v : (i == 1 ? *reinterpret_cast<void **>(&q.k_amax) : *reinterpret_cast<void **>(&q.v_amax))) = p;
+        }
+        g->q8_layers.push_back(q);
+    }
+    if (ok) ok = cudaMemcpyAsync(g->page_ints, ints.data(), total * 4, cudaMemcpyHostToDevice, g->stream) == cudaSuccess &&
+                 cudaStreamSynchronize(g->stream) == cudaSuccess;
+    if (!ok) {
+        cudaGetLastError();
+        void *bufs[] = {g->page_ints, g->v16, g->vd};
+        for (void *p : bufs)
+            if (p) cudaFree(p);
+        for (const lookat_page_pool &p : g->q8_pools)
+            if (p.base) cudaFree(p.base);
+        g->page_ints = nullptr;
+        g->v16 = g->vd = nullptr;
+        g->q8_pools.clear();
+        g->q8_layers.clear();
+        return g_fail(g, LOOKAT_ERR_NOMEM, "use_q8_cache: no device memory for the pages");
+    }
+    int32_t *const p = g->page_ints;
+    g->pages = {p, p + table_ints, p + table_ints + row_ints, p + table_ints + row_ints + page_ints, p + table_ints + row_ints + 2 * page_ints,
+                (int32_t)B, (int32_t)W, (int32_t)n_pages, page};
+    g->ones = g->pages.n_free + 4;
+    g->counts = g->ones + row_ints;
+    g->q8 = true;
+    return LOOKAT_OK;
+}
+
+lookat_status lookat_gpt2_fork(lookat_gpt2 *handle, const int32_t *parents)
+{
+    if (!handle) return LOOKAT_ERR_INVALID_ARG;
+    Gpt2 *g = reinterpret_cast<Gpt2 *>(handle);
+    g->err[0] = 0;
+    if (!g->q8) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "fork: the model does not use the 8-bit paged cache");
+    G_TRY(lookat_pages_fork(g->attn, &g->pages, parents));
+    return LOOKAT_OK;
+}
+
+lookat_status lookat_gpt2_q8_state(lookat_gpt2 *handle, int32_t layer, lookat_q8_cache *cache, lookat_page_state *state)
+{
+    if (!handle) return LOOKAT_ERR_INVALID_ARG;
+    Gpt2 *g = reinterpret_cast<Gpt2 *>(handle);
+    g->err[0] = 0;
+    if (!g->q8) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "q8_state: the model does not use the 8-bit paged cache");
+    if (layer < 0 || layer >= g->cfg.n_layer) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "layer %d out of range", layer);
+    if (cache) *cache = g->q8_layers[layer];
+    if (state) *state = g->pages;
     return LOOKAT_OK;
 }
 
