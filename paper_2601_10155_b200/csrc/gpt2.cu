@@ -74,6 +74,42 @@ bool dev_alloc(T **p, size_t n)
     return true;
 }
 
+// the 8-bit cache's arrays and the page state of empty rows; false if device memory runs out
+bool q8_allocate(Gpt2 *g, int page, int format, size_t W, size_t n_pages)
+{
+    const lookat_gpt2_config &c = g->cfg;
+    const size_t B = g->B, d = c.d_model, H = c.n_head;
+    // [tables | seq_lens | refs | free_list | n_free | ones | counts], parts of a multiple of 4 ints
+    const size_t row_ints = (B + 3) / 4 * 4, page_ints = (n_pages + 3) / 4 * 4, total = 3 * page_ints + 3 * row_ints + 4;
+    std::vector<int32_t> ints(total, 0);
+    g->q8_pools.reserve(4 * (size_t)c.n_layer);
+    g->q8_layers.reserve(c.n_layer);
+    const size_t at_refs = page_ints + row_ints, at_free = at_refs + page_ints, at_n_free = at_free + page_ints, at_ones = at_n_free + 4;
+    for (size_t i = 0; i < n_pages; ++i) {
+        ints[i] = -1;
+        ints[at_free + i] = (int32_t)(n_pages - 1 - i);
+    }
+    ints[at_n_free] = (int32_t)n_pages;
+    for (size_t i = 0; i < B; ++i) ints[at_ones + i] = 1;
+    if (!dev_alloc(&g->page_ints, total) || !dev_alloc(&g->v16, B * g->capacity * d) || !dev_alloc(&g->vd, B * d)) return false;
+    for (int l = 0; l < c.n_layer; ++l) {
+        const size_t bytes[4] = {d * page, H * sizeof(float), d * page, H * sizeof(float)};
+        unsigned char *p[4];
+        for (int i = 0; i < 4; ++i) {
+            if (!dev_alloc(&p[i], n_pages * bytes[i])) return false;
+            g->q8_pools.push_back({p[i], (int64_t)bytes[i]});
+            if (cudaMemsetAsync(p[i], 0, n_pages * bytes[i], g->stream) != cudaSuccess) return false;
+        }
+        g->q8_layers.push_back({p[0], reinterpret_cast<float *>(p[1]), p[2], reinterpret_cast<float *>(p[3]), (int32_t)n_pages, page, format});
+    }
+    int32_t *const q = g->page_ints;
+    g->pages = {q, q + page_ints, q + at_refs, q + at_free, q + at_n_free, (int32_t)B, (int32_t)W, (int32_t)n_pages, page};
+    g->ones = q + at_ones;
+    g->counts = g->ones + row_ints;
+    return cudaMemcpyAsync(q, ints.data(), total * sizeof(int32_t), cudaMemcpyHostToDevice, g->stream) == cudaSuccess &&
+           cudaStreamSynchronize(g->stream) == cudaSuccess;
+}
+
 __global__ void fill_ints_kernel(int32_t *p, int n, int value)
 {
     for (int i = threadIdx.x; i < n; i += blockDim.x) p[i] = value;
@@ -378,54 +414,33 @@ lookat_status lookat_gpt2_use_q8_cache(lookat_gpt2 *handle, int32_t page, int32_
     if (page != 16 && page != 32 && page != 64 && page != 128) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "use_q8_cache: page=%d is not 16, 32, 64 or 128", page);
     if (format != LOOKAT_Q8_INT8 && format != LOOKAT_Q8_E4M3) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "use_q8_cache: unknown 8-bit format %d", format);
     const lookat_gpt2_config &c = g->cfg;
-    const size_t B = g->B, W = ((size_t)g->capacity + page - 1) / page, n_pages = B * W, d = c.d_model, H = c.n_head;
+    const size_t W = ((size_t)g->capacity + page - 1) / page, n_pages = g->B * W;
     if (n_pages > (1u << 20) || 4 * c.n_layer > LOOKAT_MAX_POOLS)
         return g_fail(g, LOOKAT_ERR_UNSUPPORTED, "use_q8_cache: %zu pages in %d arrays are more than a page state holds", n_pages, 4 * c.n_layer);
     int prev = -1;
     cudaGetDevice(&prev);
     cudaSetDevice(g->device);
     struct Restore { int d; ~Restore() { if (d >= 0) cudaSetDevice(d); } } restore{prev};
-    // [tables | seq_lens | refs | free_list | n_free | ones | counts], parts of a multiple of 4 ints
-    const size_t row_ints = (B + 3) / 4 * 4, page_ints = (n_pages + 3) / 4 * 4, table_ints = page_ints, total = table_ints + 3 * row_ints + 2 * page_ints + 4;
-    std::vector<int32_t> ints(total, 0);
-    int32_t *const free_list = ints.data() + table_ints + row_ints + page_ints, *const n_free = free_list + page_ints;
-    for (size_t i = 0; i < n_pages; ++i) ints[i] = -1, free_list[i] = (int32_t)(n_pages - 1 - i);
-    n_free[0] = (int32_t)n_pages;
-    for (size_t i = 0; i < B; ++i) n_free[4 + i] = 1;
-    bool ok = dev_alloc(&g->page_ints, total) && dev_alloc(&g->v16, B * g->capacity * d) && dev_alloc(&g->vd, B * d);
-    for (int l = 0; ok && l < c.n_layer; ++l) {
-        lookat_q8_cache q = {nullptr, nullptr, nullptr, nullptr, (int32_t)n_pages, page, format};
-        for (int i = 0; ok && i < 4; ++i) {
-            const size_t bytes = (i & 1) ? H * sizeof(float) : d * page;
-            unsigned char *p = nullptr;
-            ok = dev_alloc(&p, n_pages * bytes) && cudaMemsetAsync(p, 0, n_pages * bytes, g->stream) == cudaSuccess;
-            g->q8_pools.push_back({p, (int64_t)bytes});
-            (i == 0 ? q.k : i == 2 ? q.v : (i == 1 ? *reinterpret_cast<void **>(&q.k_amax) : *reinterpret_cast<void **>(&q.v_amax))) = p;
-        }
-        g->q8_layers.push_back(q);
+    bool ok = false;
+    try {
+        ok = q8_allocate(g, page, format, W, n_pages);
+    } catch (const std::bad_alloc &) {                       // (no exception leaves a C entry point)
     }
-    if (ok) ok = cudaMemcpyAsync(g->page_ints, ints.data(), total * 4, cudaMemcpyHostToDevice, g->stream) == cudaSuccess &&
-                 cudaStreamSynchronize(g->stream) == cudaSuccess;
-    if (!ok) {
-        cudaGetLastError();
-        void *bufs[] = {g->page_ints, g->v16, g->vd};
-        for (void *p : bufs)
-            if (p) cudaFree(p);
-        for (const lookat_page_pool &p : g->q8_pools)
-            if (p.base) cudaFree(p.base);
-        g->page_ints = nullptr;
-        g->v16 = g->vd = nullptr;
-        g->q8_pools.clear();
-        g->q8_layers.clear();
-        return g_fail(g, LOOKAT_ERR_NOMEM, "use_q8_cache: no device memory for the pages");
+    if (ok) {
+        g->q8 = true;
+        return LOOKAT_OK;
     }
-    int32_t *const p = g->page_ints;
-    g->pages = {p, p + table_ints, p + table_ints + row_ints, p + table_ints + row_ints + page_ints, p + table_ints + row_ints + 2 * page_ints,
-                (int32_t)B, (int32_t)W, (int32_t)n_pages, page};
-    g->ones = g->pages.n_free + 4;
-    g->counts = g->ones + row_ints;
-    g->q8 = true;
-    return LOOKAT_OK;
+    cudaGetLastError();
+    void *bufs[] = {g->page_ints, g->v16, g->vd};
+    for (void *p : bufs)
+        if (p) cudaFree(p);
+    for (const lookat_page_pool &p : g->q8_pools)
+        if (p.base) cudaFree(p.base);
+    g->page_ints = nullptr;
+    g->v16 = g->vd = nullptr;
+    g->q8_pools.clear();
+    g->q8_layers.clear();
+    return g_fail(g, LOOKAT_ERR_NOMEM, "use_q8_cache: no memory for the pages");
 }
 
 lookat_status lookat_gpt2_fork(lookat_gpt2 *handle, const int32_t *parents)

@@ -458,6 +458,93 @@ def test_a_captured_step_replays_like_the_calls():
     assert torch.equal(results[0][2], results[1][2])
 
 
+def test_a_captured_prompt_in_pieces_replays():
+    """Few queries over many tokens (two kernels, the second launched early) from a graph, inputs changed between replays."""
+    rng = np.random.default_rng(23)
+    lens = [2100, 400]
+    k, ka, v, va, tables = make_cache(rng, lens, 64, 2, 128, 128, "int8")
+    cache, stream = on_gpu(k, ka, v, va, "int8"), torch.cuda.Stream()
+    tb, sl = dev(tables), dev(np.array(lens, np.int32))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        lk = Lookat(4, 2, 128, 128, 1, 16, stream=stream)
+        q, out = torch.zeros((2, 4, 50, 128), dtype=torch.float16, device="cuda"), torch.empty((2, 4, 50, 128), device="cuda")
+        lk.lookat_attend_q8(cache, q, tb, sl, out=out)
+        stream.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=stream):
+            lk.lookat_attend_q8(cache, q, tb, sl, out=out)
+        for _ in range(3):
+            q.copy_(dev(rng.standard_normal((2, 4, 50, 128)).astype(np.float16)))
+            g.replay()
+            got = out.clone()
+            want = lk.lookat_attend_q8(cache, q, tb, sl)
+            stream.synchronize()
+            assert torch.equal(got, want)
+        del g
+
+
+def test_two_contexts_on_two_streams_at_once():
+    """Each context has its workspace: calls that overlap on the GPU do not touch one another's pieces."""
+    rng = np.random.default_rng(24)
+    lens = [6000, 300, 4000]
+    k, ka, v, va, tables = make_cache(rng, lens, 32, 2, 128, 128, "e4m3")
+    cache, tb, sl = on_gpu(k, ka, v, va, "e4m3"), dev(tables), dev(np.array(lens, np.int32))
+    qs = [dev((rng.standard_normal((3, 8, L_q, 128))).astype(np.float16)) for L_q in (1, 20)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in qs]
+    lks = [Lookat(8, 2, 128, 128, 1, 16, stream=s) for s in streams]
+    want = []
+    for lk, q in zip(lks, qs):
+        want.append(lk.lookat_attend_q8(cache, q, tb, sl))
+        torch.cuda.synchronize()
+    for _ in range(20):
+        got = [lk.lookat_attend_q8(cache, q, tb, sl) for lk, q in zip(lks, qs)]
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_offsets_beyond_32_bits():
+    """A cache of 5 GB per array, rows in its last pages."""
+    if torch.cuda.mem_get_info()[0] < 16 << 30:
+        pytest.skip("needs 16 GB of device memory")
+    rng = np.random.default_rng(25)
+    H, P, d, n_pages, lens = 8, 128, 128, 40000, [300, 5]
+    small_k, small_ka, small_v, small_va, tables = make_cache(rng, lens, P, H, d, d, "int8", spare=0)
+    cache = Q8Cache.empty(n_pages, H, P, d, d)
+    first = n_pages - small_k.shape[0]
+    for t, x in zip(cache.pools(), (small_k.view(np.int8), small_ka, small_v.view(np.int8), small_va)):
+        t[first:] = dev(x)
+    moved = np.where(tables >= 0, tables + first, -1).astype(np.int32)
+    lk = Lookat(16, H, d, d, 1, 16)
+    for L_q in (1, 40):
+        q = rng.standard_normal((2, 16, L_q, d)).astype(np.float16)
+        got = lk.lookat_attend_q8(cache, dev(q), dev(moved), dev(np.array(lens, np.int32)))
+        out, mag, reach = q8.attend(small_k, small_ka, small_v, small_va, q, tables, lens, "int8", lk.scale)
+        assert (np.abs(got.double().cpu().numpy() - out) <= attend_bound(out, mag, reach, d, 300, np.nanmax(small_va), False)).all()
+    x = [rng.standard_normal((2, H, 9, d)).astype(np.float16) for _ in range(2)]
+    lk.lookat_q8_append(cache, dev(x[0]), dev(x[1]), dev(moved), dev(np.array(lens, np.int32)))
+    # (row 1 holds 5 tokens: it would begin before its first one)
+    for raw, a, y in ((small_k, small_ka, x[0]), (small_v, small_va, x[1])):
+        q8.append(raw, a, y, tables, lens, [9, 9], "int8")
+    torch.cuda.synchronize()
+    for t, r in zip(cache.pools(), (small_k, small_ka, small_v, small_va)):
+        got = t[first:].contiguous()
+        assert np.array_equal(host8(got) if t.element_size() == 1 else got.cpu().numpy(), r)
+    # the same pages moved to the front
+    ps = PageState.empty(2, 3, n_pages, P)
+    ps.tables[:, :moved.shape[1]] = dev(moved)
+    ps.seq_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+    held = torch.tensor([p for row in moved for p in row if p >= 0], device="cuda")
+    ps.refs[held] = 1
+    before = [t[torch.sort(held).values].clone() for t in cache.pools()]
+    lk.lookat_pages_compact(ps, cache.pools())
+    torch.cuda.synchronize()
+    assert int(ps.n_free) == n_pages - len(held)
+    for t, b in zip(cache.pools(), before):
+        assert torch.equal(t[:len(held)].view(torch.uint8), b.view(torch.uint8))
+
+
 def test_a_capture_that_would_have_to_allocate_is_refused_and_old_graphs_stay_valid():
     rng = np.random.default_rng(22)
     lens = [50, 20]
