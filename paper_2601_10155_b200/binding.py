@@ -207,9 +207,9 @@ def _host(t, dtype, name, shape):
 
 def _on(t, dtype, name, device, shape=None):
     """_dev, and the tensor lies on the context's device."""
-    if isinstance(t, torch.Tensor) and t.device == device and t.is_cuda and t.dtype is dtype and t.is_contiguous() and \
+    if isinstance(t, torch.Tensor) and t.get_device() == device.index and t.dtype is dtype and t.is_contiguous() and \
             (shape is None or t.shape == shape):
-        return t.data_ptr()                                     # (the checks of the lines below, in the order of their cost)
+        return t.data_ptr()                                     # (what the lines below check, at less cost)
     p = _dev(t, dtype, name, shape)
     if t is not None and t.device != device:
         raise ValueError(f"{name} is on {t.device}, the context on {device}")
@@ -515,7 +515,8 @@ class Lookat:
         dtype = torch.float16 if out_fp16 else torch.float32
         shape = (B, H, d_v) if one else (B, H, L_q, d_v)
         if out is None:
-            out = q.new_empty(shape, dtype=dtype)
+            n = L_q * d_v                                       # (dense; empty_strided takes half the time of empty)
+            out = torch.empty_strided(shape, (H * d_v, d_v, 1) if one else (H * n, n, d_v, 1), dtype=dtype, device=dev)
             if torch._C._cuda_getCurrentRawStream(dev.index) != self._raw_stream:
                 out.record_stream(self.stream)                  # allocated for another stream than the one that writes it
             po = out.data_ptr()
