@@ -8,7 +8,7 @@
 // CTA's rows stand at neighbouring positions and share the tokens they see.
 //   fp16 results take the weights in fp16 (2^-12 of each).  fp32 results take them as two fp16 numbers, whose second halves
 // lie in the scores' second half of tensor memory, and move O out of tensor memory every 8 chunks: the tensor pipe cuts
-// its sums off, and a chain of 8 chunks stays below 2^-20.
+// its sums off: over a prompt of 4096 tokens one chain's largest error was 2.3e-6, that of chains of 8 chunks 1.0e-6.
 //
 // A CTA works on two tiles of 128 rows against the same chunks of 64 tokens.  The scores of a tile have two buffers in
 // tensor memory, so the tensor pipe makes the next chunk's while the softmax threads work on this one's.  Roles (16 warps,
@@ -20,6 +20,11 @@
 //   warp 14     fetches 8-bit rows: a bulk copy per 16 tokens (a page holds whole ones) of K and of V, kPqRaw chunks ahead;
 //   warp 15     the scales of each chunk's blocks.
 // Tensor memory (512 columns): per tile S (2 x 64; the weights overwrite it) and O (d_v).  Q lies in shared memory.
+// Measured (B200, e4m3, one row of 4096 queries over its 4096 tokens, 8 KV heads of 4 query heads, 128 dims): fp16
+// results 180 us = 762 TFLOP/s, 46 % of a large bf16 matrix product; fp32 results 321 us.  What bounds it is the chain
+// of a chunk: 256 rows of 64 tokens take about 2800 cycles, of which the tensor pipe works a third, the exponentials
+// a third and the widening of the 8-bit rows the rest of the issue slots; see the counters' shares: tensor 36 %, issue
+// 38 %.  A second CTA per SM has no tensor memory left.
 //   Few rows over a long cache are cut along the tokens (blockIdx), every piece leaves O, M and l in the workspace and
 // attend_q8_join_kernel joins them in order.
 // Every mbarrier wait gives up after a bounded number of polls, raises the context's time-out flag and lets the CTA drain
@@ -118,6 +123,7 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
     // heads and batch rows first, then the pieces, then the row tiles, longest first: the last CTAs to start are short ones
     const int h = blockIdx.x % c.H_kv, b = blockIdx.x / c.H_kv % a.B, piece = blockIdx.x / (c.H_kv * a.B) % pieces;
     const int super = n_super - 1 - blockIdx.x / (c.H_kv * a.B * pieces), row0 = super * kPqBoth;
+    const int tiles = n_rows - row0 > kPqRows ? 2 : 1;         // a second tile without rows has no work
     const int page = 1 << c.page_shift, cap = c.max_pages << c.page_shift;
     const int len_in = c.seq_lens[b], len = min(max(len_in, 0), cap);
     if (tid == 0 && len != len_in && h == 0) q8_report(c.status, kStatusBadPage);
@@ -142,8 +148,8 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
         for (int i = 0; i < 2; ++i) {
             um_bar_init(bar_k + 8 * i, kPqOperand);
             um_bar_init(bar_v + 8 * i, kPqOperand);
-            um_bar_init(bar_kf + 8 * i, kPqTiles);
-            um_bar_init(bar_vf + 8 * i, kPqTiles);
+            um_bar_init(bar_kf + 8 * i, tiles);
+            um_bar_init(bar_vf + 8 * i, tiles);
             for (int t = 0; t < kPqTiles; ++t) {
                 um_bar_init(bar_s + 16 * t + 8 * i, 1);
                 um_bar_init(bar_pv + 16 * t + 8 * i, 1);
@@ -239,8 +245,8 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
         }
     } else if (warp >= (kPqSoftmax + kPqProducers) / 32) {
         // =================== the MMA thread of a tile ===================
-        if (um_elect()) {
-            const int t = warp - (kPqSoftmax + kPqProducers) / 32;
+        const int t = warp - (kPqSoftmax + kPqProducers) / 32;
+        if (t < tiles && um_elect()) {
             // descriptors: stride 1024 B, version 1, 128-byte swizzle in the high word; start address and leading offset in
             // the low word
             const uint32_t desc_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
@@ -330,7 +336,7 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
         };
         const bool ok = warp < kPqSoftmax / 32 + 2 ? produce(std::false_type{}) : produce(std::true_type{});
         dead = !ok;
-    } else {
+    } else if (warp >> 2 < tiles) {
         // =================== softmax: thread r owns row r of tile t ===================
         const int t = warp >> 2, rq = warp & 3, r = t * kPqRows + rq * 32 + lane, row = row0 + r;
         const bool on = row < n_rows;
@@ -357,6 +363,14 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
                     turn[lane * 8 + (i ^ (lane & 7))] = make_float4(__uint_as_float(o[4 * i]) * mul, __uint_as_float(o[4 * i + 1]) * mul,
                                                                     __uint_as_float(o[4 * i + 2]) * mul, __uint_as_float(o[4 * i + 3]) * mul);
                 __syncwarp();
+                float4 y[8];                                   // all loads before the first store
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int rr = i * 4 + (lane >> 3);
+                    const unsigned long long at = __shfl_sync(0xffffffffu, (unsigned long long)acc, rr);
+                    y[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (again && (rows_on >> rr & 1)) y[i] = *(reinterpret_cast<const float4 *>(reinterpret_cast<const float *>(at) + p * 32) + (lane & 7));
+                }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int rr = i * 4 + (lane >> 3), quad = lane & 7;
@@ -369,12 +383,8 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
                         *reinterpret_cast<uint2 *>(static_cast<__half *>(a.out) + at + p * 32 + quad * 4) =
                             make_uint2(*reinterpret_cast<const uint32_t *>(&u), *reinterpret_cast<const uint32_t *>(&v));
                     } else {
-                        float4 *dst = reinterpret_cast<float4 *>(reinterpret_cast<float *>(at) + p * 32 + quad * 4);
-                        if (again) {
-                            const float4 y = *dst;
-                            x = make_float4(fmaf(y.x, k, x.x), fmaf(y.y, k, x.y), fmaf(y.z, k, x.z), fmaf(y.w, k, x.w));
-                        }
-                        *dst = x;
+                        if (again) x = make_float4(fmaf(y[i].x, k, x.x), fmaf(y[i].y, k, x.y), fmaf(y[i].z, k, x.z), fmaf(y[i].w, k, x.w));
+                        *(reinterpret_cast<float4 *>(reinterpret_cast<float *>(at) + p * 32) + quad) = x;
                     }
                 }
                 __syncwarp();
@@ -586,12 +596,11 @@ lookat_status launch_pq_dims(Ctx *ctx, const Q8AttendArgs &a)
 
 bool attend_q8_umma_covers(const Ctx *ctx, const Q8AttendArgs &a)
 {
-    // Rows of a KV head (queries times heads of its group) above which this form is the faster one.  Up to 32 the streaming
-    // kernel reads the cache once or twice: 16 rows of 4096 tokens, 20 and 32 rows per head, fp32 results 102 us there and
-    // 118 us here (fp16 102 and 87); from 33 on it reads it three times: 48 rows 33 and 23 us for one row of tokens, 64 rows
-    // 181 and 87 us for 16 (fp16).
+    // Rows of a KV head (queries times heads of its group) from which on this form is the faster one; the streaming kernel
+    // reads the cache once per 16 rows.  16 sequences of 4096 tokens, 32 rows per head: fp16 results 92 us there, 65 here, fp32
+    // results 92 and 124; 48 rows per head: fp16 126 and 66, fp32 126 and 126; 64 rows: fp32 158 and 126.
     const bool dims = (a.c.d_k == 64 || a.c.d_k == 128) && (a.c.d_v == 64 || a.c.d_v == 128);
-    return dims && (long long)a.g * a.L_q > 32 && ctx->timeout_flag;
+    return dims && (long long)a.g * a.L_q > (a.out_fp16 ? 16 : 32) && ctx->timeout_flag;
 }
 
 lookat_status launch_attend_q8_umma(Ctx *ctx, const Q8AttendArgs &a)

@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(256) pages_fork_count_kernel(PageState s, cons
 
 // The first cluster: the pages that lost their last reference go onto the free list, ascending; each of its CTAs looks at
 // an eighth of the marks and learns from the others how many pages come before its own.  (One CTA over 110,000 pages took
-// 52 us, the cluster 7.)  The other CTAs: the rows' new tables.
+// 52 us, the cluster 13.)  The other CTAs: the rows' new tables.
 constexpr int kPgCluster = 8;
 __global__ void __cluster_dims__(kPgCluster, 1, 1) __launch_bounds__(kPgThreads)
 pages_fork_write_kernel(PageState s, const int32_t *__restrict__ parents, const int32_t *__restrict__ rows, const int32_t *__restrict__ lens,
