@@ -75,7 +75,8 @@ lookat_status lookat_q8_append(lookat_ctx *ctx, const lookat_q8_cache *cache, co
  * Attention over the cache: for query i of L_q, at position p = seq_lens[b] - L_q + i,
  *   s_t = q . k_t * scale,  alpha = softmax of s over the tokens t = 0..p,  o = sum_t alpha_t v_t.
  * One generated token (L_q = 1), a few draft tokens, or a prompt or a piece of it.  A query without a token to attend
- * (p < 0, an empty row) gives zeros.
+ * (p < 0, an empty row) gives zeros.  What lies behind a row's last token may be anything; the row's own numbers and
+ * scales are finite (lookat_q8_append writes no others: a NaN among the values reaches every query of the row).
  *
  *   q          fp16 [B][H_q][L_q][d_k]
  *   tables     int32 [B][max_pages];  seq_lens  int32 [B]
@@ -117,7 +118,7 @@ enum { LOOKAT_MAX_POOLS = 256 };
  * every pool -- the last of the holders keeps the page --, then a page for each further block.  Pages come off the top
  * of the free list.  All or nothing: if the pages do not suffice, a row would pass max_pages, or a length or a begun page's
  * entry is out of range, nothing changes but n_new, which is set to 0 for every row, and lookat_last_error reports it.
- *   n_new   in/out int32 [B]; negative counts are taken as 0
+ *   n_new   in/out int32 [B]; negative counts are taken as 0, and a row with 0 keeps its pages as they are
  */
 lookat_status lookat_pages_extend(lookat_ctx *ctx, const lookat_page_state *state, int32_t *n_new, const lookat_page_pool *pools,
                                   int32_t n_pools);
