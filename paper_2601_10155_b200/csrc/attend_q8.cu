@@ -35,10 +35,14 @@ constexpr int kAqWarps = 4, kAqThreads = kAqWarps * 32;
 constexpr int kAqTile = 16 * kAqWarps;          // tokens of a CTA's step
 constexpr int kAqStages = 3;                    // tiles in a warp's ring
 // Cutting a unit costs about 5 us (pieces through global memory, a counter, the join), a step of a lone CTA 0.7 us: units of
-// up to kAqWhole steps stay whole (23 rows of 500 tokens, 8 KV heads: 12.7 us whole, 17 cut in two), pieces have at least
-// kAqMinChunk steps (one row of 1024 tokens, 12 heads: 11.4 us in pieces of 4, 14.2 of 8, 14.8 whole).
-constexpr int kAqWhole = 10, kAqMinChunk = 4;
-constexpr int kAqJoinCells = 1;                 // what joining a unit's results costs, in steps
+// up to kAqWhole steps stay whole (rows of 200 to 900 tokens, 8 KV heads: 16.3 us, 24.1 with units of up to 16 steps whole;
+// rows of 500 tokens, 16 columns: 19 us whole, 23 cut), a CTA's part has at least kAqMinChunk steps and a cell (one row of
+// 1024 tokens, 12 heads: 9.5 us with 3, 10.0 with 4, 11.3 with 6, 14.4 whole).  What joining a unit costs weighs as much as
+// kAqJoinCells steps when the work is cut (23 rows of up to 8189 tokens, 16 columns: 78.5 us with 1, 65 with 3, 64 with 4,
+// 63 with 6; rows of 32768 tokens, 4 columns: 173, 171, 169, 169; rows of up to 4000 tokens, 8 columns of 64 dims: 15.9,
+// 15.5, 14.8, 16.2).
+constexpr int kAqWhole = 10, kAqMinChunk = 3;
+constexpr int kAqJoinCells = 4;
 constexpr int kAqMaxParts = 128;                // pieces that a unit is cut into at most (one CTA joins them)
 constexpr float kAqSlack = 8.f;                 // how far scores may run ahead of M (base-2 units)
 
@@ -194,7 +198,7 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
         }
         total *= units;
         chunk = (total + gridDim.x - 1) / gridDim.x;
-        chunk = max(chunk, (long long)kAqJoinCells + max(longest <= kAqWhole ? longest : kAqMinChunk, (longest + kAqMaxParts - 2) / (kAqMaxParts - 1)));
+        chunk = max(chunk, (long long)max(longest <= kAqWhole ? kAqJoinCells + longest : 1 + kAqMinChunk, 1 + (longest + kAqMaxParts - 2) / (kAqMaxParts - 1)));
         pos = chunk * blockIdx.x;
         if (pos >= total) return;                               // (the whole CTA)
         end = (int)min(chunk, total - pos);
