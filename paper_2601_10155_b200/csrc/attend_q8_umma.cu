@@ -597,8 +597,8 @@ lookat_status launch_pq_dims(Ctx *ctx, const Q8AttendArgs &a)
 bool attend_q8_umma_covers(const Ctx *ctx, const Q8AttendArgs &a)
 {
     // Rows of a KV head (queries times heads of its group) from which on this form is the faster one; the streaming kernel
-    // reads the cache once per 16 rows.  16 sequences of 4096 tokens, 32 rows per head: fp16 results 92 us there, 65 here, fp32
-    // results 92 and 124; 48 rows per head: fp16 126 and 66, fp32 126 and 126; 64 rows: fp32 158 and 126.
+    // reads the cache once per 16 rows.  16 sequences of 4096 tokens, 32 rows per head: fp16 results 88 us there, 65 here, fp32
+    // results 88 and 124; 48 rows per head: fp16 126 and 66, fp32 126 and 126; 64 rows: fp32 158 and 126.
     const bool dims = (a.c.d_k == 64 || a.c.d_k == 128) && (a.c.d_v == 64 || a.c.d_v == 128);
     return dims && (long long)a.g * a.L_q > (a.out_fp16 ? 16 : 32) && ctx->timeout_flag;
 }
