@@ -181,3 +181,18 @@ def compact(st, page):
     # pages that nobody holds keep refs as they are (0)
     st["free"] = list(range(n - 1, len(live) - 1, -1))
     return remap
+
+
+# ---- how far fp32 attention may be off ----
+def attend_rms_tolerance(reach, d_k, L):
+    """Bound of ||got - out|| / ||out|| for fp32 results over values that do not depend on the scores.
+
+    A relative error e_t of the weights alpha_t changes the result by sum_t alpha_t e_t (v_t - out).  Values of independent
+    signs add up as alpha_t v_t do in out itself, so the norm of that is at most the largest |e_t| of out's norm, twice that
+    with the share in the denominator.  |e_t|: a score is d_k / 16 products of 16 dims that are added one after another,
+    each addition off by at most 2^-23 of sum |q k| <= reach, then a few roundings of the scaled score, its block's exponent
+    (a few units) and its distance to the maximum; the exponential and the weight's two fp16 numbers are good to 2^-22 each.
+    Sums: chains of up to 64 additions in the tensor pipe, which cuts off (2^-23 each), and roundings of independent sign in
+    the fp32 sums over the tokens (2^-24 times the root of their number)."""
+    e = (d_k / 16 + 6) * 2.0 ** -23 * (float(np.max(reach)) + 4) + 2 * 2.0 ** -22
+    return 2 * e + 64 * 2.0 ** -23 + math.sqrt(L) * 2.0 ** -24

@@ -379,11 +379,11 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
                 }
             }
 
-            // weights; amax^V = 2^e f
+            // weights; amax^V = 2^e f.  A block of zeros adds to l alone, and l has fp32's range: its e keeps it from leading M
             const int vb = __float_as_int(meta.y) >> 23;
-            const float e = vb > 0 ? (float)(vb - 127) : 0.f;
+            const float e = vb > 0 ? (float)(vb - 127) : kQ8ZeroExponent;
             const float f = vb > 0 ? __int_as_float((__float_as_int(meta.y) & 0x7fffff) | 0x3f800000) : meta.y;
-            const float inv_e = vb > 0 ? __int_as_float((254 - vb) << 23) : 1.f;
+            const float inv_e = vb > 0 ? __int_as_float((254 - vb) << 23) : kQ8ZeroInverse;
             const int tok = at.step * kAqTile + warp * 16 + g;
             uint32_t ph[NT][2], pl[NT][2];
             bool beyond = false;

@@ -233,8 +233,8 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
                 entry = entry_of(ch + 1);
                 PqMeta m;
                 m.ks = ak * (kQ8Unit<FORMAT> * a.scale_log2);
-                m.le = !there ? -INFINITY : av > 0.f ? log2f(av) : 0.f;            // (amax 0: the numbers are 0, the weights count)
-                m.inv = av > 0.f ? 1.f / av : 1.f;
+                m.le = !there ? -INFINITY : av > 0.f ? log2f(av) : kQ8ZeroExponent;
+                m.inv = av > 0.f ? 1.f / av : kQ8ZeroInverse;
                 m.pad = 0.f;
                 // the slot's last reader was the softmax of chunk ch - 2, over when the value MMAs of that chunk are done (and
                 // those of chunk ch, the barrier's next phase, wait for these scales)

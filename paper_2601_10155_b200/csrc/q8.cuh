@@ -14,6 +14,13 @@ constexpr int kStatusNoPages = 8;           // lookat_pages_extend found too few
 
 constexpr float kQ8RangeInt8 = 127.f, kQ8RangeE4m3 = 448.f;
 
+// The attention's running exponent M follows the largest score + log2 amax^V, so that the fp16 weights serve blocks of any
+// size.  A block of zero values (amax 0) counts in the softmax's denominator l but adds nothing to the sum: with an exponent
+// far below every real one (fp16 amax: -24 to 16) it does not push the other blocks' weights out of fp16's range.  Its weights
+// are lost to l only where they are below 2^-46 of the largest (2^-126 is the least fp32 weight), and l stays below 2^110.
+// With an exponent of 0, one such block among values of 1e-4 made the result 1.5e-4 wrong, among values of 1e-5 1.6e-3.
+constexpr float kQ8ZeroExponent = -64.f, kQ8ZeroInverse = 0x1p64f;
+
 // Where the tokens of the cache are, as the kernels take it.
 struct Q8View {
     uint8_t *k, *v;
