@@ -81,8 +81,10 @@ lookat_status lookat_q8_append(lookat_ctx *ctx, const lookat_q8_cache *cache, co
  *   q          fp16 [B][H_q][L_q][d_k]
  *   tables     int32 [B][max_pages];  seq_lens  int32 [B]
  *   out        [B][H_q][L_q][d_v], fp32, or fp16 with out_fp16 = 1
- * Scores, softmax statistics and sums are fp32; with out_fp16 the softmax weights of prompts (more than 16 queries times
- * heads of a group) are rounded to fp16 before the sum.  Requires 1 <= B <= 65535, 1 <= L_q <= 2^20, H_q * L_q <= 2^30.
+ * Scores, softmax statistics and sums are fp32.  The weights of the sum are two fp16 numbers each: 22 bits for a token
+ * whose weight times its block's amax is at least 2^-13 of the row's largest such product, fewer below, none below 2^-35.
+ * With out_fp16 those of prompts (more than 16 queries times heads of a group) are one fp16 number: 11 bits down to 2^-21.
+ * Requires 1 <= B <= 65535, 1 <= L_q <= 2^20, H_q * L_q <= 2^30.
  * Returns LOOKAT_ERR_TIMEOUT once if an earlier attention kernel of the context gave up a bounded wait (its output is not
  * valid).
  */

@@ -5,8 +5,11 @@
 //     s = (n^K . q) amax^K / R * scale             x = s log2(e)
 //     w = 2^(x + e - M),   amax^V = 2^e f          (f in [1, 2); M follows the largest x + e, lazily)
 //     O += (w f) n^V,   l += w 2^-e,               o = O / (R l)
-// so that one running exponent M serves blocks of any size: w f is at most 2^9 where it matters and is a sum of two fp16
-// numbers (22 bits), the 8-bit numbers are fp16 numbers as they are, and every sum is fp32.
+// so that one running exponent M serves blocks of any size.  The 8-bit numbers are fp16 numbers as they are, and every sum is
+// fp32.  w f is a sum of two fp16 numbers and uses their whole range: M lies kAqLift below the largest x + e, so the
+// largest weight is 2^10 to 2^14, those down to 2^-13 of it have 22 bits, and what is dropped is 2^-35 of it.  (The lift
+// cancels in O / (R l).  Without it, a row of 4096 tokens whose first takes 96 % of the weight and has values near zero was
+// 1.5e-4 off.)
 //
 // It is bound by HBM: (d_k + d_v) bytes per token and KV head against 4 d flops per column, so the products run on
 // mma.sync.m16n8k16 (tokens or value dims are the rows, columns the 8 columns; the tensor pipe is under half used) and the
@@ -44,7 +47,10 @@ constexpr int kAqStages = 3;                    // tiles in a warp's ring
 constexpr int kAqWhole = 10, kAqMinChunk = 3;
 constexpr int kAqJoinCells = 4;
 constexpr int kAqMaxParts = 128;                // pieces that a unit is cut into at most (one CTA joins them)
-constexpr float kAqSlack = 8.f;                 // how far scores may run ahead of M (base-2 units)
+// How far M lies below the largest score (base-2 units), and how far scores may run ahead of that before M moves: f is below
+// 2, so w f stays below 2^(lift + slack + 1) = 2^15.  A smaller slack leaves more bits to small weights and moves M more
+// often: 23 ragged rows with 4 drafts 65.5 us with a slack of 4, 6 or 8, 66.8 with 2; one column: no difference.
+constexpr float kAqLift = 10.f, kAqSlack = 4.f;
 
 __device__ __forceinline__ uint32_t aq_smem(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 template <int BYTES>
@@ -393,9 +399,9 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
                 for (int i = 0; i < 4; ++i) {
                     const float x = fmaf(sc[nt][i] + sd[nt][i], ks, e);
                     sc[nt][i] = tok + 8 * (i >> 1) <= last[nt][i & 1] ? x : -INFINITY;
-                    beyond |= sc[nt][i] > m_ref[nt][i & 1] + kAqSlack;
+                    beyond |= sc[nt][i] > m_ref[nt][i & 1] + (kAqLift + kAqSlack);
                 }
-            if (__any_sync(0xffffffffu, beyond)) {              // M moves (seldom): the largest of the tile, per column
+            if (__any_sync(0xffffffffu, beyond)) {              // M moves (seldom): to the largest of the tile, per column, less the lift
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -404,7 +410,7 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 4));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
                         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
-                        top = fmaxf(top, m_ref[nt][k]);
+                        top = fmaxf(top - kAqLift, m_ref[nt][k]);
                         const float keep = ex2_approx(m_ref[nt][k] - top);
                         m_ref[nt][k] = top;
                         l_sum[nt][k] *= keep;

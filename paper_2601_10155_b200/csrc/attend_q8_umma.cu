@@ -4,7 +4,7 @@
 //     S = Q n^K^T   (fp16 operands, exact)            y = S amax^K / R scale log2(e) + log2(amax^V) - M
 //     w = 2^y       O += w n^V       l += w / amax^V       o = O / (R l)
 // Scale and offset of y belong to a block of tokens (a page), so blocks of any size share one running exponent M per row;
-// M follows the largest score lazily.  A row is one (query, query head) pair of a KV head: row = query * g + head, so a
+// M follows the largest score lazily, kPqLift below it: the weights use fp16's whole range.  A row is one (query, query head) pair of a KV head: row = query * g + head, so a
 // CTA's rows stand at neighbouring positions and share the tokens they see.
 //   fp16 results take the weights in fp16 (2^-12 of each).  fp32 results take them as two fp16 numbers, whose second halves
 // lie in the scores' second half of tensor memory, and move O out of tensor memory every 8 chunks: the tensor pipe cuts
@@ -44,7 +44,16 @@ constexpr int kPqGroups = kPqChunk / 16;        // groups of 16 tokens: a page h
 constexpr int kPqRaw = 3;                       // chunks of 8-bit rows in shared memory
 constexpr int kPqFlush = 8;                     // chunks that O stays in tensor memory for fp32 results
 constexpr int kPqMinPiece = 8;                  // chunks below which a row's tokens are not cut further
-constexpr float kPqSlack = 8.f;
+// How far M lies below the largest score (base-2 units), and how far scores may run ahead of that before M moves: weights
+// stay up to 2^(lift + slack) = 2^15.  With fp32 results the ones down to 2^-14 of the largest have 22 bits and what is dropped
+// is 2^-36 of it; with fp16 results those down to 2^-21 have 11.  (The lift cancels in O / (R l).)  Moving M costs a pass
+// over O in tensor memory: a prompt of 4096 tokens, fp16 results: slack 8 180 us, 6 or 4 183, 2 188 to 200; fp32 results: 321,
+// 325, 326, 330.  The bits are worth that to fp32 results alone: a row of 4096 tokens whose first takes 96 % of the weight and
+// has values near zero is 4e-4 off without a lift, 5e-6 with 7 and 1e-6 with 11.
+template <bool FULL>
+constexpr float kPqSlack = FULL ? 4.f : 8.f;
+template <bool FULL>
+constexpr float kPqLift = 15.f - kPqSlack<FULL>;
 
 struct PqMeta {                                 // of 16 tokens: y = s * ks + le - M, l += w * inv
     float ks, le, inv, pad;
@@ -442,11 +451,11 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
 #pragma unroll
             for (int i = 0; i < kPqChunk / 2; ++i) tops[i & 3] = pq_max3(tops[i & 3], y[i].x, y[i].y);
             const float top = fmaxf(pq_max3(tops[0], tops[1], tops[2]), tops[3]);
-            // M moves only when the scores run ahead of it by more than kPqSlack (base-2 units), or to the first score
-            const bool move = top > kPqSlack || (!set && top > -INFINITY);
+            // M moves only when the scores run ahead by more than kPqSlack, or to the first score
+            const bool move = top > kPqLift<FULL> + kPqSlack<FULL> || (!set && top > -INFINITY);
             float alpha = 1.f;
             if (__any_sync(0xffffffffu, move)) {
-                const float d = move ? top : 0.f;
+                const float d = move ? top - kPqLift<FULL> : 0.f;
                 alpha = set ? ex2_approx(-d) : 1.f;            // (no score so far: O and l are zero)
                 set |= move;
                 m_run += d;

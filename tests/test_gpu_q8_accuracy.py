@@ -92,3 +92,41 @@ def test_a_block_of_zero_values_that_takes_the_weight(Lq):
     q = rng.standard_normal((2, 2, Lq, 64)).astype(np.float16)
     q[..., 0] = 4.0
     check([(k, v), (k[:90], 0 * v[:90])], q, 16, "int8")
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("small", [0.01, 0.0])
+@pytest.mark.parametrize("n,Hq,H,Lq", [(4096, 2, 1, 1), (4096, 8, 1, 1), (4096, 8, 1, 2), (4096, 2, 1, 40), (32768, 4, 1, 1), (32768, 2, 1, 20)])
+def test_a_token_that_takes_most_of_the_weight(fmt, small, n, Hq, H, Lq):
+    """A first token 12 nats above the rest whose own values are small: the result is made of the many small weights."""
+    rng = np.random.default_rng(43)
+    k, v = a_row(rng, n, H, 64)
+    k[:, :, 0] = 0
+    k[0, :, 0] = 24.0                                           # 24 * 4 / 8 = 12
+    k[0, :, 1:] = 0
+    v[0] *= small
+    q = rng.standard_normal((1, Hq, Lq, 64)).astype(np.float16)
+    q[..., 0] = 4.0
+    check([(k, v)], q, 64, fmt)
+
+
+@pytest.mark.parametrize("Lq", [1, 40])
+def test_a_last_token_far_above_the_ones_before(Lq):
+    """The running maximum moves by many powers of two at once, and step by step."""
+    rng = np.random.default_rng(44)
+    k, v = a_row(rng, 1500, 1, 64)
+    k[:, 0, 0] = np.linspace(0, 20, 1500)                       # scores rise by 10 nats over the row
+    k[1400, 0, 0] = 60.0
+    q = rng.standard_normal((1, 2, Lq, 64)).astype(np.float16)
+    q[..., 0] = 4.0
+    got, out, reach = attend([(k, v)], q, 32, "e4m3")
+    assert off(got, out) <= q8.attend_rms_tolerance(reach, 64, 1500)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("lens,Lq,P,Hq,H,d", [([1000], 1, 64, 8, 2, 128), ([3000, 70], 70, 64, 4, 1, 128), ([2500], 300, 16, 2, 2, 64),
+                                              ([9000, 4097, 63], 1, 64, 8, 2, 128), ([5000, 7], 3, 16, 4, 1, 64), ([2000], 1, 32, 16, 1, 128)])
+def test_fp32_results_of_ordinary_rows(fmt, lens, Lq, P, Hq, H, d):
+    rng = np.random.default_rng(45)
+    q = (0.9 * rng.standard_normal((len(lens), Hq, Lq, d))).astype(np.float16)
+    check([a_row(rng, n, H, d) for n in lens], q, P, fmt)
