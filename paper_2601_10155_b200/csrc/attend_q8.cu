@@ -306,9 +306,7 @@ attend_q8_kernel(Q8AttendArgs a, float *__restrict__ parts, unsigned *__restrict
         const size_t to = (((size_t)b * a.H_q + unit / groups * a.g + cc % a.g) * a.L_q + cc / a.g) * d_v + quad * 4;
         x = make_float4(x.x * r, x.y * r, x.z * r, x.w * r);
         if (a.out_fp16) {
-            const __half2 p = __floats2half2_rn(x.x, x.y), q = __floats2half2_rn(x.z, x.w);
-            *reinterpret_cast<uint2 *>(static_cast<__half *>(a.out) + to) =
-                make_uint2(*reinterpret_cast<const uint32_t *>(&p), *reinterpret_cast<const uint32_t *>(&q));
+            *reinterpret_cast<uint2 *>(static_cast<__half *>(a.out) + to) = make_uint2(q8_half2(x.x, x.y), q8_half2(x.z, x.w));
         } else {
             *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + to) = x;
         }

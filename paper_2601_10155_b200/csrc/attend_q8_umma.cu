@@ -388,9 +388,7 @@ attend_q8_umma_kernel(Q8AttendArgs a, int *__restrict__ timeout_flag, int n_supe
                     const unsigned long long at = __shfl_sync(0xffffffffu, (unsigned long long)(halves ? out_at : (size_t)acc), rr);
                     if (!(rows_on >> rr & 1)) continue;
                     if (halves) {
-                        const __half2 u = __floats2half2_rn(x.x, x.y), v = __floats2half2_rn(x.z, x.w);
-                        *reinterpret_cast<uint2 *>(static_cast<__half *>(a.out) + at + p * 32 + quad * 4) =
-                            make_uint2(*reinterpret_cast<const uint32_t *>(&u), *reinterpret_cast<const uint32_t *>(&v));
+                        *reinterpret_cast<uint2 *>(static_cast<__half *>(a.out) + at + p * 32 + quad * 4) = make_uint2(q8_half2(x.x, x.y), q8_half2(x.z, x.w));
                     } else {
                         if (again) x = make_float4(fmaf(y[i].x, k, x.x), fmaf(y[i].y, k, x.y), fmaf(y[i].z, k, x.z), fmaf(y[i].w, k, x.w));
                         *(reinterpret_cast<float4 *>(reinterpret_cast<float *>(at) + p * 32) + quad) = x;
@@ -558,7 +556,7 @@ __global__ void __launch_bounds__(256) attend_q8_join_kernel(Q8AttendArgs a, int
     const size_t at = pq_out_row(a, b, h, row) * DV + lane * kEach;
 #pragma unroll
     for (int i = 0; i < kEach; i += 2) {
-        if (a.out_fp16) *reinterpret_cast<__half2 *>(static_cast<__half *>(a.out) + at + i) = __floats2half2_rn(o[i] * mul, o[i + 1] * mul);
+        if (a.out_fp16) *reinterpret_cast<uint32_t *>(static_cast<__half *>(a.out) + at + i) = q8_half2(o[i] * mul, o[i + 1] * mul);
         else *reinterpret_cast<float2 *>(static_cast<float *>(a.out) + at + i) = make_float2(o[i] * mul, o[i + 1] * mul);
     }
 }

@@ -123,6 +123,14 @@ __device__ __forceinline__ void q8_pairs(uint32_t w, uint32_t &lo, uint32_t &hi)
         asm("{\n.reg .b16 x, y;\nmov.b32 {x, y}, %2;\ncvt.rn.f16x2.e4m3x2 %0, x;\ncvt.rn.f16x2.e4m3x2 %1, y;\n}" : "=r"(lo), "=r"(hi) : "r"(w));
     }
 }
+// Two fp16 results.  A weighted mean of values lies among them, within fp16's range, but the rounded weights of a prompt can
+// put it up to 2^-11 above: what passes 65504 is 65504, not infinity (a NaN stays one).
+__device__ __forceinline__ uint32_t q8_half2(float x, float y)
+{
+    uint32_t d;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %2, %1;" : "=r"(d) : "f"(x), "f"(y));
+    return d;
+}
 template <int FORMAT>
 constexpr float kQ8Unit = 1.f / (FORMAT == LOOKAT_Q8_INT8 ? kQ8RangeInt8 : kQ8RangeE4m3);      // value of a number per amax
 

@@ -130,3 +130,33 @@ def test_fp32_results_of_ordinary_rows(fmt, lens, Lq, P, Hq, H, d):
     rng = np.random.default_rng(45)
     q = (0.9 * rng.standard_normal((len(lens), Hq, Lq, d))).astype(np.float16)
     check([a_row(rng, n, H, d) for n in lens], q, P, fmt)
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("n,width", [(200, 0), (700, 64)])
+@pytest.mark.parametrize("Hq,Lq", [(1, 1), (4, 60)])
+def test_fp16_results_of_the_largest_values_stay_finite(fmt, n, width, Hq, Lq):
+    """Every value is the largest fp16 number, so every mean of them is.  All tokens but the first weigh the same, about
+    half of the first: where that weight is rounded up, the sum is up to 2^-11 above its denominator."""
+    rng = np.random.default_rng(46)
+    sign = np.where(rng.random(64) < 0.5, -1.0, 1.0)
+    k, v = np.zeros((n, 1, 64)), np.tile(65504.0 * sign, (n, 1, 1))
+    k[0, :, 0] = 1.0
+    q = np.zeros((1, Hq, Lq, 64), np.float16)
+    q[..., 0] = rng.uniform(0.85, 1.15, (1, Hq, Lq)) * 8 * np.log(2)
+    got, out, _ = attend([(k, v)], q, 16, fmt, width=width, fp16=True)
+    assert np.isfinite(got).all()
+    # a weight's rounding, then the result's
+    assert (np.abs(got - 65504.0 * sign) <= 65504 * 2.0 ** -10).all()
+
+
+def test_a_query_that_is_not_a_number_reaches_its_own_result_only():
+    rng = np.random.default_rng(47)
+    k, v = a_row(rng, 100, 1, 64)
+    q = rng.standard_normal((1, 2, 40, 64)).astype(np.float16)
+    clean, out, _ = attend([(k, v)], q, 16, "int8", fp16=True)
+    q[0, 1, 7, 3] = np.nan
+    got, _, _ = attend([(k, v)], q, 16, "int8", fp16=True)
+    assert np.isnan(got[0, 1, 7]).all()
+    got[0, 1, 7] = clean[0, 1, 7]
+    assert np.array_equal(got, clean)
