@@ -59,7 +59,7 @@ typedef struct lookat_q8_cache {
  *   k_new, v_new  fp16 [B][H_kv][n][d_k], [B][H_kv][n][d_v]; of row b the first n_new[b] tokens count
  *   tables        int32 [B][max_pages]
  *   seq_lens      int32 [B], lengths that count the new tokens: they go to positions seq_lens[b] - n_new[b] ...
- *   n_new         NULL (n for every row) or int32 [B], 0..n
+ *   n_new         NULL (n for every row) or int32 [B], up to n; negative counts are taken as 0, as lookat_pages_extend does
  * Per block, with x the new tokens in it (NaN taken as 0, infinities as +-65504):
  *   amax' = max(amax if the block holds earlier tokens of the row, else 0; |x|)
  *   new numbers     n = round(R x / amax')        earlier ones, where amax has grown:  n = round(n amax / amax')

@@ -123,8 +123,8 @@ __global__ void __launch_bounds__(THREADS == 32 ? 128 : THREADS, THREADS == 256 
     if (b >= a.B) return;                                       // (whole groups leave)
 
     const int page = 1 << c.page_shift, cap = c.max_pages << c.page_shift;
-    const int len_in = c.seq_lens[b], count_in = a.n_new ? a.n_new[b] : a.n;
-    const int len = min(max(len_in, 0), cap), count = min(max(count_in, 0), a.n);
+    const int len_in = c.seq_lens[b], count_in = a.n_new ? max(a.n_new[b], 0) : a.n;
+    const int len = min(max(len_in, 0), cap), count = min(count_in, a.n);
     const int first = len_in - count;                           // position of the row's token 0 (may be out of range)
     if (lane == 0 && (len_in != len || count_in != count || first < 0)) q8_report(c.status, kStatusBadPage);
     if (count == 0) return;

@@ -23,3 +23,22 @@ def finding(lk):
     return lk.lookat_last_error()
 
 
+def test_a_negative_count_is_zero_in_a_whole_step():
+    """extend takes a negative count as 0 and leaves it as it is; append then takes it the same way, without a finding."""
+    lk = Lookat(2, 2, 64, 64, 1, 16)
+    cache, ps = Q8Cache.empty(6, 2, 16, 64, 64), PageState.empty(3, 2, 6, 16)
+    x = torch.randn(3, 2, 5, 64, device="cuda").half()
+    n_new = i32([5, -1, -2147483648])
+    lk.lookat_pages_extend(ps, n_new, cache.pools())
+    lk.lookat_q8_append(cache, x, x, ps.tables, ps.seq_lens, n_new)
+    lk.lookat_attend_q8(cache, x[:, :, :1].contiguous(), ps.tables, ps.seq_lens)
+    assert finding(lk) == ""
+    assert ps.seq_lens.tolist() == [5, 0, 0] and n_new.tolist() == [5, -1, -2147483648]
+    # a row that holds tokens keeps them, scales among them
+    before = [t.clone() for t in cache.pools()]
+    lk.lookat_q8_append(cache, 9 * x, 9 * x, ps.tables, ps.seq_lens, i32([-3, 0, -1]))
+    assert finding(lk) == "" and all(torch.equal(a, b) for a, b in zip(before, cache.pools()))
+    lk.lookat_q8_append(cache, x, x, ps.tables, ps.seq_lens, i32([6, 0, 0]))             # more than there are: still a finding
+    assert "outside its range" in finding(lk)
+
+
