@@ -287,6 +287,9 @@ class PagePools:
             self.c[i] = lookat_page_pool(_on(t, t.dtype, f"pool {i}", self.device), t.numel() // max(1, t.shape[0]) * t.element_size())
 
 
+_NO_POOLS = PagePools(())
+
+
 class Lookat:
     """A library context for one attention shape on one device and stream.
 
@@ -530,24 +533,22 @@ class Lookat:
     def _pages(self, state, pools):
         if state.device != self.device:
             raise ValueError(f"the page state is on {state.device}, the context on {self.device}")
-        if pools is None:
-            return None
         if not isinstance(pools, PagePools):
-            pools = PagePools(pools)
+            pools = PagePools(() if pools is None else pools)
         if pools.tensors and (pools.n_pages != state.n_pages or pools.device != self.device):
             raise ValueError(f"the pools have {pools.n_pages} pages on {pools.device}, the state {state.n_pages} on {state.device}")
         return pools
 
     def lookat_pages_extend(self, state, n_new, pools):
         """Pages for n_new[b] more tokens per row (n_new all 0 afterwards if there are too few); pools: the tensors kept
-        by pages, or a PagePools of them."""
+        by pages, a PagePools of them, or None."""
         pools = self._pages(state, pools)
         self._check(self._lib.lookat_pages_extend(self._h, state.c, _on(n_new, torch.int32, "n_new", self.device, (state.B,)),
                                                   pools.c, len(pools.tensors)))
 
     def lookat_pages_fork(self, state, parents):
         """Row b continues from row parents[b]; -1 empties it."""
-        self._pages(state, None)
+        self._pages(state, _NO_POOLS)
         self._check(self._lib.lookat_pages_fork(self._h, state.c, _on(parents, torch.int32, "parents", self.device, (state.B,))))
 
     def lookat_pages_compact(self, state, pools, remap=None):

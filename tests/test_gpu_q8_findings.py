@@ -42,3 +42,14 @@ def test_a_negative_count_is_zero_in_a_whole_step():
     assert "outside its range" in finding(lk)
 
 
+def test_page_calls_without_pools():
+    """None stands for no pools, as NULL does in C."""
+    lk = Lookat(2, 2, 64, 64, 1, 16)
+    ps = state([[0, -1], [1, -1]], [5, 16], [1, 1, 0, 0], [2, 3])
+    lk.lookat_pages_extend(ps, i32([1, 1]), None)
+    assert finding(lk) == "" and ps.tables.tolist() == [[0, -1], [1, 3]] and ps.seq_lens.tolist() == [6, 17]
+    remap = i32([9] * 4)
+    lk.lookat_pages_compact(ps, None, remap)
+    assert finding(lk) == "" and remap.tolist() == [0, 1, -1, 2] and ps.tables.tolist() == [[0, -1], [1, 2]]
+
+
