@@ -21,7 +21,8 @@
  * DEVICE-SIDE FINDINGS.  Lengths and tables live on the device, so the host cannot refuse them.  Kernels check each
  * entry before they use it: a length is taken as at least 0 and at most max_pages * page; the tokens of a page outside
  * 0..n_pages-1 are left out (not attended, not stored).  The finding is recorded in the context's status word and
- * lookat_last_error reports it once after the caller has synchronised.  Nothing out of range is read or written.
+ * lookat_last_error reports it once after the caller has synchronised, one kind of finding per call.  Nothing out of range is
+ * read or written.
  *
  * WORKSPACE.  The context's scratch grows on demand; a call that would have to allocate while its stream is being
  * captured returns LOOKAT_ERR_INVALID_ARG (make one call of the same size before the capture).  Scratch that a graph

@@ -331,15 +331,18 @@ const char *lookat_last_error(const lookat_ctx *handle)
 {
     if (!handle) return "context is NULL";
     Ctx *ctx = const_cast<Ctx *>(reinterpret_cast<const Ctx *>(handle));
-    // asynchronous findings of the debug build's device-side checks (meaningful once the caller has synchronised)
+    // asynchronous findings of the device-side checks (meaningful once the caller has synchronised): one per call, so that
+    // none hides another
     if (ctx->status_word && *(volatile int *)ctx->status_word) {
         const int word = *(volatile int *)ctx->status_word;
-        *(volatile int *)ctx->status_word = 0;
-        if (word & kStatusCopyTimeout)
+        const int bit = word & kStatusCopyTimeout ? kStatusCopyTimeout : word & kStatusNoPages ? kStatusNoPages
+                        : word & kStatusBadPage   ? kStatusBadPage     : word;
+        *(volatile int *)ctx->status_word = word & ~bit;
+        if (bit == kStatusCopyTimeout)
             snprintf(ctx->err, sizeof(ctx->err), "attend: a bounded wait for a bulk copy ran out; the output of that call is not valid");
-        else if (word & kStatusNoPages)
+        else if (bit == kStatusNoPages)
             snprintf(ctx->err, sizeof(ctx->err), "pages_extend: too few free pages or table entries; nothing was changed and n_new was set to 0");
-        else if (word & kStatusBadPage)
+        else if (bit == kStatusBadPage)
             snprintf(ctx->err, sizeof(ctx->err), "8-bit cache: a page id, length or count outside its range was met; its tokens were left out");
         else
             snprintf(ctx->err, sizeof(ctx->err),

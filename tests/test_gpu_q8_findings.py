@@ -53,3 +53,13 @@ def test_page_calls_without_pools():
     assert finding(lk) == "" and remap.tolist() == [0, 1, -1, 2] and ps.tables.tolist() == [[0, -1], [1, 2]]
 
 
+def test_two_findings_are_both_reported():
+    lk = Lookat(2, 2, 64, 64, 1, 16)
+    cache, ps = Q8Cache.empty(2, 2, 16, 64, 64), state([[0, -1]], [10], [1, 0], [1])
+    q = torch.zeros(1, 2, 1, 64, dtype=torch.float16, device="cuda")
+    lk.lookat_attend_q8(cache, q, i32([[7, 0]]), ps.seq_lens)
+    lk.lookat_pages_extend(ps, i32([100]), [])
+    first, second = finding(lk), finding(lk)
+    assert "too few free pages" in first and "outside its range" in second
+
+
