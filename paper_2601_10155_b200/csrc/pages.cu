@@ -351,7 +351,8 @@ __global__ void __launch_bounds__(256) pages_compact_move_kernel(const __grid_co
     const int cap = s.max_pages << s.page_shift;
     pdl_wait();
     for (int b = blockIdx.x; b < s.B; b += gridDim.x) {
-        const int n = pg_blocks(min(max(s.seq_lens[b], 0), cap), s.page_shift);
+        const int len_in = s.seq_lens[b], len = min(max(len_in, 0), cap), n = pg_blocks(len, s.page_shift);
+        if (threadIdx.x == 0 && len != len_in) q8_report(s.status, kStatusBadPage);
         int32_t *row = s.tables + (size_t)b * s.max_pages;
         for (int i = threadIdx.x; i < n; i += blockDim.x) {
             const int p = row[i];

@@ -63,3 +63,15 @@ def test_two_findings_are_both_reported():
     assert "too few free pages" in first and "outside its range" in second
 
 
+def test_compact_reports_a_length_out_of_range():
+    lk = Lookat(2, 2, 64, 64, 1, 16)
+    for bad in (-1, 33):
+        ps = state([[0, 1], [2, -1]], [bad, 16], [1, 1, 1, 0], [3])
+        lk.lookat_pages_compact(ps, [])
+        assert "outside its range" in finding(lk)
+        lk = Lookat(2, 2, 64, 64, 1, 16)
+    ps = state([[0, 1], [2, -1]], [32, 0], [1, 1, 0, 0], [2, 3])
+    lk.lookat_pages_compact(ps, [])
+    assert finding(lk) == ""
+
+
