@@ -177,6 +177,7 @@ __global__ void __launch_bounds__(256) pages_extend_apply_kernel(const __grid_co
         for (int k = threadIdx.x & 7; k < t.y; k += 8) {
             const int p = s.free_list[t.x - k];
             if (pg_valid(p, s)) s.refs[p] = 1;
+            else q8_report(s.status, kStatusBadPage);           // (the row's tokens there are left out by whoever reads the table)
             row[k] = p;
         }
         if ((threadIdx.x & 7) == 0 && t.w >= 0) atomicSub(s.refs + t.w, 1);

@@ -75,3 +75,30 @@ def test_compact_reports_a_length_out_of_range():
     assert finding(lk) == ""
 
 
+def test_extend_reports_a_free_list_entry_out_of_range():
+    for entry in (-3, 4, 2 ** 31 - 1):
+        lk = Lookat(2, 2, 64, 64, 1, 16)
+        ps = state([[0, -1], [1, -1]], [16, 16], [1, 1, 0, 0], [entry, 2])
+        lk.lookat_pages_extend(ps, i32([1, 1]), [torch.zeros(4, 4, device="cuda")])
+        assert "outside its range" in finding(lk)
+        assert ps.refs.tolist() == [1, 1, 1, 0] and ps.tables[0].tolist() == [0, 2]
+
+
+def test_lengths_beyond_the_table_are_taken_as_its_end():
+    """Row 0 asks for more tokens than its table holds, row 1 for fewer than none: the first attends its whole table."""
+    rng = np.random.default_rng(13)
+    k, v = (rng.integers(-127, 128, (9, 2, 16, 64)).astype(np.int8) for _ in range(2))
+    ka, va = (rng.uniform(0.5, 2, (9, 2)).astype(np.float32) for _ in range(2))
+    tables = np.array([[3, 0, 8, 5, 2, 7, 1], [4, 6, 4, 4, 4, 4, 4]], np.int32)
+    dev = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    for L_q in (1, 6, 70):
+        lk = Lookat(4, 2, 64, 64, 1, 16)
+        q = rng.standard_normal((2, 4, L_q, 64)).astype(np.float16)
+        got = lk.lookat_attend_q8(Q8Cache(dev(k), dev(ka), dev(v), dev(va)), dev(q), dev(tables), i32([100000, -3]))
+        assert "outside its range" in finding(lk)
+        out, _, reach = q8.attend(k.view(np.uint8), ka, v.view(np.uint8), va, q, tables, [112, 0], "int8", lk.scale)
+        got = got.double().cpu().numpy()
+        assert (got[1] == 0).all()
+        assert np.linalg.norm(got[0] - out[0]) <= q8.attend_rms_tolerance(reach, 64, 112) * np.linalg.norm(out[0])
+
+
