@@ -49,6 +49,9 @@ typedef struct lookat_gpt2_layer {
 lookat_status lookat_gpt2_create(const lookat_gpt2_config *cfg, int device, void *cuda_stream, int32_t B, int32_t capacity,
                                  lookat_gpt2 **out);
 void lookat_gpt2_destroy(lookat_gpt2 *model);
+
+/* Host string describing the last call's error ("" if none); where there is none, or it has been read, the device-side findings of
+ * the model's kernels (lookat_q8.h), which lookat_last_error reports for a context: meaningful once the caller has synchronised. */
 const char *lookat_gpt2_last_error(const lookat_gpt2 *model);
 
 /* wte fp16 [vocab][d] (also the output projection), wpe fp16 [n_pos][d], final LayerNorm gain and bias fp16 [d];

@@ -680,7 +680,11 @@ class LookatGpt2:
 
     def _check(self, st):
         if st != 0:
-            raise LookatError(st, self._lib.lookat_gpt2_last_error(self._h).decode())
+            raise LookatError(st, self.lookat_gpt2_last_error())
+
+    def lookat_gpt2_last_error(self) -> str:
+        """The last call's error, or what the model's kernels have found (after a synchronisation)."""
+        return self._lib.lookat_gpt2_last_error(self._h).decode()
 
     def close(self):
         if self._h is not None:

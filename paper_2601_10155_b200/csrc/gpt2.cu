@@ -20,6 +20,7 @@ struct Gpt2 {
     cudaStream_t stream;
     lookat_ctx *attn;                       // the attention context: H heads of 64 dims, m subspaces, K centroids
     char err[512];
+    bool err_read;                          // lookat_gpt2_last_error has returned err
     // weights (caller-owned device memory)
     const __half *wte, *wpe, *lnf_g, *lnf_b;
     std::vector<lookat_gpt2_layer> layers;
@@ -58,6 +59,7 @@ lookat_status g_fail(Gpt2 *g, lookat_status st, const char *fmt, ...)
     va_start(ap, fmt);
     vsnprintf(g->err, sizeof(g->err), fmt, ap);
     va_end(ap);
+    g->err_read = false;
     return st;
 }
 
@@ -120,6 +122,7 @@ __global__ void fill_ints_kernel(int32_t *p, int n, int value)
         lookat_status st__ = (expr);                                                             \
         if (st__ != LOOKAT_OK) {                                                                 \
             if (!g->err[0]) snprintf(g->err, sizeof(g->err), "%s", lookat_last_error(g->attn)); \
+            g->err_read = false;                                                                 \
             return st__;                                                                         \
         }                                                                                        \
     } while (0)
@@ -253,7 +256,13 @@ void lookat_gpt2_destroy(lookat_gpt2 *handle)
 
 const char *lookat_gpt2_last_error(const lookat_gpt2 *handle)
 {
-    return handle ? reinterpret_cast<const Gpt2 *>(handle)->err : "model is NULL";
+    if (!handle) return "model is NULL";
+    Gpt2 *g = const_cast<Gpt2 *>(reinterpret_cast<const Gpt2 *>(handle));
+    // first what the last call refused, then what the kernels of the attention context found
+    const int *word = ctx_of(g)->status_word;
+    if (word && *(const volatile int *)word && (!g->err[0] || g->err_read)) snprintf(g->err, sizeof(g->err), "%s", lookat_last_error(g->attn));
+    g->err_read = true;
+    return g->err;
 }
 
 uint64_t lookat_gpt2_kernel_launches(const lookat_gpt2 *handle)

@@ -1,0 +1,67 @@
+"""The GPT-2 harness over the 8-bit paged cache when something goes wrong between steps: nothing is lost silently."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2601_10155_b200 import synth
+from paper_2601_10155_b200.binding import LookatError, LookatGpt2, _RawDeviceArray, lookat_page_state, lookat_q8_cache
+
+pytestmark = pytest.mark.gpu
+
+B, T0, VOCAB, PAGE = 3, 32, 300, 16
+IDS = synth.token_ids(52, B, T0 + 8, VOCAB)
+WEIGHTS = synth.gpt2_weights(51, n_layer=2, n_head=2, d_model=128, vocab=VOCAB, n_pos=T0 + 8, plain_init=False)
+
+
+def ids(t):
+    return torch.from_numpy(np.ascontiguousarray(IDS[:, t])).cuda()
+
+
+def model(stream=None):
+    m = LookatGpt2(WEIGHTS, B, T0 + 8, 4, 16, fit_iters=1, stream=stream)
+    m.lookat_gpt2_use_q8_cache(PAGE)
+    return m
+
+
+def prompt(m):
+    m.lookat_gpt2_prefill(torch.from_numpy(np.ascontiguousarray(IDS[:, :T0])).cuda())
+    torch.cuda.synchronize()
+    return m
+
+
+def step(m, t):
+    hidden, _, _ = m.lookat_gpt2_decode(ids(T0 + t), want_hidden=True)
+    torch.cuda.synchronize()
+    return hidden
+
+
+def pages(m):
+    """The model's own page state: tables, seq_lens, refs, free_list, n_free."""
+    c, s = lookat_q8_cache(), lookat_page_state()
+    m._check(m._lib.lookat_gpt2_q8_state(m._h, 0, ctypes.byref(c), ctypes.byref(s)))
+    view = lambda p, *shape: torch.as_tensor(_RawDeviceArray(p, shape, "<i4"), device="cuda")  # noqa: E731
+    return view(s.tables, s.B, s.max_pages), view(s.seq_lens, s.B), view(s.refs, s.n_pages), view(s.free_list, s.n_pages), view(s.n_free, 1)
+
+
+def finding(m):
+    torch.cuda.synchronize()
+    return m.lookat_gpt2_last_error()
+
+
+def test_findings_of_the_models_kernels_are_reported():
+    m = prompt(model())
+    tables = pages(m)[0]
+    assert finding(m) == ""
+    held = int(tables[1, 0])
+    tables[1, 0] = 10000
+    step(m, 0)
+    with pytest.raises(LookatError, match="layer 9"):           # a refused call's own error comes first
+        m.lookat_gpt2_q8_state(9)
+    assert "outside its range" in finding(m)
+    tables[1, 0] = held
+    step(m, 1)
+    assert finding(m) == ""
+
+
