@@ -78,7 +78,8 @@ lookat_status lookat_gpt2_decode(lookat_gpt2 *model, const int32_t *ids, float *
  * (lookat_pages_extend over the pools of all layers), appends and attends (lookat_q8_append, lookat_attend_q8) in every layer.
  *
  * lookat_gpt2_fork: every row continues from row parents[b] (device int32 [B], each in 0..B-1), as a beam search does
- * between steps (lookat_pages_fork; the pages are shared until a row writes to one).
+ * between steps (lookat_pages_fork; the pages are shared until a row writes to one).  A row whose parent is outside 0..B-1
+ * continues from itself, which lookat_gpt2_last_error reports.
  *
  * lookat_gpt2_q8_state: a layer's cache and the page state of the batch (device pointers, for checks); either out pointer
  * may be NULL.  All three return LOOKAT_ERR_INVALID_ARG where the model does not use (or already uses) that cache.

@@ -740,7 +740,7 @@ class LookatGpt2:
         self._check(self._lib.lookat_gpt2_use_q8_cache(self._h, page, 0 if dtype == torch.int8 else 1))
 
     def lookat_gpt2_fork(self, parents):
-        """Row b continues from row parents[b] (int32 [B], each in 0..B-1)."""
+        """Row b continues from row parents[b] (int32 [B], each in 0..B-1; else from itself, with a finding)."""
         self._check(self._lib.lookat_gpt2_fork(self._h, _on(parents, torch.int32, "parents", self.device, (self.B,))))
 
     def lookat_gpt2_q8_state(self, layer):

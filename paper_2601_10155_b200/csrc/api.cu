@@ -343,7 +343,7 @@ const char *lookat_last_error(const lookat_ctx *handle)
         else if (bit == kStatusNoPages)
             snprintf(ctx->err, sizeof(ctx->err), "pages_extend: too few free pages or table entries; nothing was changed and n_new was set to 0");
         else if (bit == kStatusBadPage)
-            snprintf(ctx->err, sizeof(ctx->err), "8-bit cache: a page id, length or count outside its range was met; its tokens were left out");
+            snprintf(ctx->err, sizeof(ctx->err), "8-bit cache: a page id, length, count or parent row outside its range was met and left out");
         else
             snprintf(ctx->err, sizeof(ctx->err),
                      "debug check: a code >= K was found in a code cache and clamped to K - 1; results computed from it are not valid");

@@ -11,6 +11,7 @@
 
 #include "common.cuh"
 #include "lookat_gpt2.h"
+#include "q8.cuh"
 
 namespace lookat {
 
@@ -43,7 +44,7 @@ struct Gpt2 {
     std::vector<lookat_q8_cache> q8_layers;
     std::vector<lookat_page_pool> q8_pools; // k, k_amax, v, v_amax of every layer
     lookat_page_state pages;
-    int32_t *page_ints, *ones, *counts;     // the page state's arrays; 1 per row (a step's tokens); the prompt's tokens per row, or -1
+    int32_t *page_ints, *ones, *counts;     // the page state's arrays; 1 per row (a step's tokens); the prompt's tokens per row, -1, or a fork's parents
     __half *v16, *vd;                       // [B][H][T][64] of the layer being processed (prompt pass), [B][H][64] of a step
     // optional per-category device timing of a decode step (events between the launches of one step)
     bool profile;
@@ -115,6 +116,18 @@ bool q8_allocate(Gpt2 *g, int page, int format, size_t W, size_t n_pages)
 __global__ void fill_ints_kernel(int32_t *p, int n, int value)
 {
     for (int i = threadIdx.x; i < n; i += blockDim.x) p[i] = value;
+}
+
+// a fork's parents; a row whose parent is out of range continues from itself (the model's rows all have one length: none
+// may become empty), and the finding is recorded
+__global__ void checked_parents_kernel(const int32_t *parents, int32_t *out, int B, int *status)
+{
+    for (int b = threadIdx.x; b < B; b += blockDim.x) {
+        const int p = parents[b];
+        const bool ok = p >= 0 && p < B;
+        out[b] = ok ? p : b;
+        if (!ok) q8_report(status, kStatusBadPage);
+    }
 }
 
 #define G_TRY(expr)                                                                              \
@@ -458,7 +471,15 @@ lookat_status lookat_gpt2_fork(lookat_gpt2 *handle, const int32_t *parents)
     Gpt2 *g = reinterpret_cast<Gpt2 *>(handle);
     g->err[0] = 0;
     if (!g->q8) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "fork: the model does not use the 8-bit paged cache");
-    G_TRY(lookat_pages_fork(g->attn, &g->pages, parents));
+    if (!parents || (reinterpret_cast<uintptr_t>(parents) & 3)) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "fork: parents is NULL or not 4-byte aligned");
+    Ctx *ctx = ctx_of(g);
+    int prev = -1;
+    cudaGetDevice(&prev);
+    cudaSetDevice(g->device);
+    struct Restore { int d; ~Restore() { if (d >= 0) cudaSetDevice(d); } } restore{prev};
+    checked_parents_kernel<<<1, 32, 0, g->stream>>>(parents, g->counts, g->B, ctx->status_word);
+    G_TRY(check_launch(ctx, "checked_parents_kernel"));
+    G_TRY(lookat_pages_fork(g->attn, &g->pages, g->counts));
     return LOOKAT_OK;
 }
 

@@ -65,3 +65,18 @@ def test_findings_of_the_models_kernels_are_reported():
     assert finding(m) == ""
 
 
+@pytest.mark.parametrize("bad", [-1, 3, 2 ** 31 - 1, -2 ** 31])
+def test_a_parent_out_of_range_leaves_the_row_as_it_is(bad):
+    """The harness's rows all have one length: a row cannot become empty between steps."""
+    m, want = prompt(model()), prompt(model())
+    step(m, 0), step(want, 0)
+    parents = torch.tensor([2, bad, 2], dtype=torch.int32, device="cuda")
+    m.lookat_gpt2_fork(parents)
+    want.lookat_gpt2_fork(torch.tensor([2, 1, 2], dtype=torch.int32, device="cuda"))
+    assert "outside its range" in finding(m) and finding(want) == ""
+    assert parents.tolist() == [2, bad, 2]
+    assert pages(m)[1].tolist() == [T0 + 1] * B
+    for t in (1, 2):
+        assert torch.equal(step(m, t), step(want, t))
+
+
