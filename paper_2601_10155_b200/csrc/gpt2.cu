@@ -44,7 +44,7 @@ struct Gpt2 {
     std::vector<lookat_q8_cache> q8_layers;
     std::vector<lookat_page_pool> q8_pools; // k, k_amax, v, v_amax of every layer
     lookat_page_state pages;
-    int32_t *page_ints, *ones, *counts;     // the page state's arrays; 1 per row (a step's tokens); the prompt's tokens per row, -1, or a fork's parents
+    int32_t *page_ints, *counts;            // the page state's arrays; per row a step's or the prompt's tokens, or a fork's parents
     __half *v16, *vd;                       // [B][H][T][64] of the layer being processed (prompt pass), [B][H][64] of a step
     // optional per-category device timing of a decode step (events between the launches of one step)
     bool profile;
@@ -82,18 +82,17 @@ bool q8_allocate(Gpt2 *g, int page, int format, size_t W, size_t n_pages)
 {
     const lookat_gpt2_config &c = g->cfg;
     const size_t B = g->B, d = c.d_model, H = c.n_head;
-    // [tables | seq_lens | refs | free_list | n_free | ones | counts], parts of a multiple of 4 ints
-    const size_t row_ints = (B + 3) / 4 * 4, page_ints = (n_pages + 3) / 4 * 4, total = 3 * page_ints + 3 * row_ints + 4;
+    // [tables | seq_lens | refs | free_list | n_free | counts], parts of a multiple of 4 ints
+    const size_t row_ints = (B + 3) / 4 * 4, page_ints = (n_pages + 3) / 4 * 4, total = 3 * page_ints + 2 * row_ints + 4;
     std::vector<int32_t> ints(total, 0);
     g->q8_pools.reserve(4 * (size_t)c.n_layer);
     g->q8_layers.reserve(c.n_layer);
-    const size_t at_refs = page_ints + row_ints, at_free = at_refs + page_ints, at_n_free = at_free + page_ints, at_ones = at_n_free + 4;
+    const size_t at_refs = page_ints + row_ints, at_free = at_refs + page_ints, at_n_free = at_free + page_ints;
     for (size_t i = 0; i < n_pages; ++i) {
         ints[i] = -1;
         ints[at_free + i] = (int32_t)(n_pages - 1 - i);
     }
     ints[at_n_free] = (int32_t)n_pages;
-    for (size_t i = 0; i < B; ++i) ints[at_ones + i] = 1;
     if (!dev_alloc(&g->page_ints, total) || !dev_alloc(&g->v16, B * g->capacity * d) || !dev_alloc(&g->vd, B * d)) return false;
     for (int l = 0; l < c.n_layer; ++l) {
         const size_t bytes[4] = {d * page, H * sizeof(float), d * page, H * sizeof(float)};
@@ -107,8 +106,7 @@ bool q8_allocate(Gpt2 *g, int page, int format, size_t W, size_t n_pages)
     }
     int32_t *const q = g->page_ints;
     g->pages = {q, q + page_ints, q + at_refs, q + at_free, q + at_n_free, (int32_t)B, (int32_t)W, (int32_t)n_pages, page};
-    g->ones = q + at_ones;
-    g->counts = g->ones + row_ints;
+    g->counts = q + at_n_free + 4;
     return cudaMemcpyAsync(q, ints.data(), total * sizeof(int32_t), cudaMemcpyHostToDevice, g->stream) == cudaSuccess &&
            cudaStreamSynchronize(g->stream) == cudaSuccess;
 }
@@ -348,7 +346,7 @@ lookat_status lookat_gpt2_prefill(lookat_gpt2 *handle, const int32_t *ids, int32
         G_TRY(launch_linear(ctx, g->att16, 0, (const __half *)w.w_o, plain((const __half *)w.b_o, rows, d, d, 0, g->x, g->x, 0)));
         G_TRY(mlp(g, w, rows));
         if (g->q8) {
-            G_TRY(lookat_q8_append(g->attn, &g->q8_layers[l], g->k16, g->v16, B, T, g->pages.tables, g->pages.max_pages, g->pages.seq_lens, nullptr));
+            G_TRY(lookat_q8_append(g->attn, &g->q8_layers[l], g->k16, g->v16, B, T, g->pages.tables, g->pages.max_pages, g->pages.seq_lens, g->counts));
         } else {
             // Section 3.4: codebooks from the prompt's keys of every head, then the prompt's codes
             G_TRY(lookat_fit_codebooks(g->attn, g->k16, B, T, c.fit_iters, seed + (uint64_t)l, nullptr, g->books[l], nullptr));
@@ -384,7 +382,10 @@ lookat_status lookat_gpt2_decode(lookat_gpt2 *handle, const int32_t *ids, float 
     G_TRY(launch_embed(ctx, ids, g->wte, g->wpe, g->x, B, 1, pos, d, c.vocab));
     mark(g, LOOKAT_GPT2_CAT_EMBED);
     if (g->q8) {
-        G_TRY(lookat_pages_extend(g->attn, &g->pages, g->ones, g->q8_pools.data(), (int32_t)g->q8_pools.size()));
+        // (a refused extension leaves 0 in counts: nothing is appended then, and the next step asks anew)
+        fill_ints_kernel<<<1, 32, 0, g->stream>>>(g->counts, B, 1);
+        G_TRY(check_launch(ctx, "fill_ints_kernel"));
+        G_TRY(lookat_pages_extend(g->attn, &g->pages, g->counts, g->q8_pools.data(), (int32_t)g->q8_pools.size()));
         mark(g, LOOKAT_GPT2_CAT_ATTENTION);
     }
     for (int l = 0; l < c.n_layer; ++l) {
@@ -403,7 +404,7 @@ lookat_status lookat_gpt2_decode(lookat_gpt2 *handle, const int32_t *ids, float 
         mark(g, LOOKAT_GPT2_CAT_QKV);
         if (g->q8) {
             const lookat_page_state &ps = g->pages;
-            G_TRY(lookat_q8_append(g->attn, &g->q8_layers[l], g->kd, g->vd, B, 1, ps.tables, ps.max_pages, ps.seq_lens, nullptr));
+            G_TRY(lookat_q8_append(g->attn, &g->q8_layers[l], g->kd, g->vd, B, 1, ps.tables, ps.max_pages, ps.seq_lens, g->counts));
             G_TRY(lookat_attend_q8(g->attn, &g->q8_layers[l], g->qd, B, 1, ps.tables, ps.max_pages, ps.seq_lens, g->attn_out, 0));
         } else {
             // append (Section 3.4 "Encoding") and Algorithm 1 over tokens 0..pos, one launch

@@ -80,3 +80,26 @@ def test_a_parent_out_of_range_leaves_the_row_as_it_is(bad):
         assert torch.equal(step(m, t), step(want, t))
 
 
+def test_a_refused_step_does_not_make_later_ones_write_over_the_newest_token():
+    """The free list runs out at a page border: the step is refused on the device and reported, nothing is written, and the
+    steps after the pages are back take room again."""
+    m = prompt(model())                                         # 32 tokens: the next one needs a page
+    tables, seq_lens, refs, free_list, n_free = pages(m)
+    before = [t.clone() for t in m.lookat_gpt2_q8_state(1)]
+    free = int(n_free)
+    n_free.zero_()
+    step(m, 0)
+    assert "too few free pages" in finding(m)
+    n_free.fill_(free)
+    for a, b in zip(before, m.lookat_gpt2_q8_state(1)):
+        assert torch.equal(a, b)
+    for t in (1, 2):
+        step(m, t)
+        assert finding(m) == "" and seq_lens.tolist() == [T0 + t] * B
+    after = m.lookat_gpt2_q8_state(1)
+    for b in range(B):                                          # the prompt's tokens are as they were
+        for i in range(T0 // PAGE):
+            for x, y in ((before[0], after[0]), (before[2], after[2])):
+                assert torch.equal(x[before[4][b, i]], y[after[4][b, i]])
+
+
