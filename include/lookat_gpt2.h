@@ -81,6 +81,9 @@ lookat_status lookat_gpt2_decode(lookat_gpt2 *model, const int32_t *ids, float *
  * between steps (lookat_pages_fork; the pages are shared until a row writes to one).  A row whose parent is outside 0..B-1
  * continues from itself, which lookat_gpt2_last_error reports.
  *
+ * A prompt or a step that returns an error after it has taken its pages leaves rows that are longer than what they hold: the
+ * model then refuses steps and forks until the next prompt.
+ *
  * lookat_gpt2_q8_state: a layer's cache and the page state of the batch (device pointers, for checks); either out pointer
  * may be NULL.  All three return LOOKAT_ERR_INVALID_ARG where the model does not use (or already uses) that cache.
  */

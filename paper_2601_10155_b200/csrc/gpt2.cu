@@ -41,6 +41,7 @@ struct Gpt2 {
     int pos;                                // tokens in the cache
     // the 8-bit paged cache in place of codes and values (lookat_gpt2_use_q8_cache)
     bool q8;
+    bool torn;                              // a prompt or a step ended with an error after it had changed the rows' lengths
     std::vector<lookat_q8_cache> q8_layers;
     std::vector<lookat_page_pool> q8_pools; // k, k_amax, v, v_amax of every layer
     lookat_page_state pages;
@@ -322,6 +323,7 @@ lookat_status lookat_gpt2_prefill(lookat_gpt2 *handle, const int32_t *ids, int32
     const long long rows = (long long)B * T;
     G_TRY(launch_embed(ctx, ids, g->wte, g->wpe, g->x, rows, T, 0, d, c.vocab));
     if (g->q8) {                                             // whatever the rows held is freed, then room for the prompt
+        g->torn = true;                                      // until the prompt is in
         for (int value : {-1, (int)T}) {
             fill_ints_kernel<<<1, 32, 0, g->stream>>>(g->counts, B, value);
             G_TRY(check_launch(ctx, "fill_ints_kernel"));
@@ -360,6 +362,7 @@ lookat_status lookat_gpt2_prefill(lookat_gpt2 *handle, const int32_t *ids, int32
         cudaMemcpyAsync(hidden_out, g->x, (size_t)rows * d * sizeof(float), cudaMemcpyDeviceToDevice, g->stream) != cudaSuccess)
         return g_fail(g, LOOKAT_ERR_CUDA, "copy of the hidden states failed");
     g->pos = T;
+    g->torn = false;
     return LOOKAT_OK;
 }
 
@@ -369,6 +372,7 @@ lookat_status lookat_gpt2_decode(lookat_gpt2 *handle, const int32_t *ids, float 
     Gpt2 *g = reinterpret_cast<Gpt2 *>(handle);
     g->err[0] = 0;
     if (!g->have_weights || g->pos < 1) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "run the prompt first");
+    if (g->torn) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "an earlier call failed half way: run the prompt again");
     if (!ids) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "ids is NULL");
     if (g->pos >= g->capacity) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "the cache is full (%d tokens)", g->capacity);
     Ctx *ctx = ctx_of(g);
@@ -382,6 +386,7 @@ lookat_status lookat_gpt2_decode(lookat_gpt2 *handle, const int32_t *ids, float 
     G_TRY(launch_embed(ctx, ids, g->wte, g->wpe, g->x, B, 1, pos, d, c.vocab));
     mark(g, LOOKAT_GPT2_CAT_EMBED);
     if (g->q8) {
+        g->torn = true;                                      // until the step is done
         // (a refused extension leaves 0 in counts: nothing is appended then, and the next step asks anew)
         fill_ints_kernel<<<1, 32, 0, g->stream>>>(g->counts, B, 1);
         G_TRY(check_launch(ctx, "fill_ints_kernel"));
@@ -425,6 +430,7 @@ lookat_status lookat_gpt2_decode(lookat_gpt2 *handle, const int32_t *ids, float 
         mark(g, LOOKAT_GPT2_CAT_LM_HEAD);
     }
     g->pos = pos + 1;
+    g->torn = false;
     return LOOKAT_OK;
 }
 
@@ -472,6 +478,7 @@ lookat_status lookat_gpt2_fork(lookat_gpt2 *handle, const int32_t *parents)
     Gpt2 *g = reinterpret_cast<Gpt2 *>(handle);
     g->err[0] = 0;
     if (!g->q8) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "fork: the model does not use the 8-bit paged cache");
+    if (g->torn) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "fork: an earlier call failed half way: run the prompt again");
     if (!parents || (reinterpret_cast<uintptr_t>(parents) & 3)) return g_fail(g, LOOKAT_ERR_INVALID_ARG, "fork: parents is NULL or not 4-byte aligned");
     Ctx *ctx = ctx_of(g);
     int prev = -1;

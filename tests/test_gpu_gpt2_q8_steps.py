@@ -103,3 +103,45 @@ def test_a_refused_step_does_not_make_later_ones_write_over_the_newest_token():
                 assert torch.equal(x[before[4][b, i]], y[after[4][b, i]])
 
 
+def attention_of(m):
+    """The model's attention context (its address follows the configuration, three ints and the stream)."""
+    at = ctypes.sizeof(m.cfg)
+    at = (at + 12 + 7) // 8 * 8 + 8
+    h = ctypes.c_void_p.from_address(m._h.value + at)
+    assert m._lib.lookat_kernel_launches(h) == m.lookat_gpt2_kernel_launches() > 0
+    return h
+
+
+def test_a_step_that_failed_half_way_is_not_repeated_on_top_of_itself():
+    """A time-out is found after the step has taken its pages (a self-test kernel's wait that nothing ends): the model then
+    refuses steps and forks until the next prompt, and is as good as new after it."""
+    m, want = prompt(model()), prompt(model())
+    step(m, 0)
+    m._lib.lookat_selftest_timeout(attention_of(m))
+    torch.cuda.synchronize()
+    with pytest.raises(LookatError, match="gave up"):
+        step(m, 1)
+    for _ in range(2):
+        with pytest.raises(LookatError, match="prompt"):
+            step(m, 1)
+    with pytest.raises(LookatError, match="prompt"):
+        m.lookat_gpt2_fork(torch.zeros(B, dtype=torch.int32, device="cuda"))
+    prompt(m)
+    for t in range(3):
+        assert torch.equal(step(m, t), step(want, t))
+
+
+def test_a_prompt_that_failed_half_way_leaves_nothing_to_continue():
+    m, want = prompt(model()), prompt(model())
+    step(m, 0)
+    m._lib.lookat_selftest_timeout(attention_of(m))
+    torch.cuda.synchronize()
+    with pytest.raises(LookatError, match="gave up"):
+        prompt(m)
+    with pytest.raises(LookatError, match="prompt"):
+        step(m, 1)
+    prompt(m)
+    for t in range(3):
+        assert torch.equal(step(m, t), step(want, t))
+
+
