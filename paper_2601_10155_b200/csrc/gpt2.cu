@@ -129,6 +129,16 @@ __global__ void checked_parents_kernel(const int32_t *parents, int32_t *out, int
     }
 }
 
+// The attention context's workspaces, by one call of each kind over the empty rows: no later step or fork has to allocate, so
+// each can be captured and none fails for want of memory after it has taken its pages.
+bool q8_reserve(Gpt2 *g)
+{
+    const lookat_page_state &ps = g->pages;
+    return lookat_pages_fork(g->attn, &ps, g->counts) == LOOKAT_OK &&
+           lookat_pages_extend(g->attn, &ps, g->counts, g->q8_pools.data(), (int32_t)g->q8_pools.size()) == LOOKAT_OK &&
+           lookat_attend_q8(g->attn, &g->q8_layers[0], g->qd, g->B, 1, ps.tables, ps.max_pages, ps.seq_lens, g->attn_out, 0) == LOOKAT_OK;
+}
+
 #define G_TRY(expr)                                                                              \
     do {                                                                                         \
         lookat_status st__ = (expr);                                                             \
@@ -452,7 +462,7 @@ lookat_status lookat_gpt2_use_q8_cache(lookat_gpt2 *handle, int32_t page, int32_
     struct Restore { int d; ~Restore() { if (d >= 0) cudaSetDevice(d); } } restore{prev};
     bool ok = false;
     try {
-        ok = q8_allocate(g, page, format, W, n_pages);
+        ok = q8_allocate(g, page, format, W, n_pages) && q8_reserve(g);
     } catch (const std::bad_alloc &) {                       // (no exception leaves a C entry point)
     }
     if (ok) {

@@ -145,3 +145,20 @@ def test_a_prompt_that_failed_half_way_leaves_nothing_to_continue():
         assert torch.equal(step(m, t), step(want, t))
 
 
+def test_the_first_step_can_be_captured():
+    """The workspaces are made with the cache, so no step and no fork has to allocate."""
+    want = prompt(model())
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        m = prompt(model(stream=s))
+        x, hidden, parents = ids(T0), torch.zeros(B, 128, device="cuda"), torch.arange(B, dtype=torch.int32, device="cuda")
+        s.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            got, _, _ = m.lookat_gpt2_decode(x, want_hidden=True)
+            hidden.copy_(got)
+            m.lookat_gpt2_fork(parents)
+        g.replay()
+        s.synchronize()
+        assert finding(m) == "" and torch.equal(hidden, step(want, 0))
+        del g
