@@ -223,11 +223,13 @@ _contexts = {}
 
 
 def _context(n_q, n_kv, d):
-    """The framework's context for an attention shape, made once as a user's program does."""
-    if (n_q, n_kv, d) not in _contexts:
+    """The framework's context for an attention shape on the current device and stream, made once as a user's program does."""
+    device = torch.cuda.current_device()
+    key = n_q, n_kv, d, device, torch._C._cuda_getCurrentRawStream(device)
+    if key not in _contexts:
         from paper_2601_10155_b200.binding import Lookat
-        _contexts[n_q, n_kv, d] = Lookat(n_q, n_kv, d, d, 4, 256)
-    return _contexts[n_q, n_kv, d]
+        _contexts[key] = Lookat(n_q, n_kv, d, d, 4, 256, device=device)
+    return _contexts[key]
 
 
 def run(state):
