@@ -73,9 +73,10 @@ lookat_status lookat_gpt2_decode(lookat_gpt2 *model, const int32_t *ids, float *
 /*
  * The same model over the 8-bit paged cache (lookat_q8.h) instead of codes and fp16 values: the paper's scalar-quantised
  * comparison, in a form that beams can share.  lookat_gpt2_use_q8_cache is called once, before the first prompt; it
- * allocates B * ceil(capacity / page) pages per layer, which suffice however the rows share them.  From then on
- * lookat_gpt2_prefill quantises the prompt's keys and values (no codebooks are fitted) and lookat_gpt2_decode makes room
- * (lookat_pages_extend over the pools of all layers), appends and attends (lookat_q8_append, lookat_attend_q8) in every layer.
+ * allocates B * ceil(capacity / page) pages per layer, which suffice however the rows share them, and frees the codebooks,
+ * codes and values.  From then on lookat_gpt2_prefill quantises the prompt's keys and values (no codebooks are fitted) and
+ * lookat_gpt2_decode makes room (lookat_pages_extend over the pools of all layers), appends and attends (lookat_q8_append,
+ * lookat_attend_q8) in every layer.
  *
  * lookat_gpt2_fork: every row continues from row parents[b] (device int32 [B], each in 0..B-1), as a beam search does
  * between steps (lookat_pages_fork; the pages are shared until a row writes to one).  A row whose parent is outside 0..B-1
@@ -93,7 +94,7 @@ lookat_status lookat_gpt2_q8_state(lookat_gpt2 *model, int32_t layer, lookat_q8_
 
 /* Device pointers to a layer's state (for checks): codebooks fp32 [H][m][K][64/m], codes uint8 [B][H][capacity][m],
  * values fp16 [B][H][capacity][64], prompt_keys fp16 [B][H][T][64] (NULL unless kept).  Any out pointer may be NULL.  With
- * the 8-bit cache the first three are not written. */
+ * the 8-bit cache the first three are NULL. */
 lookat_status lookat_gpt2_layer_state(lookat_gpt2 *model, int32_t layer, const float **codebooks, const uint8_t **codes,
                                       const void **values, const void **prompt_keys);
 

@@ -467,6 +467,14 @@ lookat_status lookat_gpt2_use_q8_cache(lookat_gpt2 *handle, int32_t page, int32_
     }
     if (ok) {
         g->q8 = true;
+        // what this cache takes the place of (cudaFree waits for the work that uses it)
+        for (int l = 0; l < c.n_layer; ++l) {
+            void *gone[] = {g->books[l], g->codes[l], g->values[l]};
+            for (void *p : gone) cudaFree(p);
+            g->books[l] = nullptr;
+            g->codes[l] = nullptr;
+            g->values[l] = nullptr;
+        }
         return LOOKAT_OK;
     }
     cudaGetLastError();

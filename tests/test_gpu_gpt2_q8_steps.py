@@ -162,3 +162,21 @@ def test_the_first_step_can_be_captured():
         s.synchronize()
         assert finding(m) == "" and torch.equal(hidden, step(want, 0))
         del g
+
+
+def test_the_cache_replaces_codes_and_values():
+    """Codebooks, codes and fp16 values are given back: the 8-bit cache takes less than they did."""
+    cap = 1024
+    w = synth.gpt2_weights(53, n_layer=4, n_head=8, d_model=512, vocab=50, n_pos=cap)
+    torch.cuda.synchronize()
+    m = LookatGpt2(w, 16, cap, 4, 16, fit_iters=1)
+    torch.cuda.synchronize()
+    before = torch.cuda.mem_get_info()[0]
+    m.lookat_gpt2_use_q8_cache(PAGE)
+    torch.cuda.synchronize()
+    # per layer: 16.8 MB of values and 2 MB of codes go, 16.8 MB of pages come; 16.8 MB of values for a prompt, once
+    assert before - torch.cuda.mem_get_info()[0] < 20 << 20
+    assert m.lookat_gpt2_layer_state(0)[:3] == (None, None, None)
+    m.lookat_gpt2_prefill(torch.zeros(16, 40, dtype=torch.int32, device="cuda"))
+    m.lookat_gpt2_decode(torch.zeros(16, dtype=torch.int32, device="cuda"))
+    assert finding(m) == ""
