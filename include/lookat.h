@@ -63,9 +63,9 @@ void lookat_destroy(lookat_ctx *ctx);
 /* Host string describing the last error this context returned ("" if none).  In the debug build of the library
  * (compiled with -DLOOKAT_DEBUG, liblookat_debug.so) the attend kernels check every code they read from a cache:
  * a code >= K is clamped to K - 1 before it is used as an index and the finding is recorded in a status word of the
- * context; after the caller has synchronised the stream, this call reports it once.  The normal build does not
- * check: a code >= K there is the caller's error (the streaming kernels then read garbage inside their tables, the
- * any-shape kernel reads past the table). */
+ * context; after the caller has synchronised the stream, this call reports it once (after the error of a refused call that
+ * it has not returned yet).  The normal build does not check: a code >= K there is the caller's error (the streaming
+ * kernels then read garbage inside their tables, the any-shape kernel reads past the table). */
 const char *lookat_last_error(const lookat_ctx *ctx);
 
 /* 1 in the debug build of the library, 0 otherwise. */

@@ -18,6 +18,7 @@ lookat_status set_error(Ctx *ctx, lookat_status st, const char *fmt, ...)
         va_start(ap, fmt);
         vsnprintf(ctx->err, sizeof(ctx->err), fmt, ap);
         va_end(ap);
+        ctx->err_read = 0;
     }
     return st;
 }
@@ -331,9 +332,9 @@ const char *lookat_last_error(const lookat_ctx *handle)
 {
     if (!handle) return "context is NULL";
     Ctx *ctx = const_cast<Ctx *>(reinterpret_cast<const Ctx *>(handle));
-    // asynchronous findings of the device-side checks (meaningful once the caller has synchronised): one per call, so that
-    // none hides another
-    if (ctx->status_word && *(volatile int *)ctx->status_word) {
+    // asynchronous findings of the device-side checks (meaningful once the caller has synchronised): one per call and after
+    // the error of a refused call, so that none hides another
+    if (ctx->status_word && *(volatile int *)ctx->status_word && (!ctx->err[0] || ctx->err_read)) {
         const int word = *(volatile int *)ctx->status_word;
         const int bit = word & kStatusCopyTimeout ? kStatusCopyTimeout : word & kStatusNoPages ? kStatusNoPages
                         : word & kStatusBadPage   ? kStatusBadPage     : word;
@@ -348,6 +349,7 @@ const char *lookat_last_error(const lookat_ctx *handle)
             snprintf(ctx->err, sizeof(ctx->err),
                      "debug check: a code >= K was found in a code cache and clamped to K - 1; results computed from it are not valid");
     }
+    ctx->err_read = 1;
     return ctx->err;
 }
 

@@ -31,6 +31,7 @@ struct Ctx {
     int *status_word;          // pinned, device-visible: LOOKAT_STATUS_* bits set by the debug build's checks
     float scale;           // resolved softmax scale
     char err[512];
+    int err_read;          // lookat_last_error has returned err
     uint64_t launches;
 
     // attend scratch: chunk partials  o [B][H_q][splits][d_v], (M, l) [B][H_q][splits][2]

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from oracle import q8
-from paper_2601_10155_b200.binding import Lookat, PageState, Q8Cache
+from paper_2601_10155_b200.binding import Lookat, LookatError, PageState, Q8Cache
 
 pytestmark = pytest.mark.gpu
 
@@ -102,3 +102,14 @@ def test_lengths_beyond_the_table_are_taken_as_its_end():
         assert np.linalg.norm(got[0] - out[0]) <= q8.attend_rms_tolerance(reach, 64, 112) * np.linalg.norm(out[0])
 
 
+def test_a_refused_call_is_not_explained_by_an_earlier_finding():
+    lk = Lookat(2, 2, 64, 64, 1, 16)
+    cache, lens = Q8Cache.empty(2, 2, 16, 64, 64), i32([10])
+    q = torch.zeros(1, 2, 1, 64, dtype=torch.float16, device="cuda")
+    lk.lookat_attend_q8(cache, q, i32([[7, 0]]), lens)
+    torch.cuda.synchronize()
+    with pytest.raises(LookatError, match="L_q=0"):
+        lk.lookat_attend_q8(cache, q[:, :, :0].contiguous(), i32([[0, 0]]), lens)
+    assert "outside its range" in finding(lk)
+    with pytest.raises(LookatError, match="L_q=0"):
+        lk.lookat_attend_q8(cache, q[:, :, :0].contiguous(), i32([[0, 0]]), lens)
