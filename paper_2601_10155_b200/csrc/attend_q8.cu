@@ -13,9 +13,10 @@
 //
 // It is bound by HBM: (d_k + d_v) bytes per token and KV head against 4 d flops per column, so the products run on
 // mma.sync.m16n8k16 (tokens or value dims are the rows, columns the 8 columns; the tensor pipe is under half used) and the
-// design serves the loads.  Every lane copies by cp.async exactly the bytes that its own fragments are made of, into
-// slots of its own: no barrier, no bank conflict and no shuffle between the copy and the product, and the ring
-// (kAqStages tiles per warp) holds the bytes in flight without registers.
+// design serves the loads.  Every warp has a ring of its own (kAqStages tiles), which holds the bytes in flight without
+// registers: its lanes copy linearly by cp.async into a permuted order (aq_piece), so that the reads of the fragments meet no
+// bank conflict and need no shuffle.  A lane reads pieces that other lanes of its warp copied: every lane waits for its own
+// copies (wait_group) and the __syncwarp behind that makes them visible to the others; no barrier of the CTA is needed.
 //   Scores: rows = 16 tokens, k = dims.  Lane (g, t) supplies rows g, g + 8; which dims stand behind its k indices is free
 //     as long as q agrees: it takes the 16-byte pieces t, t + 4, .. of a token row, a product step per 4 bytes.
 //   Values: rows = dims, k = 16 tokens.  Lane (g, t) supplies tokens 2t, 2t+1, 2t+8, 2t+9 and, with the dims permuted the
@@ -24,7 +25,7 @@
 // Measured (B200): 16 rows of 32768 int8 tokens, 8 KV heads of 4 query heads, 128 + 128 dims, 1.07 GB of cache: 190 us =
 // 5.65 TB/s, 88 % of a large copy's rate (a kernel of the copies alone: 180 us); 226-234 us in a long run under the power
 // cap, where the 512 warp instructions per 16 tokens (issue slots 59 % full) bound it.  One row of GPT-2's 12 heads over
-// 128 tokens: 5.2 us.
+// 128 tokens: 5.4 us.
 // Work: rows, units and 64-token tiles form one flat sequence, cut evenly among the resident CTAs on the device (the host
 // does not know the lengths).  A unit cut between CTAs is joined by the CTA that finishes it last, in the order of the
 // pieces, so the result does not depend on timing.
@@ -37,9 +38,10 @@ namespace {
 constexpr int kAqWarps = 4, kAqThreads = kAqWarps * 32;
 constexpr int kAqTile = 16 * kAqWarps;          // tokens of a CTA's step
 constexpr int kAqStages = 3;                    // tiles in a warp's ring
-// Cutting a unit costs about 5 us (pieces through global memory, a counter, the join), a step of a lone CTA 0.7 us: units of
-// up to kAqWhole steps stay whole (rows of 200 to 900 tokens, 8 KV heads: 16.3 us, 24.1 with units of up to 16 steps whole;
-// rows of 500 tokens, 16 columns: 19 us whole, 23 cut), a CTA's part has at least kAqMinChunk steps and a cell (one row of
+// Cutting a unit costs about 5 us (pieces through global memory, a counter, the join), a step of a lone CTA 0.7 us: where no unit
+// has more than kAqWhole steps, a CTA's part is at least the longest unit, so that units of one length stay whole and others
+// are cut once at most (rows of 200 to 900 tokens, 8 KV heads: 16.3 us, 24.1 with the rule at 16 steps; rows of 500
+// tokens, 16 columns: 19 us whole, 23 cut); else a part has at least kAqMinChunk steps and a cell (one row of
 // 1024 tokens, 12 heads: 9.5 us with 3, 10.0 with 4, 11.3 with 6, 14.4 whole).  What joining a unit costs weighs as much as
 // kAqJoinCells steps when the work is cut (23 rows of up to 8189 tokens, 16 columns: 78.5 us with 1, 65 with 3, 64 with 4,
 // 63 with 6; rows of 32768 tokens, 4 columns: 173, 171, 169, 169; rows of up to 4000 tokens, 8 columns of 64 dims: 15.9,

@@ -9,6 +9,7 @@
 //   fp16 results take the weights in fp16 (2^-12 of each).  fp32 results take them as two fp16 numbers, whose second halves
 // lie in the scores' second half of tensor memory, and move O out of tensor memory every 8 chunks: the tensor pipe cuts
 // its sums off: over a prompt of 4096 tokens one chain's largest error was 2.3e-6, that of chains of 8 chunks 1.0e-6.
+// (The fp32 variants spill 76 to 112 bytes at 128 registers, the fp16 ones nothing at 122.)
 //
 // A CTA works on two tiles of 128 rows against the same chunks of 64 tokens.  The scores of a tile have two buffers in
 // tensor memory, so the tensor pipe makes the next chunk's while the softmax threads work on this one's.  Roles (16 warps,
@@ -21,7 +22,7 @@
 //   warp 15     the scales of each chunk's blocks.
 // Tensor memory (512 columns): per tile S (2 x 64; the weights overwrite it) and O (d_v).  Q lies in shared memory.
 // Measured (B200, e4m3, one row of 4096 queries over its 4096 tokens, 8 KV heads of 4 query heads, 128 dims): fp16
-// results 180 us = 762 TFLOP/s, 46 % of a large bf16 matrix product; fp32 results 321 us.  What bounds it is the chain
+// results 180 us = 762 TFLOP/s, 46 % of a large bf16 matrix product; fp32 results 326 us.  What bounds it is the chain
 // of a chunk: 256 rows of 64 tokens take about 2800 cycles, of which the tensor pipe works a third, the exponentials
 // a third and the widening of the 8-bit rows the rest of the issue slots; see the counters' shares: tensor 36 %, issue
 // 38 %.  A second CTA per SM has no tensor memory left.
@@ -43,7 +44,11 @@ constexpr int kPqSoftmax = kPqBoth, kPqProducers = 128, kPqOperand = kPqProducer
 constexpr int kPqGroups = kPqChunk / 16;        // groups of 16 tokens: a page holds whole ones
 constexpr int kPqRaw = 3;                       // chunks of 8-bit rows in shared memory
 constexpr int kPqFlush = 8;                     // chunks that O stays in tensor memory for fp32 results
-constexpr int kPqMinPiece = 8;                  // chunks below which a row's tokens are not cut further
+// Least chunks of a piece of a row as long as its table.  The host knows the table's width alone: a shorter row has as many
+// pieces of fewer chunks, down to one.  (Holding those to 8 chunks too, in the kernel, was slower: 40 queries over 256 tokens in
+// a table for 32768, fp32 results, 19.3 us cut into single chunks and 23.8 as one piece, 17.9 in a table that fits; 200 queries
+// over 1000 tokens 24.0 and 30.2.  The join is there in any case.)
+constexpr int kPqMinPiece = 8;
 // How far M lies below the largest score (base-2 units), and how far scores may run ahead of that before M moves: weights
 // stay up to 2^(lift + slack) = 2^15.  With fp32 results the ones down to 2^-14 of the largest have 22 bits and what is dropped
 // is 2^-36 of it; with fp16 results those down to 2^-21 have 11.  (The lift cancels in O / (R l).)  Moving M costs a pass
