@@ -167,6 +167,7 @@ def test_the_first_step_can_be_captured():
 def test_the_cache_replaces_codes_and_values():
     """Codebooks, codes and fp16 values are given back: the 8-bit cache takes less than they did."""
     cap = 1024
+    step(prompt(model()), 0)                                    # (the kernels are loaded before memory is counted)
     w = synth.gpt2_weights(53, n_layer=4, n_head=8, d_model=512, vocab=50, n_pos=cap)
     torch.cuda.synchronize()
     m = LookatGpt2(w, 16, cap, 4, 16, fit_iters=1)
