@@ -29,6 +29,8 @@ EXPORTS = [
     "lookat_linear", "lookat_linear_qkv", "lookat_layernorm", "lookat_embed", "lookat_causal_attention", "lookat_argmax",
     # include/lookat_q8.h
     "lookat_q8_append", "lookat_attend_q8", "lookat_pages_extend", "lookat_pages_fork", "lookat_pages_compact",
+    # include/lookat_serve.h
+    "lookat_rope_table", "lookat_rope", "lookat_attend_packed", "lookat_q8_append_packed", "lookat_beam_select",
 ]
 
 STATUS = {0: "LOOKAT_OK", 1: "LOOKAT_ERR_INVALID_ARG", 2: "LOOKAT_ERR_UNSUPPORTED",
@@ -71,6 +73,20 @@ class lookat_page_state(ctypes.Structure):
 
 class lookat_page_pool(ctypes.Structure):
     _fields_ = [("base", ctypes.c_void_p), ("page_bytes", ctypes.c_int64)]
+
+
+class lookat_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class lookat_rope_config(ctypes.Structure):
+    _fields_ = [("rotary_dim", ctypes.c_int32), ("scaling", ctypes.c_int32)] + \
+               [(n, ctypes.c_double) for n in ("base", "factor", "original_len", "low", "high")]
+
+
+class lookat_beam_state(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("scores", "lengths", "finished", "tokens")] + \
+               [(n, ctypes.c_int32) for n in ("groups", "beams", "max_len")]
 
 
 _libs = {}
@@ -177,6 +193,18 @@ def load_library(debug: bool = False) -> ctypes.CDLL:
     lib.lookat_pages_fork.restype = i32
     lib.lookat_pages_compact.argtypes = [vp, ctypes.POINTER(lookat_page_state), ctypes.POINTER(lookat_page_pool), i32, vp]
     lib.lookat_pages_compact.restype = i32
+    # what runs around it (include/lookat_serve.h)
+    rows = ctypes.POINTER(lookat_rows)
+    lib.lookat_rope_table.argtypes = [ctypes.POINTER(lookat_rope_config), ctypes.POINTER(u64), ctypes.POINTER(ctypes.c_float)]
+    lib.lookat_rope_table.restype = i32
+    lib.lookat_rope.argtypes = [vp, rows, rows, i64, vp, vp, i32, i32, ctypes.c_float, rows, rows]
+    lib.lookat_rope.restype = i32
+    lib.lookat_attend_packed.argtypes = [vp, rows, rows, rows, i64, i32, vp, rows]
+    lib.lookat_attend_packed.restype = i32
+    lib.lookat_q8_append_packed.argtypes = [vp, ctypes.POINTER(lookat_q8_cache), rows, rows, i64, i32, vp, vp, i32, vp]
+    lib.lookat_q8_append_packed.restype = i32
+    lib.lookat_beam_select.argtypes = [vp, ctypes.POINTER(lookat_beam_state), vp, i64, i32, i32, ctypes.c_double, vp, vp]
+    lib.lookat_beam_select.restype = i32
     lib.lookat_is_debug_build.argtypes = []
     lib.lookat_is_debug_build.restype = i32
     _libs[debug] = lib
@@ -214,6 +242,66 @@ def _on(t, dtype, name, device, shape=None):
     if t is not None and t.device != device:
         raise ValueError(f"{name} is on {t.device}, the context on {device}")
     return p
+
+
+def _rows(t, name, device, shape):
+    """fp16 [tokens][heads][d] with dense vectors, as the library takes packed rows; a view of a wider tensor will do."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor (the library has no CPU path)")
+    if t.dtype is not torch.float16:
+        raise TypeError(f"{name} must have dtype torch.float16, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the context on {device}")
+    ts, hs, one = t.stride()
+    if one != 1 and shape[2] > 1:
+        raise ValueError(f"{name}: a vector's elements must lie next to each other")
+    return lookat_rows(t.data_ptr(), ts, hs)
+
+
+class RopeTable:
+    """The speeds of rotary positions (include/lookat_serve.h): turns per position of each pair on the device, and the factor on
+    cosines and sines.  scaling: none, linear, base, bands or ramp."""
+
+    SCALINGS = ("none", "linear", "base", "bands", "ramp")
+
+    def __init__(self, rotary_dim, base=10000.0, scaling="none", factor=1.0, original_len=0.0, low=1.0, high=32.0, device="cuda"):
+        if scaling not in self.SCALINGS:
+            raise ValueError(f"scaling must be one of {self.SCALINGS}, got {scaling!r}")
+        cfg = lookat_rope_config(rotary_dim, self.SCALINGS.index(scaling), base, factor, original_len, low, high)
+        turns, amplitude = (ctypes.c_uint64 * max(1, rotary_dim // 2))(), ctypes.c_float()
+        st = load_library().lookat_rope_table(ctypes.byref(cfg), turns, ctypes.byref(amplitude))
+        if st != 0:
+            raise LookatError(st, "lookat_rope_table: settings out of range")
+        self.rotary_dim, self.amplitude = rotary_dim, amplitude.value
+        self.host = list(turns)                                 # fractions of 2^64
+        self.turns = torch.tensor([t - (1 << 64) if t >> 63 else t for t in self.host], dtype=torch.int64, device=device)
+
+
+class BeamState:
+    """The beams of a batch (include/lookat_serve.h): scores fp32, lengths and finished int32 [groups][beams], tokens int32
+    [groups][beams][max_len] or None."""
+
+    def __init__(self, scores, lengths, finished, tokens=None):
+        if not isinstance(scores, torch.Tensor) or scores.dim() != 2:
+            raise ValueError("scores must have shape [groups][beams]")
+        shape, dev, i32 = tuple(scores.shape), scores.device, torch.int32
+        if tokens is not None and tokens.dim() != 3:
+            raise ValueError("tokens must have shape [groups][beams][max_len]")
+        self.scores, self.lengths, self.finished, self.tokens = scores, lengths, finished, tokens
+        self.groups, self.beams, self.device = *shape, dev
+        max_len = 0 if tokens is None else tokens.shape[2]
+        self.c = lookat_beam_state(_dev(scores, torch.float32, "scores"), _on(lengths, i32, "lengths", dev, shape), _on(finished, i32, "finished", dev, shape),
+                                   None if max_len == 0 else _on(tokens, i32, "tokens", dev, (*shape, max_len)), *shape, max_len)
+
+    @classmethod
+    def empty(cls, groups, beams, max_len, device="cuda"):
+        """Beams before their first step: only the first of each group counts."""
+        scores = torch.full((groups, beams), -math.inf, dtype=torch.float32, device=device)
+        scores[:, 0] = 0.0
+        z = lambda *s: torch.zeros(s, dtype=torch.int32, device=device)  # noqa: E731
+        return cls(scores, z(groups, beams), z(groups, beams), z(groups, beams, max_len) if max_len else None)
 
 
 class Q8Cache:
@@ -556,6 +644,72 @@ class Lookat:
         pools = self._pages(state, pools)
         self._check(self._lib.lookat_pages_compact(self._h, state.c, pools.c, len(pools.tensors),
                                                    _on(remap, torch.int32, "remap", self.device, (state.n_pages,))))
+
+    # -- what runs around it (include/lookat_serve.h) --------------------------------
+    def _empty(self, shape, dtype):
+        out = torch.empty(shape, dtype=dtype, device=self.device)
+        if torch._C._cuda_getCurrentRawStream(self.device.index) != self._raw_stream:
+            out.record_stream(self.stream)                      # allocated for another stream than the one that writes it
+        return out
+
+    def lookat_rope(self, q, k, positions, table, interleaved=False, q_out=None, k_out=None):
+        """Rotary positions of q [tokens][H_q][d_k] and k [tokens][H_kv][d_k] (either may be None); new tensors unless results are
+        given, which may be q and k themselves."""
+        H, H_kv, d, _ = self._shape
+        dev = self.device
+        T = (k if q is None else q).shape[0]
+        if table.turns.device != dev:
+            raise ValueError(f"the table is on {table.turns.device}, the context on {dev}")
+        args = []
+        for x, heads, name in ((q, H, "q"), (k, H_kv, "k")):
+            args.append(None if x is None else _rows(x, name, dev, (T, heads, d)))
+        if q is not None and q_out is None:
+            q_out = self._empty((T, H, d), torch.float16)
+        if k is not None and k_out is None:
+            k_out = self._empty((T, H_kv, d), torch.float16)
+        outs = [None if x is None else _rows(x, name, dev, (T, heads, d)) for x, heads, name in ((q_out, H, "q_out"), (k_out, H_kv, "k_out"))]
+        self._check(self._lib.lookat_rope(self._h, *args, T, _on(positions, torch.int32, "positions", dev, (T,)), table.turns.data_ptr(), table.rotary_dim,
+                                          1 if interleaved else 0, table.amplitude, *outs))
+        return q_out, k_out
+
+    def lookat_attend_packed(self, q, k, v, starts, out=None):
+        """Exact causal attention of packed prompts: q [tokens][H_q][d_k], k [tokens][H_kv][d_k], v [tokens][H_kv][d_v], row b the
+        tokens starts[b] .. starts[b + 1] - 1; tokens of no row keep what `out` held."""
+        H, H_kv, d_k, d_v = self._shape
+        dev = self.device
+        T, B = q.shape[0], starts.shape[0] - 1
+        if out is None:
+            out = self._empty((T, H, d_v), torch.float16)
+        self._check(self._lib.lookat_attend_packed(self._h, _rows(q, "q", dev, (T, H, d_k)), _rows(k, "k", dev, (T, H_kv, d_k)),
+                                                   _rows(v, "v", dev, (T, H_kv, d_v)), T, B, _on(starts, torch.int32, "starts", dev, (B + 1,)),
+                                                   _rows(out, "out", dev, (T, H, d_v))))
+        return out
+
+    def lookat_q8_append_packed(self, cache, k, v, starts, tables, seq_lens):
+        """Quantises the packed tokens starts[b] .. starts[b + 1] - 1 as the newest of row b; k [tokens][H_kv][d_k]."""
+        _, H, d_k, d_v = self._shape
+        dev = self.device
+        B, max_pages, tb, sl = self._q8(cache, tables, seq_lens)
+        T = k.shape[0]
+        self._check(self._lib.lookat_q8_append_packed(self._h, cache.c, _rows(k, "k", dev, (T, H, d_k)), _rows(v, "v", dev, (T, H, d_v)), T, B,
+                                                      _on(starts, torch.int32, "starts", dev, (B + 1,)), tb, max_pages, sl))
+
+    def lookat_beam_select(self, state, logits, eos=-1, length_penalty=0.0, next_ids=None, parents=None):
+        """One step of beam search over logits [groups * beams][vocab] (rows may lie further apart); the state moves in place.
+        Returns (next_ids, parents), int32 [groups * beams]."""
+        dev, rows = self.device, state.groups * state.beams
+        if state.device != dev:
+            raise ValueError(f"the beams are on {state.device}, the context on {dev}")
+        if not isinstance(logits, torch.Tensor) or not logits.is_cuda or logits.dtype is not torch.float32:
+            raise TypeError("logits must be a CUDA tensor of dtype torch.float32")
+        if logits.device != dev or logits.dim() != 2 or logits.shape[0] != rows or logits.shape[1] < 1 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+            raise ValueError(f"logits must have shape [{rows}][vocab] with dense rows on {dev}")
+        vocab = logits.shape[1]
+        next_ids = self._empty((rows,), torch.int32) if next_ids is None else next_ids
+        parents = self._empty((rows,), torch.int32) if parents is None else parents
+        self._check(self._lib.lookat_beam_select(self._h, state.c, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, vocab, eos, length_penalty,
+                                                 _on(next_ids, torch.int32, "next_ids", dev, (rows,)), _on(parents, torch.int32, "parents", dev, (rows,))))
+        return next_ids, parents
 
     def lookat_kernel_launches(self) -> int:
         return int(self._lib.lookat_kernel_launches(self._h))

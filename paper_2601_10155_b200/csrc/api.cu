@@ -8,6 +8,7 @@
 
 #include "common.cuh"
 #include "q8.cuh"
+#include "serve.cuh"
 
 namespace lookat {
 
@@ -311,7 +312,8 @@ void lookat_destroy(lookat_ctx *handle)
                     ctx->step_q,  ctx->step_k,  ctx->step_out};
     for (void *p : bufs)
         if (p) cudaFree(p);
-    for (Workspace *w : {&ctx->q8_partials, &ctx->q8_tickets, &ctx->q8_pieces, &ctx->page_lists, &ctx->page_marks}) {
+    for (Workspace *w : {&ctx->q8_partials, &ctx->q8_tickets, &ctx->q8_pieces, &ctx->page_lists, &ctx->page_marks, &ctx->beam_parts,
+                         &ctx->beam_tickets}) {
         if (w->ptr) cudaFree(w->ptr);
         for (int i = 0; i < w->n_outgrown; ++i) cudaFree(w->outgrown[i]);
     }
@@ -337,7 +339,7 @@ const char *lookat_last_error(const lookat_ctx *handle)
     if (ctx->status_word && *(volatile int *)ctx->status_word && (!ctx->err[0] || ctx->err_read)) {
         const int word = *(volatile int *)ctx->status_word;
         const int bit = word & kStatusCopyTimeout ? kStatusCopyTimeout : word & kStatusNoPages ? kStatusNoPages
-                        : word & kStatusBadPage   ? kStatusBadPage     : word;
+                        : word & kStatusBadPage   ? kStatusBadPage     : word & kStatusBadStart   ? kStatusBadStart : word;
         *(volatile int *)ctx->status_word = word & ~bit;
         if (bit == kStatusCopyTimeout)
             snprintf(ctx->err, sizeof(ctx->err), "attend: a bounded wait for a bulk copy ran out; the output of that call is not valid");
@@ -345,6 +347,8 @@ const char *lookat_last_error(const lookat_ctx *handle)
             snprintf(ctx->err, sizeof(ctx->err), "pages_extend: too few free pages or table entries; nothing was changed and n_new was set to 0");
         else if (bit == kStatusBadPage)
             snprintf(ctx->err, sizeof(ctx->err), "8-bit cache: a page id, length, count or parent row outside its range was met and left out");
+        else if (bit == kStatusBadStart)
+            snprintf(ctx->err, sizeof(ctx->err), "packed rows: a row whose start or end is out of range or order was met and taken as empty");
         else
             snprintf(ctx->err, sizeof(ctx->err),
                      "debug check: a code >= K was found in a code cache and clamped to K - 1; results computed from it are not valid");

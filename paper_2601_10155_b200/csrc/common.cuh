@@ -57,6 +57,8 @@ struct Ctx {
     size_t step_q_cap, step_k_cap, step_out_cap;   // bytes
     // 8-bit paged cache: partial results and arrival counters of the attention; lists of pages, tables being rewritten
     Workspace q8_partials, q8_tickets, q8_pieces, page_lists, page_marks;
+    // beam selection: the best and the sums of the rows' parts, arrival counters
+    Workspace beam_parts, beam_tickets;
 
     // per-launch timing of the attend kernel: an event pair per timed launch, read only after the timed run
     int timing;

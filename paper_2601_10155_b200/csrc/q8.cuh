@@ -41,6 +41,10 @@ struct Q8AppendArgs {
     const __half *k_new, *v_new;    // [B][H_kv][n][d]
     const int32_t *n_new;           // [B] or null
     int B, n, format;
+    // packed rows (lookat_q8_append_packed): row b's new tokens are starts[b] .. starts[b + 1] - 1 of n, their vectors
+    // ts elements apart by tokens and hs by heads
+    const int32_t *starts;          // [B + 1], or null
+    long long k_ts, k_hs, v_ts, v_hs;
 };
 lookat_status launch_q8_append(Ctx *ctx, const Q8AppendArgs &a);
 

@@ -9,7 +9,9 @@
 //
 // One group of threads per (row, KV head, K or V, block): it reads the block's new tokens once (kept in registers between
 // the maximum and the rounding), so nothing is read from HBM twice and no two groups share a block.
-#include "q8.cuh"
+#include <type_traits>
+
+#include "serve.cuh"
 
 namespace lookat {
 
@@ -110,20 +112,51 @@ __device__ __forceinline__ uint4 ap_shrink16(uint4 u, float was, float now)
 // THREADS per group: as many as hold a block's new tokens in kApKeep units each, since what bounds the kernel is how many
 // groups wait for their loads at a time (4 rows of up to 4096 tokens, 8 heads of 128 dims, pages of 64: 24 us with 128
 // threads, 25 with 256, 35 with 512; pages of 16: 39, 51 and 97)
-template <int FORMAT, int THREADS>
+//
+// PACKED: the rows' tokens stand one behind the other (a.starts), and the host does not know the rows' lengths.  A row of c
+// tokens touches at most c / page + 2 blocks (rounded down), so row b has the slots from starts[b] / page + 2 b on: those of
+// different rows lie apart, a bisection over the rows finds a slot's, and n / page + 2 B slots do for any lengths.
+template <int FORMAT, int THREADS, bool PACKED>
 __global__ void __launch_bounds__(THREADS == 32 ? 128 : THREADS, THREADS == 256 ? 4 : 8) q8_append_kernel(Q8AppendArgs a, int blocks_per_row)
 {
     constexpr int kGroups = THREADS == 32 ? 4 : 1;
     const int lane = THREADS == 32 ? (threadIdx.x & 31) : threadIdx.x;
     const long long item = (long long)blockIdx.x * kGroups + (THREADS == 32 ? threadIdx.x >> 5 : 0);
     const Q8View &c = a.c;
-    const int j = (int)(item % blocks_per_row), which = (int)(item / blocks_per_row & 1);
-    const long long bh = item / blocks_per_row >> 1;
-    const int b = (int)(bh / c.H_kv), h = (int)(bh % c.H_kv);
-    if (b >= a.B) return;                                       // (whole groups leave)
+    int j, which, b, h, start = 0;
+    long long bh = 0;
+    if constexpr (PACKED) {                                     // [slot][head][K or V]
+        which = (int)(item & 1);
+        h = (int)((item >> 1) % c.H_kv);
+        const long long slot = (item >> 1) / c.H_kv;
+        if (slot >= blocks_per_row) return;                     // (here the number of slots; whole groups leave)
+        auto slot0 = [&](int row) { return (long long)(min(max(__ldg(a.starts + row), 0), a.n) >> c.page_shift) + 2ll * row; };
+        int lo = 0, hi = a.B;                                   // the last row whose first slot is not behind this one
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            (slot0(mid) <= slot ? lo : hi) = mid;
+        }
+        b = lo;
+        j = (int)(slot - slot0(b));
+        if (j < 0) return;
+    } else {
+        j = (int)(item % blocks_per_row), which = (int)(item / blocks_per_row & 1);
+        bh = item / blocks_per_row >> 1;
+        b = (int)(bh / c.H_kv), h = (int)(bh % c.H_kv);
+        if (b >= a.B) return;                                   // (whole groups leave)
+    }
 
     const int page = 1 << c.page_shift, cap = c.max_pages << c.page_shift;
-    const int len_in = c.seq_lens[b], count_in = a.n_new ? max(a.n_new[b], 0) : a.n;
+    const int len_in = c.seq_lens[b];
+    int count_in;
+    if constexpr (PACKED) {
+        const Packed rows = {a.starts, a.B, a.n, c.status};
+        if (item == 0) packed_check(rows, lane, THREADS);
+        count_in = packed_row(rows, b, start);
+        if (count_in == 0) return;
+    } else {
+        count_in = a.n_new ? max(a.n_new[b], 0) : a.n;
+    }
     const int len = min(max(len_in, 0), cap), count = min(count_in, a.n);
     const int first = len_in - count;                           // position of the row's token 0 (may be out of range)
     if (lane == 0 && (len_in != len || count_in != count || first < 0)) q8_report(c.status, kStatusBadPage);
@@ -133,8 +166,22 @@ __global__ void __launch_bounds__(THREADS == 32 ? 128 : THREADS, THREADS == 256 
     if (lo >= hi) return;
     const int pid = c.tables[(size_t)b * c.max_pages + blk];   // (looked at once the new tokens are on their way too)
     const int d = which ? c.d_v : c.d_k, old = lo - (blk << c.page_shift);
-    const uint4 *src = reinterpret_cast<const uint4 *>((which ? a.v_new : a.k_new) + ((size_t)bh * a.n + (lo - first)) * d);
     const int units = (hi - lo) * d / 16;
+    // unit u: 16 elements of token u / (d / 16) of the block's new ones (below 2^11: the product with 2^20 / (d / 16) rounded up
+    // gives the quotient)
+    const unsigned per = (unsigned)d / 16, inverse = PACKED ? ((1u << 20) + per - 1) / per : 0;
+    const __half *src = which ? a.v_new : a.k_new;
+    const long long ts = which ? a.v_ts : a.k_ts;
+    if constexpr (PACKED) src += (start + (lo - first)) * ts + h * (which ? a.v_hs : a.k_hs);
+    else src += ((size_t)bh * a.n + (lo - first)) * d;
+    auto load = [&](int u) {
+        if constexpr (PACKED) {
+            const unsigned t = (unsigned)u * inverse >> 20;
+            return ap_load(reinterpret_cast<const uint4 *>(src + t * ts + (u - t * per) * 16));
+        } else {
+            return ap_load(reinterpret_cast<const uint4 *>(src) + 2 * u);
+        }
+    };
 
     ApUnit keep[kApKeep];
     __half2 tops2 = __halves2half2(__ushort_as_half(0), __ushort_as_half(0));
@@ -142,11 +189,11 @@ __global__ void __launch_bounds__(THREADS == 32 ? 128 : THREADS, THREADS == 256 
     for (int i = 0; i < kApKeep; ++i) {
         const int u = lane + i * THREADS;
         if (u < units) {
-            keep[i] = ap_load(src + 2 * u);
+            keep[i] = load(u);
             ap_max(tops2, keep[i]);
         }
     }
-    for (int u = lane + kApKeep * THREADS; u < units; u += THREADS) ap_max(tops2, ap_load(src + 2 * u));
+    for (int u = lane + kApKeep * THREADS; u < units; u += THREADS) ap_max(tops2, load(u));
     float top = fmaxf(__low2float(tops2), __high2float(tops2));
     if (pid < 0 || pid >= c.n_pages) {                          // (the same for the whole group)
         if (lane == 0) q8_report(c.status, kStatusBadPage);
@@ -180,7 +227,7 @@ __global__ void __launch_bounds__(THREADS == 32 ? 128 : THREADS, THREADS == 256 
         if (u < units) dst[u] = now > 0.f ? ap_round16<FORMAT>(keep[i], now, scale) : make_uint4(0u, 0u, 0u, 0u);
     }
     for (int u = lane + kApKeep * THREADS; u < units; u += THREADS)
-        dst[u] = now > 0.f ? ap_round16<FORMAT>(ap_load(src + 2 * u), now, scale) : make_uint4(0u, 0u, 0u, 0u);
+        dst[u] = now > 0.f ? ap_round16<FORMAT>(load(u), now, scale) : make_uint4(0u, 0u, 0u, 0u);
     if constexpr (THREADS == 32) __syncwarp();
     if (lane == 0) *amax_at = now;
 }
@@ -190,19 +237,23 @@ __global__ void __launch_bounds__(THREADS == 32 ? 128 : THREADS, THREADS == 256 
 lookat_status launch_q8_append(Ctx *ctx, const Q8AppendArgs &a)
 {
     const int page = 1 << a.c.page_shift;
-    const int blocks = (a.n + page - 2) / page + 1;             // blocks that n consecutive tokens can touch
-    const long long items = (long long)a.B * a.c.H_kv * 2 * blocks;
+    // blocks that n consecutive tokens can touch; packed rows: slots for all rows' blocks
+    const int blocks = a.starts ? (a.n >> a.c.page_shift) + 2 * a.B : (a.n + page - 2) / page + 1;
+    const long long items = (long long)(a.starts ? 1 : a.B) * a.c.H_kv * 2 * blocks;
     const int d = a.c.d_k > a.c.d_v ? a.c.d_k : a.c.d_v, units = (a.n < page ? a.n : page) * d / 16;     // of the largest group
     const int threads = units <= 32 * kApKeep ? 32 : units <= 128 * kApKeep ? 128 : 256;
     const long long ctas = threads == 32 ? (items + 3) / 4 : items;
     if (ctas > 0x7fffffffll) return set_error(ctx, LOOKAT_ERR_UNSUPPORTED, "q8_append: too many blocks for one call");
     auto launch = [&](auto kern) { kern<<<(unsigned)ctas, threads == 32 ? 128 : threads, 0, ctx->stream>>>(a, blocks); };
-    if (a.format == LOOKAT_Q8_INT8)
-        threads == 32 ? launch(q8_append_kernel<LOOKAT_Q8_INT8, 32>) : threads == 128 ? launch(q8_append_kernel<LOOKAT_Q8_INT8, 128>)
-                                                                                      : launch(q8_append_kernel<LOOKAT_Q8_INT8, 256>);
-    else
-        threads == 32 ? launch(q8_append_kernel<LOOKAT_Q8_E4M3, 32>) : threads == 128 ? launch(q8_append_kernel<LOOKAT_Q8_E4M3, 128>)
-                                                                                      : launch(q8_append_kernel<LOOKAT_Q8_E4M3, 256>);
+    auto sized = [&](auto format, auto packed) {
+        constexpr int F = decltype(format)::value;
+        constexpr bool P = decltype(packed)::value;
+        threads == 32 ? launch(q8_append_kernel<F, 32, P>) : threads == 128 ? launch(q8_append_kernel<F, 128, P>) : launch(q8_append_kernel<F, 256, P>);
+    };
+    using Int8 = std::integral_constant<int, LOOKAT_Q8_INT8>;
+    using E4m3 = std::integral_constant<int, LOOKAT_Q8_E4M3>;
+    if (a.format == LOOKAT_Q8_INT8) a.starts ? sized(Int8{}, std::true_type{}) : sized(Int8{}, std::false_type{});
+    else a.starts ? sized(E4m3{}, std::true_type{}) : sized(E4m3{}, std::false_type{});
     return check_launch(ctx, "q8_append_kernel");
 }
 
