@@ -19,7 +19,7 @@ LIB = os.path.join(PKG, "liblookat.so")
 LIB_DEBUG = os.path.join(PKG, "liblookat_debug.so")
 SOURCES = ["api.cu", "attend.cu", "attend_multi.cu", "attend_static.cu", "attend_pqv.cu", "prefill.cu", "prefill_umma.cu", "lut.cu", "encode.cu", "encode_mma.cu", "fit.cu", "probe.cu", "linear_umma.cu", "gpt2_ops.cu", "gpt2.cu",
            "q8_api.cu", "q8_append.cu", "attend_q8.cu", "attend_q8_umma.cu", "pages.cu",
-           "serve_api.cu", "rope.cu", "attend_packed.cu", "beam.cu"]
+           "serve_api.cu", "rope.cu", "attend_packed.cu", "attend_packed_umma.cu", "beam.cu"]
 
 
 def _nvcc() -> str:

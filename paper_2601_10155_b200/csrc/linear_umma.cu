@@ -416,6 +416,24 @@ bool make_tile_map_f16(void *map, const void *base, unsigned long long inner, un
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool make_rows_map_f16(void *map, const void *base, int d, int heads, long long tokens, long long head_stride, long long token_stride,
+                       int box_tokens, int *heads_last)
+{
+    tensor_map_encode_fn encode = tensor_map_encoder();
+    if (!encode) return false;
+    const cuuint64_t hs = (cuuint64_t)(heads > 1 ? head_stride : d) * 2, ts = (cuuint64_t)(tokens > 1 ? token_stride : d) * 2;
+    *heads_last = heads > 1 && tokens > 1 && hs > ts;
+    const int h = *heads_last ? 2 : 1, t = *heads_last ? 1 : 2;
+    cuuint64_t dims[3] = {(cuuint64_t)d, 0, 0}, strides[2];
+    dims[h] = (cuuint64_t)heads, dims[t] = (cuuint64_t)tokens;
+    strides[h - 1] = hs, strides[t - 1] = ts;
+    cuuint32_t box[3] = {64, 1, 1}, estr[3] = {1, 1, 1};
+    box[t] = (cuuint32_t)box_tokens;
+    return encode(static_cast<CUtensorMap *>(map), CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 lookat_status launch_linear(Ctx *ctx, const void *x, int x_fp32, const __half *w_t, LinearArgs p)
 {
     p.timeout_flag = ctx->timeout_flag;
