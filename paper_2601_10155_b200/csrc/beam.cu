@@ -5,6 +5,8 @@
 //     fp64, so that the ranks of different beams are compared to 1e-8;
 //   - its `beams` best logits (a beam's candidates rank as its logits do), sorted over the lanes: lane i holds the i-th.  A logit
 //     enters if it beats the last of them, which soon is rare; the first 512 logits' lane maxima give the bar to begin with.
+// Rows are read in the same order whatever their alignment (16-byte loads where all rows lie on such borders, else 4-byte ones):
+// beams with equal logits and scores get equal ranks, and the lower one goes first.
 // The CTA's warps join in shared memory.  The last CTA of a group to finish (a counter, no waiting) joins the parts, ranks
 // in fp64, and moves the beams.
 #include "serve.cuh"
@@ -13,7 +15,8 @@ namespace lookat {
 
 namespace {
 
-constexpr int kBsThreads = 256, kBsWarps = kBsThreads / 32, kBsVecs = 4, kBsMost = 32;      // kBsVecs: 16-byte pieces per thread and batch
+constexpr int kBsThreads = 256, kBsWarps = kBsThreads / 32, kBsVecs = 4, kBsMost = 32;
+constexpr int kBsBatch = kBsThreads * kBsVecs * 4;            // logits that a CTA has in flight
 
 struct BsPart {                     // of a row: its best logits, sum exp(x - m) and m
     float best[kBsMost];
@@ -55,6 +58,13 @@ __device__ __forceinline__ float bs_max_nan(float a, float b)   // NaN if either
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
     return d;
 }
+// whole numbers in the order of floats
+__device__ __forceinline__ int bs_ordered(float x)
+{
+    const int i = __float_as_int(x);
+    return i < 0 ? i ^ 0x7fffffff : i;
+}
+__device__ __forceinline__ float bs_number(int i) { return __int_as_float(i < 0 ? i ^ 0x7fffffff : i); }
 // the (n + 1)-th largest of the lanes' numbers
 __device__ __forceinline__ float bs_nth(float v, int n, int lane)
 {
@@ -69,131 +79,12 @@ __device__ __forceinline__ float bs_nth(float v, int n, int lane)
     return __shfl_sync(0xffffffffu, v, n);
 }
 
-__global__ void __launch_bounds__(kBsThreads)
-beam_select_kernel(BeamArgs a, int splits, BsPart *__restrict__ parts, unsigned *__restrict__ tickets)
+// The group's parts joined and ranked, its beams moved.
+__device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const BsPart *__restrict__ parts, int group, double (*s_rank)[kBsMost],
+                                         int (*s_at)[kBsMost])
 {
-    __shared__ float s_key[kBsWarps][kBsMost];
-    __shared__ double s_rank[kBsWarps][kBsMost];
-    __shared__ int s_at[kBsWarps][kBsMost];
-    __shared__ double s_sum[kBsWarps];
-    __shared__ float s_m[kBsWarps];
-    __shared__ int s_bad[kBsWarps];
-    __shared__ int s_last;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, W = a.beams;
-    const int row = blockIdx.x / splits, split = blockIdx.x % splits, group = row / W;
-    const float score = a.scores[row];
-    const bool live = a.finished[row] == 0 && score > -INFINITY && score < INFINITY;
-
-    if (live) {
-        // ---- the part's logits, in 16-byte pieces of memory: those at the row's ends hold others' logits too ----
-        const float *x0 = a.logits + (long long)row * a.stride;
-        const int skew = (int)(reinterpret_cast<uintptr_t>(x0) >> 2 & 3);
-        const float *aligned = x0 - skew;                      // (not read before x0)
-        const int vecs = (a.vocab + skew + 3) / 4, per = (vecs + splits - 1) / splits;
-        const int v0 = split * per, v1 = min(v0 + per, vecs);
-        BsList<float> list;
-        list.clear();
-        float m = -INFINITY;
-        double sum = 0.0;
-        bool bad = false;
-        for (int v = v0 + tid; v - tid < v1; v += kBsThreads * kBsVecs) {
-            float x[kBsVecs][4];
-#pragma unroll
-            for (int i = 0; i < kBsVecs; ++i) {
-                const int vec = v + i * kBsThreads, e = 4 * vec - skew;        // e: the first element
-                if (vec < v1 && e >= 0 && e + 4 <= a.vocab) {
-                    const float4 y = __ldcs(reinterpret_cast<const float4 *>(aligned) + vec);
-                    x[i][0] = y.x, x[i][1] = y.y, x[i][2] = y.z, x[i][3] = y.w;
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[i][j] = vec < v1 && e + j >= 0 && e + j < a.vocab ? __ldg(x0 + e + j) : -INFINITY;
-                }
-            }
-            float top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < kBsVecs; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) top = bs_max_nan(top, x[i][j]);
-            if (__any_sync(0xffffffffu, !(top < INFINITY))) {  // nothing of the row counts any more
-                bad = true;
-                break;
-            }
-            if (m == -INFINITY || __any_sync(0xffffffffu, top > m + 20.f)) {
-                float t = top;
-#pragma unroll
-                for (int o = 16; o; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
-                if (m > -INFINITY) sum *= exp((double)m - (double)t);
-                else if (t > -INFINITY) list.bar = bs_nth(top, W - 1, lane);
-                m = t;
-                if (m == -INFINITY) continue;
-            }
-            float add = 0.f;
-#pragma unroll
-            for (int i = 0; i < kBsVecs; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) add += ex2_approx((x[i][j] - m) * 1.4426950408889634f);
-            sum += (double)add;
-            if (!__any_sync(0xffffffffu, top >= list.bar)) continue;
-#pragma unroll
-            for (int i = 0; i < kBsVecs; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int e = 4 * (v + i * kBsThreads) - skew + j;
-                    unsigned who = __ballot_sync(0xffffffffu, list.beats(x[i][j], e));
-                    while (who) {
-                        const int src = __ffs(who) - 1;
-                        who &= who - 1;
-                        const float k = __shfl_sync(0xffffffffu, x[i][j], src);
-                        const int at = e + 4 * (src - lane);
-                        if (list.beats(k, at)) list.insert(k, at, lane, W);
-                    }
-                }
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        s_key[warp][lane] = list.key;
-        s_at[warp][lane] = list.at;
-        if (lane == 0) s_sum[warp] = sum, s_m[warp] = m, s_bad[warp] = bad;
-        __syncthreads();
-        if (warp == 0) {
-            BsPart &p = parts[(size_t)row * splits + split];
-            for (int w = 1; w < kBsWarps; ++w) {
-                const float k = s_key[w][lane];
-                const int at = s_at[w][lane];
-                unsigned who = __ballot_sync(0xffffffffu, lane < W && list.beats(k, at));
-                while (who) {
-                    const int src = __ffs(who) - 1;
-                    who &= who - 1;
-                    const float kk = __shfl_sync(0xffffffffu, k, src);
-                    const int aa = __shfl_sync(0xffffffffu, at, src);
-                    if (list.beats(kk, aa)) list.insert(kk, aa, lane, W);
-                }
-            }
-            p.best[lane] = list.key;
-            p.at[lane] = list.at;
-            float top = -INFINITY;
-            bool any_bad = false;
-            for (int w = 0; w < kBsWarps; ++w) top = fmaxf(top, s_m[w]), any_bad |= s_bad[w] != 0;
-            double total = 0.0;                                // (the same in every lane)
-            for (int w = 0; w < kBsWarps; ++w)
-                if (s_m[w] > -INFINITY) total += s_sum[w] * exp((double)s_m[w] - (double)top);
-            if (lane == 0) p.sum = total, p.m = top, p.bad = any_bad;
-            __threadfence();
-        }
-    }
-
-    // ---- the group's last CTA goes on ----
-    __syncthreads();
-    if (tid == 0) {
-        const unsigned last = (unsigned)(W * splits - 1);
-        s_last = atomicAdd(tickets + group, 1u) == last;
-        if (s_last) tickets[group] = 0;
-    }
-    __syncthreads();
-    if (!s_last) return;
-    __threadfence();
-
-    __shared__ double s_base[kBsMost], s_norm[kBsMost];       // score = base + (x - m); rank = score / norm
+    __shared__ double s_base[kBsMost];                         // score = base + (x - m)
     __shared__ float s_top[kBsMost], s_score[kBsMost];
     __shared__ int s_len[kBsMost], s_fin[kBsMost], s_parent[kBsMost];
     const int g0 = group * W;
@@ -246,7 +137,7 @@ beam_select_kernel(BeamArgs a, int splits, BsPart *__restrict__ parts, unsigned 
         } else if (counts) {
             offer((double)sc / norm, w * a.vocab + max(a.eos, 0), lane == 0);
         }
-        if (lane == 0) s_base[w] = base, s_norm[w] = norm, s_top[w] = top;
+        if (lane == 0) s_base[w] = base, s_top[w] = top;
     }
     s_rank[warp][lane] = list.key;
     s_at[warp][lane] = list.at;
@@ -285,22 +176,155 @@ beam_select_kernel(BeamArgs a, int splits, BsPart *__restrict__ parts, unsigned 
     }
 }
 
+template <bool WIDE>
+__global__ void __launch_bounds__(kBsThreads, 3)
+beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsPart *__restrict__ parts, unsigned *__restrict__ tickets)
+{
+    __shared__ float s_key[kBsWarps][kBsMost];
+    __shared__ double s_rank[kBsWarps][kBsMost];
+    __shared__ int s_at[kBsWarps][kBsMost];
+    __shared__ double s_sum[kBsWarps];
+    __shared__ float s_m[kBsWarps];
+    __shared__ int s_bad[kBsWarps];
+    __shared__ int s_last, s_bar;                              // s_bar: a logit that `beams` of the part reach, as bs_ordered
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, W = a.beams;
+    const int row = blockIdx.x / splits, split = blockIdx.x % splits, group = row / W;
+    const float score = a.scores[row];
+    const bool live = a.finished[row] == 0 && score > -INFINITY && score < INFINITY;
+
+    if (live) {                                                // (the same for the whole CTA)
+        if (tid == 0) s_bar = bs_ordered(-INFINITY);
+        __syncthreads();
+        const float *x0 = a.logits + (long long)row * a.stride;
+        const int e1 = min((split + 1) * part, a.vocab);
+        BsList<float> list;
+        list.clear();
+        float m = -INFINITY;
+        double sum = 0.0;
+        bool bad = false;
+        for (int e0 = split * part; e0 < e1; e0 += kBsBatch) {
+            // element e0 + 4 tid + 1024 i + j (wide), or e0 + tid + 256 (4 i + j)
+            float x[kBsVecs][4];
+            auto element = [&](int i, int j) { return WIDE ? e0 + 4 * (i * kBsThreads + tid) + j : e0 + (4 * i + j) * kBsThreads + tid; };
+#pragma unroll
+            for (int i = 0; i < kBsVecs; ++i) {
+                if (WIDE && element(i, 3) < e1) {
+                    const float4 y = __ldcs(reinterpret_cast<const float4 *>(x0 + element(i, 0)));
+                    x[i][0] = y.x, x[i][1] = y.y, x[i][2] = y.z, x[i][3] = y.w;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[i][j] = element(i, j) < e1 ? __ldcs(x0 + element(i, j)) : -INFINITY;
+                }
+            }
+            float top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < kBsVecs; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) top = bs_max_nan(top, x[i][j]);
+            if (__any_sync(0xffffffffu, !(top < INFINITY))) {  // nothing of the row counts any more
+                bad = true;
+                break;
+            }
+            if (m == -INFINITY || __any_sync(0xffffffffu, top > m + 20.f)) {
+                float t = top;
+#pragma unroll
+                for (int o = 16; o; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
+                if (m > -INFINITY) sum *= exp((double)m - (double)t);
+                else if (t > -INFINITY) list.bar = bs_nth(top, W - 1, lane);
+                m = t;
+                if (m == -INFINITY) continue;
+            }
+            float add = 0.f;
+#pragma unroll
+            for (int i = 0; i < kBsVecs; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) add += ex2_approx((x[i][j] - m) * 1.4426950408889634f);
+            sum += (double)add;
+            const float shared_bar = bs_number(*(volatile int *)&s_bar);
+            if (shared_bar > list.bar) list.bar = shared_bar, list.bar_at = 0x7fffffff;
+            if (!__any_sync(0xffffffffu, top >= list.bar)) continue;
+#pragma unroll
+            for (int i = 0; i < kBsVecs; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int e = element(i, j);
+                    unsigned who = __ballot_sync(0xffffffffu, list.beats(x[i][j], e));
+                    while (who) {
+                        const int src = __ffs(who) - 1;
+                        who &= who - 1;
+                        const float k = __shfl_sync(0xffffffffu, x[i][j], src);
+                        const int at = e + (WIDE ? 4 : 1) * (src - lane);
+                        if (list.beats(k, at)) list.insert(k, at, lane, W);
+                    }
+                }
+            if (lane == 0) atomicMax(&s_bar, bs_ordered(list.bar));
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        s_key[warp][lane] = list.key;
+        s_at[warp][lane] = list.at;
+        if (lane == 0) s_sum[warp] = sum, s_m[warp] = m, s_bad[warp] = bad;
+        __syncthreads();
+        if (warp == 0) {
+            BsPart &p = parts[(size_t)row * splits + split];
+            for (int w = 1; w < kBsWarps; ++w) {
+                const float k = s_key[w][lane];
+                const int at = s_at[w][lane];
+                unsigned who = __ballot_sync(0xffffffffu, lane < W && list.beats(k, at));
+                while (who) {
+                    const int src = __ffs(who) - 1;
+                    who &= who - 1;
+                    const float kk = __shfl_sync(0xffffffffu, k, src);
+                    const int aa = __shfl_sync(0xffffffffu, at, src);
+                    if (list.beats(kk, aa)) list.insert(kk, aa, lane, W);
+                }
+            }
+            p.best[lane] = list.key;
+            p.at[lane] = list.at;
+            float top = -INFINITY;
+            bool any_bad = false;
+            for (int w = 0; w < kBsWarps; ++w) top = fmaxf(top, s_m[w]), any_bad |= s_bad[w] != 0;
+            double total = 0.0;                                // (the same in every lane)
+            for (int w = 0; w < kBsWarps; ++w)
+                if (s_m[w] > -INFINITY) total += s_sum[w] * exp((double)s_m[w] - (double)top);
+            if (lane == 0) p.sum = total, p.m = top, p.bad = any_bad;
+            __threadfence();
+        }
+    }
+
+    // ---- the group's last CTA goes on ----
+    __syncthreads();
+    if (tid == 0) {
+        const unsigned last = (unsigned)(W * splits - 1);
+        s_last = atomicAdd(tickets + group, 1u) == last;
+        if (s_last) tickets[group] = 0;
+    }
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+
+    beam_finish(a, splits, parts, group, s_rank, s_at);
+}
+
 }  // namespace
 
 lookat_status launch_beam_select(Ctx *ctx, const BeamArgs &a)
 {
-    const long long rows = (long long)a.groups * a.beams, batch = kBsThreads * kBsVecs * 4;
-    // parts of a row: enough CTAs to fill the GPU a few times over, none of less than a batch of its threads
+    const long long rows = (long long)a.groups * a.beams;
+    // parts of a row: enough CTAs to fill the GPU a few times over, whole batches each
+    const int batches = (a.vocab + kBsBatch - 1) / kBsBatch;
     long long splits = (4ll * 4 * ctx->sm_count + rows - 1) / rows;
-    const long long most = (a.vocab + batch - 1) / batch;
-    if (splits > most) splits = most;
-    if (splits < 1) splits = 1;
+    if (splits > batches) splits = batches;
+    const int per = (int)((batches + splits - 1) / splits);
+    splits = (batches + per - 1) / per;
     lookat_status st = workspace(ctx, ctx->beam_parts, (size_t)(rows * splits) * sizeof(BsPart), false, "beam_select");
     if (st != LOOKAT_OK) return st;
     st = workspace(ctx, ctx->beam_tickets, (size_t)a.groups * sizeof(unsigned), true, "beam_select");
     if (st != LOOKAT_OK) return st;
-    beam_select_kernel<<<(unsigned)(rows * splits), kBsThreads, 0, ctx->stream>>>(a, (int)splits, static_cast<BsPart *>(ctx->beam_parts.ptr),
-                                                                                  static_cast<unsigned *>(ctx->beam_tickets.ptr));
+    const bool wide = (reinterpret_cast<uintptr_t>(a.logits) & 15) == 0 && a.stride % 4 == 0;
+    auto kern = wide ? beam_select_kernel<true> : beam_select_kernel<false>;
+    kern<<<(unsigned)(rows * splits), kBsThreads, 0, ctx->stream>>>(a, (int)splits, per * kBsBatch, static_cast<BsPart *>(ctx->beam_parts.ptr),
+                                                                    static_cast<unsigned *>(ctx->beam_tickets.ptr));
     return check_launch(ctx, "beam_select_kernel");
 }
 
