@@ -3,8 +3,9 @@
 // Bound by HBM: the logits are read once.  A row is cut into `splits` parts, a CTA each; in one pass a warp keeps
 //   - sum exp(x - m) against a reference m that it takes from its first logits and seldom moves: fp32 exponentials, their sums
 //     fp64, so that the ranks of different beams are compared to 1e-8;
-//   - its `beams` best logits (a beam's candidates rank as its logits do), sorted over the lanes: lane i holds the i-th.  A logit
-//     enters if it beats the last of them, which soon is rare; the first 512 logits' lane maxima give the bar to begin with.
+//   - its best 32 logits (a beam's candidates rank as its logits do), sorted over the lanes.  What reaches a bar is collected in
+//     shared memory and sorted in 32 at a time (a bitonic sort and a merge).  The CTA's first 4096 logits give the bar to begin
+//     with, near the `beams`-th largest of its threads' maxima; then few logits reach it.
 // Rows are read in the same order whatever their alignment (16-byte loads where all rows lie on such borders, else 4-byte ones):
 // beams with equal logits and scores get equal ranks, and the lower one goes first.
 // The CTA's warps join in shared memory.  The last CTA of a group to finish (a counter, no waiting) joins the parts, ranks
@@ -17,6 +18,7 @@ namespace {
 
 constexpr int kBsThreads = 256, kBsWarps = kBsThreads / 32, kBsVecs = 4, kBsMost = 32;
 constexpr int kBsBatch = kBsThreads * kBsVecs * 4;            // logits that a CTA has in flight
+constexpr int kBsHold = 64;                                    // candidates that a warp collects before it sorts them in
 
 struct BsPart {                     // of a row: its best logits, sum exp(x - m) and m
     float best[kBsMost];
@@ -26,29 +28,32 @@ struct BsPart {                     // of a row: its best logits, sum exp(x - m)
     int bad;                        // a NaN or +inf among them
 };
 
-// A warp's best so far, lane i the i-th; equal keys in rising order of `at`.
+// 32 candidates of a warp, one per lane
 template <class Key>
-struct BsList {
-    Key key, bar;                   // bar, bar_at: what a candidate has to beat (all lanes the same)
-    int at, bar_at;
-    __device__ void clear()
+struct BsBlock {
+    Key key;
+    int at;
+    __device__ bool before(Key k, int i) const { return key > k || (key == k && at < i); }      // this one goes first
+    __device__ void exchange(int mask, bool first)             // with the lane at that distance; first: this lane keeps what goes first
     {
-        key = bar = -INFINITY;
-        at = bar_at = 0x7fffffff;
+        const Key k = __shfl_xor_sync(0xffffffffu, key, mask);
+        const int i = __shfl_xor_sync(0xffffffffu, at, mask);
+        if (before(k, i) != first) key = k, at = i;
     }
-    __device__ bool beats(Key k, int i) const { return k > bar || (k == bar && k > -INFINITY && i < bar_at); }
-    // one candidate (the same in all lanes); returns its place
-    __device__ int insert(Key k, int i, int lane, int beams)
+    // first to last over the lanes, or with `up` last to first
+    __device__ void sort(int lane, bool up)
     {
-        const int place = __popc(__ballot_sync(0xffffffffu, key > k || (key == k && at < i)));
-        const Key up = __shfl_up_sync(0xffffffffu, key, 1);
-        const int up_at = __shfl_up_sync(0xffffffffu, at, 1);
-        if (lane > place) key = up, at = up_at;
-        if (lane == place) key = k, at = i;
-        const Key last = __shfl_sync(0xffffffffu, key, beams - 1);
-        const int last_at = __shfl_sync(0xffffffffu, at, beams - 1);
-        if (beats(last, last_at)) bar = last, bar_at = last_at;
-        return place;
+#pragma unroll
+        for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+            for (int j = k >> 1; j; j >>= 1) exchange(j, (((lane & k) == 0) == ((lane & j) == 0)) != up);
+    }
+    // the first 32 of this block (first to last) and of another's candidates, last to first: first to last
+    __device__ void join(Key k, int i, int lane)
+    {
+        if (!before(k, i)) key = k, at = i;
+#pragma unroll
+        for (int j = 16; j; j >>= 1) exchange(j, (lane & j) == 0);
     }
 };
 
@@ -65,28 +70,16 @@ __device__ __forceinline__ int bs_ordered(float x)
     return i < 0 ? i ^ 0x7fffffff : i;
 }
 __device__ __forceinline__ float bs_number(int i) { return __int_as_float(i < 0 ? i ^ 0x7fffffff : i); }
-// the (n + 1)-th largest of the lanes' numbers
-__device__ __forceinline__ float bs_nth(float v, int n, int lane)
-{
-#pragma unroll
-    for (int k = 2; k <= 32; k <<= 1)
-#pragma unroll
-        for (int j = k >> 1; j; j >>= 1) {
-            const float o = __shfl_xor_sync(0xffffffffu, v, j);
-            const bool larger = ((lane & k) == 0) == ((lane & j) == 0);     // descending blocks, then ascending ones
-            v = larger ? fmaxf(v, o) : fminf(v, o);
-        }
-    return __shfl_sync(0xffffffffu, v, n);
-}
 
 // The group's parts joined and ranked, its beams moved.
-__device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const BsPart *__restrict__ parts, int group, double (*s_rank)[kBsMost],
-                                         int (*s_at)[kBsMost])
+__device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const BsPart *__restrict__ parts, int group)
 {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, W = a.beams;
+    __shared__ double s_rank[kBsWarps][kBsMost];
+    __shared__ int s_at[kBsWarps][kBsMost];
     __shared__ double s_base[kBsMost];                         // score = base + (x - m)
     __shared__ float s_top[kBsMost], s_score[kBsMost];
-    __shared__ int s_len[kBsMost], s_fin[kBsMost], s_parent[kBsMost];
+    __shared__ int s_len[kBsMost], s_fin[kBsMost], s_parent[kBsMost], s_slot[kBsMost], s_token[kBsMost];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, W = a.beams;
     const int g0 = group * W;
     if (tid < W) {
         s_score[tid] = a.scores[g0 + tid];
@@ -94,18 +87,7 @@ __device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const Bs
         s_fin[tid] = a.finished[g0 + tid] != 0;
     }
     __syncthreads();
-    BsList<double> list;
-    list.clear();
-    auto offer = [&](double k, int at, bool on) {              // a candidate per lane
-        unsigned who = __ballot_sync(0xffffffffu, on && list.beats(k, at));
-        while (who) {
-            const int src = __ffs(who) - 1;
-            who &= who - 1;
-            const double kk = __shfl_sync(0xffffffffu, k, src);
-            const int aa = __shfl_sync(0xffffffffu, at, src);
-            if (list.beats(kk, aa)) list.insert(kk, aa, lane, W);
-        }
-    };
+    BsBlock<double> best = {-INFINITY, 0x7fffffff};
     for (int w = warp; w < W; w += kBsWarps) {
         const float sc = s_score[w];
         const bool counts = sc > -INFINITY && sc < INFINITY;
@@ -128,25 +110,26 @@ __device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const Bs
 #pragma unroll
                 for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
                 base = (double)sc - log(total);
-                for (int i = 0; i < splits; ++i) {
-                    const float x = __ldcg(&p[i].best[lane]);
-                    const int at = __ldcg(&p[i].at[lane]);
-                    offer((base + ((double)x - (double)top)) / norm, w * a.vocab + at, lane < W && x > -INFINITY);
+                for (int i = 0; i < splits; ++i) {             // a part's logits stand first to last: read last to first
+                    const float x = __ldcg(&p[i].best[31 - lane]);
+                    const int at = __ldcg(&p[i].at[31 - lane]);
+                    const bool on = x > -INFINITY;
+                    best.join(on ? (base + ((double)x - (double)top)) / norm : -INFINITY, on ? w * a.vocab + at : 0x7fffffff, lane);
                 }
             }
         } else if (counts) {
-            offer((double)sc / norm, w * a.vocab + max(a.eos, 0), lane == 0);
+            best.join(lane == 31 ? (double)sc / norm : -INFINITY, lane == 31 ? w * a.vocab + max(a.eos, 0) : 0x7fffffff, lane);
         }
         if (lane == 0) s_base[w] = base, s_top[w] = top;
     }
-    s_rank[warp][lane] = list.key;
-    s_at[warp][lane] = list.at;
+    s_rank[warp][lane] = best.key;
+    s_at[warp][lane] = best.at;
     __syncthreads();
     if (warp == 0) {
-        for (int w = 1; w < kBsWarps; ++w) offer(s_rank[w][lane], s_at[w][lane], lane < W && s_rank[w][lane] > -INFINITY);
+        for (int w = 1; w < min(W, kBsWarps); ++w) best.join(s_rank[w][31 - lane], s_at[w][31 - lane], lane);
         if (lane < W) {
-            const bool there = list.key > -INFINITY;
-            const int parent = there ? list.at / a.vocab : lane, token = there ? list.at % a.vocab : max(a.eos, 0);
+            const bool there = best.key > -INFINITY;
+            const int parent = there ? best.at / a.vocab : lane, token = there ? best.at % a.vocab : max(a.eos, 0);
             const bool grows = there && !s_fin[parent];
             float now = -INFINITY;
             if (there) now = s_fin[parent] ? s_score[parent] : (float)(s_base[parent] + ((double)a.logits[(long long)(g0 + parent) * a.stride + token] - (double)s_top[parent]));
@@ -157,8 +140,8 @@ __device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const Bs
             a.next_ids[g0 + lane] = token;
             a.parents[g0 + lane] = g0 + parent;
             s_parent[lane] = parent;
-            s_at[0][lane] = grows ? was : -1;                  // where its token goes
-            s_at[1][lane] = token;
+            s_slot[lane] = grows ? was : -1;
+            s_token[lane] = token;
         }
     }
     if (!a.max_len) return;
@@ -169,7 +152,7 @@ __device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const Bs
         int32_t y[kBsMost];
 #pragma unroll
         for (int w = 0; w < kBsMost; ++w)
-            if (w < W) y[w] = s_at[0][w] == c ? s_at[1][w] : tokens[(size_t)s_parent[w] * a.max_len + c];
+            if (w < W) y[w] = s_slot[w] == c ? s_token[w] : tokens[(size_t)s_parent[w] * a.max_len + c];
 #pragma unroll
         for (int w = 0; w < kBsMost; ++w)
             if (w < W) tokens[(size_t)w * a.max_len + c] = y[w];
@@ -177,16 +160,14 @@ __device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const Bs
 }
 
 template <bool WIDE>
-__global__ void __launch_bounds__(kBsThreads, 3)
+__global__ void __launch_bounds__(kBsThreads, 4)
 beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsPart *__restrict__ parts, unsigned *__restrict__ tickets)
 {
-    __shared__ float s_key[kBsWarps][kBsMost];
-    __shared__ double s_rank[kBsWarps][kBsMost];
-    __shared__ int s_at[kBsWarps][kBsMost];
+    __shared__ float s_hold[kBsWarps][kBsHold + 32];           // a warp's candidates; in the end the warps' best
+    __shared__ int s_hold_at[kBsWarps][kBsHold + 32];
     __shared__ double s_sum[kBsWarps];
     __shared__ float s_m[kBsWarps];
-    __shared__ int s_bad[kBsWarps];
-    __shared__ int s_last, s_bar;                              // s_bar: a logit that `beams` of the part reach, as bs_ordered
+    __shared__ int s_bad[kBsWarps], s_last, s_bar;             // s_bar: a logit that `beams` of the part reach, as bs_ordered
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, W = a.beams;
     const int row = blockIdx.x / splits, split = blockIdx.x % splits, group = row / W;
     const float score = a.scores[row];
@@ -197,11 +178,24 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
         __syncthreads();
         const float *x0 = a.logits + (long long)row * a.stride;
         const int e1 = min((split + 1) * part, a.vocab);
-        BsList<float> list;
-        list.clear();
-        float m = -INFINITY;
+        BsBlock<float> best = {-INFINITY, 0x7fffffff};
+        float bar = -INFINITY, m = -INFINITY;
+        int held = 0;
         double sum = 0.0;
-        bool bad = false;
+        bool bad = false, barred = false;
+        auto sort_in = [&]() {
+            __syncwarp();
+#pragma unroll 1
+            for (int i = 0; i < held; i += 32) {
+                const bool on = i + lane < held;
+                BsBlock<float> more = {on ? s_hold[warp][i + lane] : -INFINITY, on ? s_hold_at[warp][i + lane] : 0x7fffffff};
+                more.sort(lane, true);
+                best.join(more.key, more.at, lane);
+            }
+            __syncwarp();
+            held = 0;
+            bar = fmaxf(bar, __shfl_sync(0xffffffffu, best.key, W - 1));
+        };
         for (int e0 = split * part; e0 < e1; e0 += kBsBatch) {
             // element e0 + 4 tid + 1024 i + j (wide), or e0 + tid + 256 (4 i + j)
             float x[kBsVecs][4];
@@ -216,78 +210,92 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
                     for (int j = 0; j < 4; ++j) x[i][j] = element(i, j) < e1 ? __ldcs(x0 + element(i, j)) : -INFINITY;
                 }
             }
-            float top = -INFINITY;
+            float tops[kBsVecs];
 #pragma unroll
-            for (int i = 0; i < kBsVecs; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) top = bs_max_nan(top, x[i][j]);
-            if (__any_sync(0xffffffffu, !(top < INFINITY))) {  // nothing of the row counts any more
-                bad = true;
-                break;
-            }
+            for (int i = 0; i < kBsVecs; ++i) tops[i] = bs_max_nan(bs_max_nan(x[i][0], x[i][1]), bs_max_nan(x[i][2], x[i][3]));
+            const float top = bs_max_nan(bs_max_nan(tops[0], tops[1]), bs_max_nan(tops[2], tops[3]));
+            bad |= __any_sync(0xffffffffu, !(top < INFINITY)); // nothing of the row counts any more
             if (m == -INFINITY || __any_sync(0xffffffffu, top > m + 20.f)) {
                 float t = top;
 #pragma unroll
                 for (int o = 16; o; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
                 if (m > -INFINITY) sum *= exp((double)m - (double)t);
-                else if (t > -INFINITY) list.bar = bs_nth(top, W - 1, lane);
                 m = t;
-                if (m == -INFINITY) continue;
             }
-            float add = 0.f;
+            if (!barred) {
+                // the bar to begin with: as near to the `beams`-th largest of the threads' maxima as six bisections come
+                barred = true;
+                BsBlock<float> sorted = {top, lane};
+                sorted.sort(lane, false);
+                const float nth = __shfl_sync(0xffffffffu, sorted.key, W - 1);
+                if (lane == 0) s_m[warp] = m, atomicMax(&s_bar, bs_ordered(nth));
+                __syncthreads();
+                float lo = bs_number(s_bar), hi = s_m[0];
 #pragma unroll
-            for (int i = 0; i < kBsVecs; ++i)
+                for (int w = 1; w < kBsWarps; ++w) hi = fmaxf(hi, s_m[w]);
+#pragma unroll 1
+                for (int i = 0; i < 6; ++i) {
+                    const float mid = 0.5f * lo + 0.5f * hi;
+                    (__syncthreads_count(top >= mid) >= W ? lo : hi) = mid;
+                }
+                bar = lo;
+            }
+            if (bad || m == -INFINITY) continue;
+            float add[kBsVecs];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) add += ex2_approx((x[i][j] - m) * 1.4426950408889634f);
-            sum += (double)add;
-            const float shared_bar = bs_number(*(volatile int *)&s_bar);
-            if (shared_bar > list.bar) list.bar = shared_bar, list.bar_at = 0x7fffffff;
-            if (!__any_sync(0xffffffffu, top >= list.bar)) continue;
+            for (int i = 0; i < kBsVecs; ++i) {
+                add[i] = 0.f;
 #pragma unroll
-            for (int i = 0; i < kBsVecs; ++i)
+                for (int j = 0; j < 4; ++j) add[i] += ex2_approx((x[i][j] - m) * 1.4426950408889634f);
+            }
+            sum += (double)((add[0] + add[1]) + (add[2] + add[3]));
+            bar = fmaxf(bar, bs_number(*(volatile int *)&s_bar));
+            if (!__any_sync(0xffffffffu, top >= bar)) continue;
+#pragma unroll
+            for (int i = 0; i < kBsVecs; ++i) {
+                if (!__any_sync(0xffffffffu, tops[i] >= bar)) continue;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const int e = element(i, j);
-                    unsigned who = __ballot_sync(0xffffffffu, list.beats(x[i][j], e));
-                    while (who) {
-                        const int src = __ffs(who) - 1;
-                        who &= who - 1;
-                        const float k = __shfl_sync(0xffffffffu, x[i][j], src);
-                        const int at = e + (WIDE ? 4 : 1) * (src - lane);
-                        if (list.beats(k, at)) list.insert(k, at, lane, W);
+                    const bool on = x[i][j] >= bar && x[i][j] > -INFINITY;
+                    const unsigned who = __ballot_sync(0xffffffffu, on);
+                    if (!who) continue;
+                    const int at = held + __popc(who & ((1u << lane) - 1));
+                    if (on) s_hold[warp][at] = x[i][j], s_hold_at[warp][at] = element(i, j);
+                    held += __popc(who);
+                    if (held > kBsHold) {
+                        sort_in();
+                        if (lane == 0) atomicMax(&s_bar, bs_ordered(bar));
                     }
                 }
-            if (lane == 0) atomicMax(&s_bar, bs_ordered(list.bar));
+            }
         }
+        sort_in();
 #pragma unroll
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        s_key[warp][lane] = list.key;
-        s_at[warp][lane] = list.at;
+        s_hold[warp][lane] = best.key;
+        s_hold_at[warp][lane] = best.at;
         if (lane == 0) s_sum[warp] = sum, s_m[warp] = m, s_bad[warp] = bad;
-        __syncthreads();
+#pragma unroll
+        for (int half = kBsWarps / 2; half; half >>= 1) {
+            __syncthreads();
+            if (warp < half) {
+                best.join(s_hold[warp + half][31 - lane], s_hold_at[warp + half][31 - lane], lane);
+                s_hold[warp][lane] = best.key;
+                s_hold_at[warp][lane] = best.at;
+            }
+        }
         if (warp == 0) {
             BsPart &p = parts[(size_t)row * splits + split];
-            for (int w = 1; w < kBsWarps; ++w) {
-                const float k = s_key[w][lane];
-                const int at = s_at[w][lane];
-                unsigned who = __ballot_sync(0xffffffffu, lane < W && list.beats(k, at));
-                while (who) {
-                    const int src = __ffs(who) - 1;
-                    who &= who - 1;
-                    const float kk = __shfl_sync(0xffffffffu, k, src);
-                    const int aa = __shfl_sync(0xffffffffu, at, src);
-                    if (list.beats(kk, aa)) list.insert(kk, aa, lane, W);
-                }
-            }
-            p.best[lane] = list.key;
-            p.at[lane] = list.at;
+            p.best[lane] = best.key;
+            p.at[lane] = best.at;
             float top = -INFINITY;
             bool any_bad = false;
             for (int w = 0; w < kBsWarps; ++w) top = fmaxf(top, s_m[w]), any_bad |= s_bad[w] != 0;
-            double total = 0.0;                                // (the same in every lane)
-            for (int w = 0; w < kBsWarps; ++w)
-                if (s_m[w] > -INFINITY) total += s_sum[w] * exp((double)s_m[w] - (double)top);
-            if (lane == 0) p.sum = total, p.m = top, p.bad = any_bad;
+            double mine = 0.0;
+            if (lane < kBsWarps && s_m[lane] > -INFINITY) mine = s_sum[lane] * exp((double)s_m[lane] - (double)top);
+#pragma unroll
+            for (int o = kBsWarps / 2; o; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+            if (lane == 0) p.sum = mine, p.m = top, p.bad = any_bad;
             __threadfence();
         }
     }
@@ -302,8 +310,7 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
     __syncthreads();
     if (!s_last) return;
     __threadfence();
-
-    beam_finish(a, splits, parts, group, s_rank, s_at);
+    beam_finish(a, splits, parts, group);
 }
 
 }  // namespace
