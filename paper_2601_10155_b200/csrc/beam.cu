@@ -4,8 +4,8 @@
 //   - sum exp(x - m) against a reference m that it takes from its first logits and seldom moves: fp32 exponentials, their sums
 //     fp64, so that the ranks of different beams are compared to 1e-8;
 //   - its best 32 logits (a beam's candidates rank as its logits do), sorted over the lanes.  What reaches a bar is collected in
-//     shared memory and sorted in 32 at a time (a bitonic sort and a merge).  The CTA's first 4096 logits give the bar to begin
-//     with, near the `beams`-th largest of its threads' maxima; then few logits reach it.
+//     shared memory and sorted in 32 at a time (a bitonic sort and a merge).  The bar comes from the lanes' largest logits so far
+//     and is renewed at the batches 1, 2, 4, ...: few logits reach it.
 // Rows are read in the same order whatever their alignment (16-byte loads where all rows lie on such borders, else 4-byte ones):
 // beams with equal logits and scores get equal ranks, and the lower one goes first.
 // The CTA's warps join in shared memory.  The last CTA of a group to finish (a counter, no waiting) joins the parts, ranks
@@ -57,19 +57,33 @@ struct BsBlock {
     }
 };
 
-__device__ __forceinline__ float bs_max_nan(float a, float b)   // NaN if either is
+__device__ __forceinline__ float bs_max_nan(float a, float b, float c)          // NaN if one of them is
 {
     float d;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// whole numbers in the order of floats
-__device__ __forceinline__ int bs_ordered(float x)
+// exp(x - m), exp(y - m), added to sum: the differences and products two at a time
+__device__ __forceinline__ void bs_add_exp2(float2 &sum, float x, float y, float minus_m)
 {
-    const int i = __float_as_int(x);
-    return i < 0 ? i ^ 0x7fffffff : i;
+    float u, v;
+    asm("{\n.reg .b64 a, b;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %4};\nadd.rn.f32x2 a, a, b;\nmov.b64 b, {%5, %5};\nmul.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}"
+        : "=f"(u), "=f"(v) : "f"(x), "f"(y), "f"(minus_m), "f"(1.4426950408889634f));
+    u = ex2_approx(u), v = ex2_approx(v);
+    asm("{\n.reg .b64 a, b;\nmov.b64 a, {%0, %1};\nmov.b64 b, {%2, %3};\nadd.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}" : "+f"(sum.x), "+f"(sum.y) : "f"(u), "f"(v));
 }
-__device__ __forceinline__ float bs_number(int i) { return __int_as_float(i < 0 ? i ^ 0x7fffffff : i); }
+// the (n + 1)-th largest of the lanes' numbers
+__device__ __forceinline__ float bs_nth(float v, int n, int lane)
+{
+#pragma unroll
+    for (int k = 2; k <= 32; k <<= 1)
+#pragma unroll
+        for (int j = k >> 1; j; j >>= 1) {
+            const float o = __shfl_xor_sync(0xffffffffu, v, j);
+            v = ((lane & k) == 0) == ((lane & j) == 0) ? fmaxf(v, o) : fminf(v, o);
+        }
+    return __shfl_sync(0xffffffffu, v, n);
+}
 
 // The group's parts joined and ranked, its beams moved.
 __device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const BsPart *__restrict__ parts, int group)
@@ -97,24 +111,46 @@ __device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const Bs
         float top = 0.f;
         if (counts && !s_fin[w]) {
             const BsPart *p = parts + (size_t)(g0 + w) * splits;
-            top = -INFINITY;
-            bool bad = false;
-            for (int i = lane; i < splits; i += 32) top = fmaxf(top, __ldcg(&p[i].m)), bad |= __ldcg(&p[i].bad) != 0;
+            constexpr int kAhead = 8;                          // a part's logits stand first to last: read last to first
+            float x[kAhead];
+            int at[kAhead];
+            auto fetch = [&](int i0) {
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) {
+                    const BsPart &q = p[min(i0 + i, splits - 1)];
+                    x[i] = __ldcg(&q.best[31 - lane]);
+                    at[i] = __ldcg(&q.at[31 - lane]);
+                }
+            };
+            const BsPart &q = p[min(lane, splits - 1)];        // (up to 32 parts: their sums are asked for at once)
+            const float m0 = __ldcg(&q.m);
+            const double sum0 = __ldcg(&q.sum);
+            const int bad0 = __ldcg(&q.bad);
+            fetch(0);
+            top = m0;
+            bool bad = bad0 != 0;
+            for (int i = lane + 32; i < splits; i += 32) top = fmaxf(top, __ldcg(&p[i].m)), bad |= __ldcg(&p[i].bad) != 0;
 #pragma unroll
             for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
             bad = __any_sync(0xffffffffu, bad) || top == -INFINITY;
             if (!bad) {
                 double total = 0.0;
-                for (int i = lane; i < splits; i += 32)
+                if (lane < splits && m0 > -INFINITY) total = sum0 * exp((double)m0 - (double)top);
+                for (int i = lane + 32; i < splits; i += 32)
                     if (__ldcg(&p[i].m) > -INFINITY) total += __ldcg(&p[i].sum) * exp((double)__ldcg(&p[i].m) - (double)top);
 #pragma unroll
                 for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
                 base = (double)sc - log(total);
-                for (int i = 0; i < splits; ++i) {             // a part's logits stand first to last: read last to first
-                    const float x = __ldcg(&p[i].best[31 - lane]);
-                    const int at = __ldcg(&p[i].at[31 - lane]);
-                    const bool on = x > -INFINITY;
-                    best.join(on ? (base + ((double)x - (double)top)) / norm : -INFINITY, on ? w * a.vocab + at : 0x7fffffff, lane);
+#pragma unroll 1
+                for (int i0 = 0; i0 < splits; i0 += kAhead) {
+                    if (i0) fetch(i0);
+#pragma unroll
+                    for (int i = 0; i < kAhead; ++i) {
+                        const bool on = x[i] > -INFINITY && i0 + i < splits;
+                        const double rank = (base + ((double)x[i] - (double)top)) / norm, bar = __shfl_sync(0xffffffffu, best.key, W - 1);
+                        if (__any_sync(0xffffffffu, on && rank >= bar))
+                            best.join(on ? rank : -INFINITY, on ? w * a.vocab + at[i] : 0x7fffffff, lane);
+                    }
                 }
             }
         } else if (counts) {
@@ -159,61 +195,76 @@ __device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const Bs
     }
 }
 
+// the candidates that a warp holds among its best (out of line: it is called from several places and would fill the
+// instruction cache)
+__device__ __noinline__ BsBlock<float> beam_sort_in(BsBlock<float> best, const float *hold, const int *hold_at, int held)
+{
+    const int lane = threadIdx.x & 31;
+    __syncwarp();
+#pragma unroll 1
+    for (int i = 0; i < held; i += 32) {
+        const bool on = i + lane < held;
+        BsBlock<float> more = {on ? hold[i + lane] : -INFINITY, on ? hold_at[i + lane] : 0x7fffffff};
+        more.sort(lane, true);
+        best.join(more.key, more.at, lane);
+    }
+    __syncwarp();
+    return best;
+}
+
 template <bool WIDE>
 __global__ void __launch_bounds__(kBsThreads, 4)
 beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsPart *__restrict__ parts, unsigned *__restrict__ tickets)
 {
-    __shared__ float s_hold[kBsWarps][kBsHold + 32];           // a warp's candidates; in the end the warps' best
-    __shared__ int s_hold_at[kBsWarps][kBsHold + 32];
+    __shared__ float s_hold[kBsWarps][kBsHold + 128];           // a warp's candidates; in the end the warps' best
+    __shared__ int s_hold_at[kBsWarps][kBsHold + 128];
     __shared__ double s_sum[kBsWarps];
     __shared__ float s_m[kBsWarps];
-    __shared__ int s_bad[kBsWarps], s_last, s_bar;             // s_bar: a logit that `beams` of the part reach, as bs_ordered
+    __shared__ int s_bad[kBsWarps], s_last;
+    __shared__ __align__(16) float s_bars[kBsWarps];           // each a logit that `share` of the warp's reach
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, W = a.beams;
     const int row = blockIdx.x / splits, split = blockIdx.x % splits, group = row / W;
     const float score = a.scores[row];
     const bool live = a.finished[row] == 0 && score > -INFINITY && score < INFINITY;
 
     if (live) {                                                // (the same for the whole CTA)
-        if (tid == 0) s_bar = bs_ordered(-INFINITY);
-        __syncthreads();
+        const int share = (W + kBsWarps - 1) / kBsWarps;
         const float *x0 = a.logits + (long long)row * a.stride;
         const int e1 = min((split + 1) * part, a.vocab);
         BsBlock<float> best = {-INFINITY, 0x7fffffff};
         float bar = -INFINITY, m = -INFINITY;
         int held = 0;
         double sum = 0.0;
-        bool bad = false, barred = false;
+        float lane_top = -INFINITY;
+        int batch = 0;
+        bool bad = false;
         auto sort_in = [&]() {
-            __syncwarp();
-#pragma unroll 1
-            for (int i = 0; i < held; i += 32) {
-                const bool on = i + lane < held;
-                BsBlock<float> more = {on ? s_hold[warp][i + lane] : -INFINITY, on ? s_hold_at[warp][i + lane] : 0x7fffffff};
-                more.sort(lane, true);
-                best.join(more.key, more.at, lane);
-            }
-            __syncwarp();
+            best = beam_sort_in(best, s_hold[warp], s_hold_at[warp], held);
             held = 0;
             bar = fmaxf(bar, __shfl_sync(0xffffffffu, best.key, W - 1));
         };
-        for (int e0 = split * part; e0 < e1; e0 += kBsBatch) {
-            // element e0 + 4 tid + 1024 i + j (wide), or e0 + tid + 256 (4 i + j)
-            float x[kBsVecs][4];
-            auto element = [&](int i, int j) { return WIDE ? e0 + 4 * (i * kBsThreads + tid) + j : e0 + (4 * i + j) * kBsThreads + tid; };
+        // element of a batch: e0 + 4 tid + 1024 i + j (wide), or e0 + tid + 256 (4 i + j)
+        auto element = [&](int e0, int i, int j) { return WIDE ? e0 + 4 * (i * kBsThreads + tid) + j : e0 + (4 * i + j) * kBsThreads + tid; };
+        auto fetch = [&](float (&x)[kBsVecs][4], int e0) {
 #pragma unroll
             for (int i = 0; i < kBsVecs; ++i) {
-                if (WIDE && element(i, 3) < e1) {
-                    const float4 y = __ldcs(reinterpret_cast<const float4 *>(x0 + element(i, 0)));
+                if (WIDE && element(e0, i, 3) < e1) {
+                    const float4 y = __ldcs(reinterpret_cast<const float4 *>(x0 + element(e0, i, 0)));
                     x[i][0] = y.x, x[i][1] = y.y, x[i][2] = y.z, x[i][3] = y.w;
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x[i][j] = element(i, j) < e1 ? __ldcs(x0 + element(i, j)) : -INFINITY;
+                    for (int j = 0; j < 4; ++j) x[i][j] = element(e0, i, j) < e1 ? __ldcs(x0 + element(e0, i, j)) : -INFINITY;
                 }
             }
+        };
+#pragma unroll 1
+        for (int e0 = split * part; e0 < e1; e0 += kBsBatch) {
+            float x[kBsVecs][4];
+            fetch(x, e0);
             float tops[kBsVecs];
 #pragma unroll
-            for (int i = 0; i < kBsVecs; ++i) tops[i] = bs_max_nan(bs_max_nan(x[i][0], x[i][1]), bs_max_nan(x[i][2], x[i][3]));
-            const float top = bs_max_nan(bs_max_nan(tops[0], tops[1]), bs_max_nan(tops[2], tops[3]));
+            for (int i = 0; i < kBsVecs; ++i) tops[i] = bs_max_nan(x[i][0], x[i][1], bs_max_nan(x[i][2], x[i][3], x[i][3]));
+            const float top = bs_max_nan(tops[0], tops[1], bs_max_nan(tops[2], tops[3], tops[3]));
             bad |= __any_sync(0xffffffffu, !(top < INFINITY)); // nothing of the row counts any more
             if (m == -INFINITY || __any_sync(0xffffffffu, top > m + 20.f)) {
                 float t = top;
@@ -222,34 +273,27 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
                 if (m > -INFINITY) sum *= exp((double)m - (double)t);
                 m = t;
             }
-            if (!barred) {
-                // the bar to begin with: as near to the `beams`-th largest of the threads' maxima as six bisections come
-                barred = true;
-                BsBlock<float> sorted = {top, lane};
-                sorted.sort(lane, false);
-                const float nth = __shfl_sync(0xffffffffu, sorted.key, W - 1);
-                if (lane == 0) s_m[warp] = m, atomicMax(&s_bar, bs_ordered(nth));
-                __syncthreads();
-                float lo = bs_number(s_bar), hi = s_m[0];
+            // `share` logits of every warp reach the least of the warps' bars, so the beams' last does; renewed at batches 1, 2,
+            // 4, ... (what another warp has not renewed yet holds as well)
+            lane_top = fmaxf(lane_top, top);
+            ++batch;
+            if ((batch & (batch - 1)) == 0) {
+                const float nth = bs_nth(lane_top, share - 1, lane);
+                if (lane == 0) *(volatile float *)&s_bars[warp] = nth;
+                if (batch == 1) __syncthreads();
+                float least = INFINITY;
 #pragma unroll
-                for (int w = 1; w < kBsWarps; ++w) hi = fmaxf(hi, s_m[w]);
-#pragma unroll 1
-                for (int i = 0; i < 6; ++i) {
-                    const float mid = 0.5f * lo + 0.5f * hi;
-                    (__syncthreads_count(top >= mid) >= W ? lo : hi) = mid;
-                }
-                bar = lo;
+                for (int w = 0; w < kBsWarps; ++w) least = fminf(least, *(volatile float *)&s_bars[w]);
+                bar = fmaxf(bar, least);
             }
             if (bad || m == -INFINITY) continue;
-            float add[kBsVecs];
+            float2 add[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
             for (int i = 0; i < kBsVecs; ++i) {
-                add[i] = 0.f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) add[i] += ex2_approx((x[i][j] - m) * 1.4426950408889634f);
+                bs_add_exp2(add[0], x[i][0], x[i][1], -m);
+                bs_add_exp2(add[1], x[i][2], x[i][3], -m);
             }
-            sum += (double)((add[0] + add[1]) + (add[2] + add[3]));
-            bar = fmaxf(bar, bs_number(*(volatile int *)&s_bar));
+            sum += (double)((add[0].x + add[0].y) + (add[1].x + add[1].y));
             if (!__any_sync(0xffffffffu, top >= bar)) continue;
 #pragma unroll
             for (int i = 0; i < kBsVecs; ++i) {
@@ -260,13 +304,10 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
                     const unsigned who = __ballot_sync(0xffffffffu, on);
                     if (!who) continue;
                     const int at = held + __popc(who & ((1u << lane) - 1));
-                    if (on) s_hold[warp][at] = x[i][j], s_hold_at[warp][at] = element(i, j);
+                    if (on) s_hold[warp][at] = x[i][j], s_hold_at[warp][at] = element(e0, i, j);
                     held += __popc(who);
-                    if (held > kBsHold) {
-                        sort_in();
-                        if (lane == 0) atomicMax(&s_bar, bs_ordered(bar));
-                    }
                 }
+                if (held > kBsHold) sort_in();
             }
         }
         sort_in();
@@ -318,11 +359,17 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
 lookat_status launch_beam_select(Ctx *ctx, const BeamArgs &a)
 {
     const long long rows = (long long)a.groups * a.beams;
-    // parts of a row: enough CTAs to fill the GPU a few times over, whole batches each
+    // Parts of a row, whole batches each: as many as make the least of (waves of CTAs) x (batches of a part + 6), what a CTA does
+    // besides its batches taking about as long as 6 of them.
     const int batches = (a.vocab + kBsBatch - 1) / kBsBatch;
-    long long splits = (4ll * 4 * ctx->sm_count + rows - 1) / rows;
-    if (splits > batches) splits = batches;
-    const int per = (int)((batches + splits - 1) / splits);
+    const long long slots = 4ll * ctx->sm_count;
+    long long splits = 1, least = 0;
+    int per = batches;
+    for (int s = 1; s <= batches && s <= 64; ++s) {
+        const int each = (batches + s - 1) / s;
+        const long long cost = (rows * s + slots - 1) / slots * (each + 6);
+        if (s == 1 || cost < least) least = cost, per = each;
+    }
     splits = (batches + per - 1) / per;
     lookat_status st = workspace(ctx, ctx->beam_parts, (size_t)(rows * splits) * sizeof(BsPart), false, "beam_select");
     if (st != LOOKAT_OK) return st;
