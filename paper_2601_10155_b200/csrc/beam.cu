@@ -72,8 +72,8 @@ __device__ __forceinline__ void bs_add_exp2(float2 &sum, float x, float y, float
     u = ex2_approx(u), v = ex2_approx(v);
     asm("{\n.reg .b64 a, b;\nmov.b64 a, {%0, %1};\nmov.b64 b, {%2, %3};\nadd.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}" : "+f"(sum.x), "+f"(sum.y) : "f"(u), "f"(v));
 }
-// the (n + 1)-th largest of the lanes' numbers
-__device__ __forceinline__ float bs_nth(float v, int n, int lane)
+// the lanes' numbers in falling order
+__device__ __forceinline__ float bs_sorted(float v, int lane)
 {
 #pragma unroll
     for (int k = 2; k <= 32; k <<= 1)
@@ -82,117 +82,135 @@ __device__ __forceinline__ float bs_nth(float v, int n, int lane)
             const float o = __shfl_xor_sync(0xffffffffu, v, j);
             v = ((lane & k) == 0) == ((lane & j) == 0) ? fmaxf(v, o) : fminf(v, o);
         }
-    return __shfl_sync(0xffffffffu, v, n);
+    return v;
+}
+
+// What a group's beams were before the call, and where its rows' candidates stand.
+struct BsGroup {
+    float score[kBsMost];
+    int len[kBsMost], fin[kBsMost];
+    double base[kBsMost], norm[kBsMost], rank[kBsWarps][kBsMost];                   // rank = (base + (x - m)) / norm
+    float m[kBsMost];
+    int at[kBsWarps][kBsMost], parent[kBsMost], slot[kBsMost], token[kBsMost];
+};
+
+// Columns of the histories, of up to MOST beams each: all are read before the first is written.
+template <int MOST, class T>
+__device__ __forceinline__ void beam_move(T *rows, int columns, int beams, const int *parent)
+{
+    for (int c = threadIdx.x; c < columns; c += kBsThreads) {
+        T y[MOST];
+#pragma unroll
+        for (int w = 0; w < MOST; ++w)
+            if (w < beams) y[w] = rows[(size_t)parent[w] * columns + c];
+#pragma unroll
+        for (int w = 0; w < MOST; ++w)
+            if (w < beams) rows[(size_t)w * columns + c] = y[w];
+    }
 }
 
 // The group's parts joined and ranked, its beams moved.
-__device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const BsPart *__restrict__ parts, int group)
+__device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const BsPart *__restrict__ parts, int group, BsGroup &g)
 {
-    __shared__ double s_rank[kBsWarps][kBsMost];
-    __shared__ int s_at[kBsWarps][kBsMost];
-    __shared__ double s_base[kBsMost];                         // score = base + (x - m)
-    __shared__ float s_top[kBsMost], s_score[kBsMost];
-    __shared__ int s_len[kBsMost], s_fin[kBsMost], s_parent[kBsMost], s_slot[kBsMost], s_token[kBsMost];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, W = a.beams;
     const int g0 = group * W;
-    if (tid < W) {
-        s_score[tid] = a.scores[g0 + tid];
-        s_len[tid] = a.lengths[g0 + tid];
-        s_fin[tid] = a.finished[g0 + tid] != 0;
-    }
-    __syncthreads();
-    BsBlock<double> best = {-INFINITY, 0x7fffffff};
+    const BsPart *const p0 = parts + (size_t)g0 * splits;
+    // ---- the rows' sums ----
     for (int w = warp; w < W; w += kBsWarps) {
-        const float sc = s_score[w];
+        const float sc = g.score[w];
         const bool counts = sc > -INFINITY && sc < INFINITY;
-        const int grown = max(s_len[w] + (s_fin[w] ? 0 : 1), 1);
-        const double norm = a.penalty == 0.0 ? 1.0 : pow((double)grown, a.penalty);
-        double base = sc;
+        const int grown = max(g.len[w] + (g.fin[w] ? 0 : 1), 1);
+        double base = counts ? (double)sc : -INFINITY;
         float top = 0.f;
-        if (counts && !s_fin[w]) {
-            const BsPart *p = parts + (size_t)(g0 + w) * splits;
-            constexpr int kAhead = 8;                          // a part's logits stand first to last: read last to first
-            float x[kAhead];
-            int at[kAhead];
-            auto fetch = [&](int i0) {
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) {
-                    const BsPart &q = p[min(i0 + i, splits - 1)];
-                    x[i] = __ldcg(&q.best[31 - lane]);
-                    at[i] = __ldcg(&q.at[31 - lane]);
-                }
-            };
-            const BsPart &q = p[min(lane, splits - 1)];        // (up to 32 parts: their sums are asked for at once)
-            const float m0 = __ldcg(&q.m);
+        if (counts && !g.fin[w]) {
+            const BsPart *p = p0 + (size_t)w * splits, &q = p[min(lane, splits - 1)];
+            const float m0 = __ldcg(&q.m);                     // (up to 32 parts: all asked for at once)
             const double sum0 = __ldcg(&q.sum);
-            const int bad0 = __ldcg(&q.bad);
-            fetch(0);
+            bool bad = __ldcg(&q.bad) != 0;
             top = m0;
-            bool bad = bad0 != 0;
             for (int i = lane + 32; i < splits; i += 32) top = fmaxf(top, __ldcg(&p[i].m)), bad |= __ldcg(&p[i].bad) != 0;
 #pragma unroll
             for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
             bad = __any_sync(0xffffffffu, bad) || top == -INFINITY;
-            if (!bad) {
-                double total = 0.0;
-                if (lane < splits && m0 > -INFINITY) total = sum0 * exp((double)m0 - (double)top);
-                for (int i = lane + 32; i < splits; i += 32)
-                    if (__ldcg(&p[i].m) > -INFINITY) total += __ldcg(&p[i].sum) * exp((double)__ldcg(&p[i].m) - (double)top);
+            double total = 0.0;
+            if (lane < splits && m0 > -INFINITY) total = sum0 * exp((double)m0 - (double)top);
+            for (int i = lane + 32; i < splits; i += 32)
+                if (__ldcg(&p[i].m) > -INFINITY) total += __ldcg(&p[i].sum) * exp((double)__ldcg(&p[i].m) - (double)top);
 #pragma unroll
-                for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-                base = (double)sc - log(total);
-#pragma unroll 1
-                for (int i0 = 0; i0 < splits; i0 += kAhead) {
-                    if (i0) fetch(i0);
-#pragma unroll
-                    for (int i = 0; i < kAhead; ++i) {
-                        const bool on = x[i] > -INFINITY && i0 + i < splits;
-                        const double rank = (base + ((double)x[i] - (double)top)) / norm, bar = __shfl_sync(0xffffffffu, best.key, W - 1);
-                        if (__any_sync(0xffffffffu, on && rank >= bar))
-                            best.join(on ? rank : -INFINITY, on ? w * a.vocab + at[i] : 0x7fffffff, lane);
-                    }
-                }
-            }
-        } else if (counts) {
-            best.join(lane == 31 ? (double)sc / norm : -INFINITY, lane == 31 ? w * a.vocab + max(a.eos, 0) : 0x7fffffff, lane);
+            for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+            base = bad ? -INFINITY : base - log(total);
         }
-        if (lane == 0) s_base[w] = base, s_top[w] = top;
+        if (lane == 0) g.base[w] = base, g.norm[w] = a.penalty == 0.0 ? 1.0 : pow((double)grown, a.penalty), g.m[w] = top;
     }
-    s_rank[warp][lane] = best.key;
-    s_at[warp][lane] = best.at;
     __syncthreads();
-    if (warp == 0) {
-        for (int w = 1; w < min(W, kBsWarps); ++w) best.join(s_rank[w][31 - lane], s_at[w][31 - lane], lane);
-        if (lane < W) {
-            const bool there = best.key > -INFINITY;
-            const int parent = there ? best.at / a.vocab : lane, token = there ? best.at % a.vocab : max(a.eos, 0);
-            const bool grows = there && !s_fin[parent];
-            float now = -INFINITY;
-            if (there) now = s_fin[parent] ? s_score[parent] : (float)(s_base[parent] + ((double)a.logits[(long long)(g0 + parent) * a.stride + token] - (double)s_top[parent]));
-            const int was = s_len[parent];
-            a.scores[g0 + lane] = now;
-            a.lengths[g0 + lane] = was + (grows ? 1 : 0);
-            a.finished[g0 + lane] = s_fin[parent] || (grows && token == a.eos);
-            a.next_ids[g0 + lane] = token;
-            a.parents[g0 + lane] = g0 + parent;
-            s_parent[lane] = parent;
-            s_slot[lane] = grows ? was : -1;
-            s_token[lane] = token;
+    // ---- the best of all parts' candidates, which stand first to last there: read last to first ----
+    BsBlock<double> best = {-INFINITY, 0x7fffffff};
+    constexpr int kAhead = 4;
+#pragma unroll 1
+    for (int i0 = warp; i0 < W * splits; i0 += kBsWarps * kAhead) {
+        float x[kAhead];
+        int at[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const BsPart &q = p0[min(i0 + i * kBsWarps, W * splits - 1)];
+            x[i] = __ldcg(&q.best[31 - lane]);
+            at[i] = __ldcg(&q.at[31 - lane]);
         }
+#pragma unroll 1
+        for (int i = 0; i < kAhead; ++i) {
+            const int item = i0 + i * kBsWarps, w = min(item, W * splits - 1) / splits;
+            const float xi = i == 0 ? x[0] : i == 1 ? x[1] : i == 2 ? x[2] : x[3];
+            const int ai = i == 0 ? at[0] : i == 1 ? at[1] : i == 2 ? at[2] : at[3];
+            const double base = g.base[w], norm = g.norm[w];
+            bool on = item < W * splits && base > -INFINITY;
+            double score = base + ((double)xi - (double)g.m[w]);
+            int where = w * a.vocab + ai;
+            if (g.fin[w]) {                                    // itself, once
+                on = on && item == w * splits && lane == 31;
+                score = base;
+                where = w * a.vocab + max(a.eos, 0);
+            } else {
+                on = on && xi > -INFINITY;
+            }
+            const double rank = !on ? -INFINITY : norm == 1.0 ? score : score / norm, bar = __shfl_sync(0xffffffffu, best.key, W - 1);
+            if (__any_sync(0xffffffffu, on && rank >= bar)) best.join(rank, on ? where : 0x7fffffff, lane);
+        }
+    }
+    g.rank[warp][lane] = best.key;
+    g.at[warp][lane] = best.at;
+#pragma unroll 1
+    for (int half = kBsWarps / 2; half; half >>= 1) {
+        __syncthreads();
+        if (warp < half) {
+            best.join(g.rank[warp + half][31 - lane], g.at[warp + half][31 - lane], lane);
+            g.rank[warp][lane] = best.key;
+            g.at[warp][lane] = best.at;
+        }
+    }
+    if (warp == 0 && lane < W) {
+        const bool there = best.key > -INFINITY;
+        const int parent = there ? best.at / a.vocab : lane, token = there ? best.at % a.vocab : max(a.eos, 0);
+        const bool grows = there && !g.fin[parent];
+        const int was = g.len[parent];
+        a.scores[g0 + lane] = !there ? -INFINITY : g.fin[parent] ? g.score[parent] : (float)(best.key * g.norm[parent]);
+        a.lengths[g0 + lane] = was + (grows ? 1 : 0);
+        a.finished[g0 + lane] = g.fin[parent] || (grows && token == a.eos);
+        a.next_ids[g0 + lane] = token;
+        a.parents[g0 + lane] = g0 + parent;
+        g.parent[lane] = parent;
+        g.slot[lane] = grows && was >= 0 && was < a.max_len ? was : -1;
+        g.token[lane] = token;
     }
     if (!a.max_len) return;
     __syncthreads();
-    // ---- the histories, a column per thread: all beams' numbers are read before the first is written ----
+    // ---- the histories ----
     int32_t *const tokens = a.tokens + (size_t)g0 * a.max_len;
-    for (int c = tid; c < a.max_len; c += kBsThreads) {
-        int32_t y[kBsMost];
-#pragma unroll
-        for (int w = 0; w < kBsMost; ++w)
-            if (w < W) y[w] = s_slot[w] == c ? s_token[w] : tokens[(size_t)s_parent[w] * a.max_len + c];
-#pragma unroll
-        for (int w = 0; w < kBsMost; ++w)
-            if (w < W) tokens[(size_t)w * a.max_len + c] = y[w];
-    }
+    if (W <= 8 && a.max_len % 4 == 0 && (reinterpret_cast<uintptr_t>(a.tokens) & 15) == 0)
+        beam_move<8>(reinterpret_cast<int4 *>(tokens), a.max_len / 4, W, g.parent);
+    else
+        beam_move<kBsMost>(tokens, a.max_len, W, g.parent);
+    __syncthreads();
+    if (tid < W && g.slot[tid] >= 0) tokens[(size_t)tid * a.max_len + g.slot[tid]] = g.token[tid];
 }
 
 // the candidates that a warp holds among its best (out of line: it is called from several places and would fill the
@@ -216,8 +234,11 @@ template <bool WIDE>
 __global__ void __launch_bounds__(kBsThreads, 4)
 beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsPart *__restrict__ parts, unsigned *__restrict__ tickets)
 {
-    __shared__ float s_hold[kBsWarps][kBsHold + 128];           // a warp's candidates; in the end the warps' best
+    __shared__ float s_hold[kBsWarps][kBsHold + 128];           // a warp's candidates
     __shared__ int s_hold_at[kBsWarps][kBsHold + 128];
+    __shared__ __align__(8) float2 s_all[kBsThreads];          // all warps' last candidates: logit, element
+    __shared__ int s_count[kBsWarps];
+    __shared__ BsGroup s_group;
     __shared__ double s_sum[kBsWarps];
     __shared__ float s_m[kBsWarps];
     __shared__ int s_bad[kBsWarps], s_last;
@@ -227,6 +248,11 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
     const float score = a.scores[row];
     const bool live = a.finished[row] == 0 && score > -INFINITY && score < INFINITY;
 
+    if (tid < W) {                                             // (for the last CTA)
+        s_group.score[tid] = a.scores[group * W + tid];
+        s_group.len[tid] = a.lengths[group * W + tid];
+        s_group.fin[tid] = a.finished[group * W + tid] != 0;
+    }
     if (live) {                                                // (the same for the whole CTA)
         const int share = (W + kBsWarps - 1) / kBsWarps;
         const float *x0 = a.logits + (long long)row * a.stride;
@@ -237,8 +263,9 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
         double sum = 0.0;
         float lane_top = -INFINITY;
         int batch = 0;
-        bool bad = false;
+        bool bad = false, sorted = false;
         auto sort_in = [&]() {
+            sorted = true;
             best = beam_sort_in(best, s_hold[warp], s_hold_at[warp], held);
             held = 0;
             bar = fmaxf(bar, __shfl_sync(0xffffffffu, best.key, W - 1));
@@ -266,25 +293,28 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
             for (int i = 0; i < kBsVecs; ++i) tops[i] = bs_max_nan(x[i][0], x[i][1], bs_max_nan(x[i][2], x[i][3], x[i][3]));
             const float top = bs_max_nan(tops[0], tops[1], bs_max_nan(tops[2], tops[3], tops[3]));
             bad |= __any_sync(0xffffffffu, !(top < INFINITY)); // nothing of the row counts any more
-            if (m == -INFINITY || __any_sync(0xffffffffu, top > m + 20.f)) {
-                float t = top;
-#pragma unroll
-                for (int o = 16; o; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, o));
-                if (m > -INFINITY) sum *= exp((double)m - (double)t);
-                m = t;
-            }
             // `share` logits of every warp reach the least of the warps' bars, so the beams' last does; renewed at batches 1, 2,
             // 4, ... (what another warp has not renewed yet holds as well)
             lane_top = fmaxf(lane_top, top);
             ++batch;
+            float most = m;
             if ((batch & (batch - 1)) == 0) {
-                const float nth = bs_nth(lane_top, share - 1, lane);
+                const float in_order = bs_sorted(lane_top, lane), nth = __shfl_sync(0xffffffffu, in_order, share - 1);
+                most = __shfl_sync(0xffffffffu, in_order, 0);
                 if (lane == 0) *(volatile float *)&s_bars[warp] = nth;
                 if (batch == 1) __syncthreads();
                 float least = INFINITY;
 #pragma unroll
                 for (int w = 0; w < kBsWarps; ++w) least = fminf(least, *(volatile float *)&s_bars[w]);
                 bar = fmaxf(bar, least);
+            } else if (__any_sync(0xffffffffu, top > m + 20.f)) {
+                most = lane_top;
+#pragma unroll
+                for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+            }
+            if (most > m + 20.f || m == -INFINITY) {
+                if (m > -INFINITY) sum *= exp((double)m - (double)most);
+                m = most;
             }
             if (bad || m == -INFINITY) continue;
             float2 add[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
@@ -310,25 +340,42 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
                 if (held > kBsHold) sort_in();
             }
         }
-        sort_in();
+        // ---- the part's best: a warp brings what it holds, or its best if it has sorted, and each finds its place by counting ----
+        if (sorted || held > 32) {
+            sort_in();
+            held = W;
+        } else {
+            __syncwarp();
+            if (lane < held) best.key = s_hold[warp][lane], best.at = s_hold_at[warp][lane];
+        }
 #pragma unroll
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        s_hold[warp][lane] = best.key;
-        s_hold_at[warp][lane] = best.at;
-        if (lane == 0) s_sum[warp] = sum, s_m[warp] = m, s_bad[warp] = bad;
+        if (lane == 0) s_sum[warp] = sum, s_m[warp] = m, s_bad[warp] = bad, s_count[warp] = held;
+        __syncthreads();
+        int first = 0, n = 0;
 #pragma unroll
-        for (int half = kBsWarps / 2; half; half >>= 1) {
-            __syncthreads();
-            if (warp < half) {
-                best.join(s_hold[warp + half][31 - lane], s_hold_at[warp + half][31 - lane], lane);
-                s_hold[warp][lane] = best.key;
-                s_hold_at[warp][lane] = best.at;
-            }
+        for (int w = 0; w < kBsWarps; ++w) {
+            if (w == warp) first = n;
+            n += s_count[w];
         }
+        if (lane < held) s_all[first + lane] = make_float2(best.key, __int_as_float(best.at));
+        __syncthreads();
+        BsPart &p = parts[(size_t)row * splits + split];
+        if (tid < n) {
+            const float2 mine = s_all[tid];
+            const int at = __float_as_int(mine.y);
+            int place = 0;
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) {
+                const float2 o = s_all[i];
+                place += o.x > mine.x || (o.x == mine.x && __float_as_int(o.y) < at);
+            }
+            // (a warp's list that is not full ends with places that hold nothing)
+            if (place < kBsMost && mine.x > -INFINITY) p.best[place] = mine.x, p.at[place] = at;
+        }
+        const int real = __syncthreads_count(tid < n && s_all[min(tid, n - 1)].x > -INFINITY);
+        if (tid >= real && tid < kBsMost) p.best[tid] = -INFINITY, p.at[tid] = 0x7fffffff;
         if (warp == 0) {
-            BsPart &p = parts[(size_t)row * splits + split];
-            p.best[lane] = best.key;
-            p.at[lane] = best.at;
             float top = -INFINITY;
             bool any_bad = false;
             for (int w = 0; w < kBsWarps; ++w) top = fmaxf(top, s_m[w]), any_bad |= s_bad[w] != 0;
@@ -337,8 +384,8 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
 #pragma unroll
             for (int o = kBsWarps / 2; o; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
             if (lane == 0) p.sum = mine, p.m = top, p.bad = any_bad;
-            __threadfence();
         }
+        __threadfence();
     }
 
     // ---- the group's last CTA goes on ----
@@ -351,7 +398,7 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
     __syncthreads();
     if (!s_last) return;
     __threadfence();
-    beam_finish(a, splits, parts, group);
+    beam_finish(a, splits, parts, group, s_group);
 }
 
 }  // namespace
