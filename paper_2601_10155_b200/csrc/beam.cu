@@ -18,7 +18,8 @@ namespace {
 
 constexpr int kBsThreads = 256, kBsWarps = kBsThreads / 32, kBsVecs = 4, kBsMost = 32;
 constexpr int kBsBatch = kBsThreads * kBsVecs * 4;            // logits that a CTA has in flight
-constexpr int kBsHold = 64;                                    // candidates that a warp collects before it sorts them in
+constexpr int kBsRing = 2 * kBsBatch * 4;                      // bytes of the batches in shared memory
+constexpr int kBsHold = 32;                                    // candidates that a warp collects before it sorts them in
 
 struct BsPart {                     // of a row: its best logits, sum exp(x - m) and m
     float best[kBsMost];
@@ -205,10 +206,11 @@ __device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const Bs
     __syncthreads();
     // ---- the histories ----
     int32_t *const tokens = a.tokens + (size_t)g0 * a.max_len;
-    if (W <= 8 && a.max_len % 4 == 0 && (reinterpret_cast<uintptr_t>(a.tokens) & 15) == 0)
-        beam_move<8>(reinterpret_cast<int4 *>(tokens), a.max_len / 4, W, g.parent);
-    else
-        beam_move<kBsMost>(tokens, a.max_len, W, g.parent);
+    // (as wide as 32 registers allow)
+    const bool wide = a.max_len % 4 == 0 && (reinterpret_cast<uintptr_t>(a.tokens) & 15) == 0;
+    if (W <= 8 && wide) beam_move<8>(reinterpret_cast<int4 *>(tokens), a.max_len / 4, W, g.parent);
+    else if (W <= 16 && wide) beam_move<16>(reinterpret_cast<int2 *>(tokens), a.max_len / 2, W, g.parent);
+    else beam_move<kBsMost>(tokens, a.max_len, W, g.parent);
     __syncthreads();
     if (tid < W && g.slot[tid] >= 0) tokens[(size_t)tid * a.max_len + g.slot[tid]] = g.token[tid];
 }
@@ -234,6 +236,7 @@ template <bool WIDE>
 __global__ void __launch_bounds__(kBsThreads, 4)
 beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsPart *__restrict__ parts, unsigned *__restrict__ tickets)
 {
+    extern __shared__ float4 beam_smem[];
     __shared__ float s_hold[kBsWarps][kBsHold + 128];           // a warp's candidates
     __shared__ int s_hold_at[kBsWarps][kBsHold + 128];
     __shared__ __align__(8) float2 s_all[kBsThreads];          // all warps' last candidates: logit, element
@@ -242,7 +245,7 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
     __shared__ double s_sum[kBsWarps];
     __shared__ float s_m[kBsWarps];
     __shared__ int s_bad[kBsWarps], s_last;
-    __shared__ __align__(16) float s_bars[kBsWarps];           // each a logit that `share` of the warp's reach
+    __shared__ __align__(16) float s_bars[4 * kBsWarps];       // the largest of the lanes' largest logits, four of each warp
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, W = a.beams;
     const int row = blockIdx.x / splits, split = blockIdx.x % splits, group = row / W;
     const float score = a.scores[row];
@@ -254,11 +257,10 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
         s_group.fin[tid] = a.finished[group * W + tid] != 0;
     }
     if (live) {                                                // (the same for the whole CTA)
-        const int share = (W + kBsWarps - 1) / kBsWarps;
         const float *x0 = a.logits + (long long)row * a.stride;
         const int e1 = min((split + 1) * part, a.vocab);
         BsBlock<float> best = {-INFINITY, 0x7fffffff};
-        float bar = -INFINITY, m = -INFINITY;
+        float bar = -INFINITY, m = -INFINITY, minus_m = 0.f, limit = -INFINITY;     // limit: what to look at closer
         int held = 0;
         double sum = 0.0;
         float lane_top = -INFINITY;
@@ -269,62 +271,92 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
             best = beam_sort_in(best, s_hold[warp], s_hold_at[warp], held);
             held = 0;
             bar = fmaxf(bar, __shfl_sync(0xffffffffu, best.key, W - 1));
+            limit = fminf(bar, m + 20.f);
         };
-        // element of a batch: e0 + 4 tid + 1024 i + j (wide), or e0 + tid + 256 (4 i + j)
+        // A batch's logits by way of the thread's own places in shared memory, one batch ahead.  Element of a batch: e0 + 4 tid +
+        // 1024 i + j (wide), or e0 + tid + 256 (4 i + j); places hold 16 bytes: [buffer][i][thread].
         auto element = [&](int e0, int i, int j) { return WIDE ? e0 + 4 * (i * kBsThreads + tid) + j : e0 + (4 * i + j) * kBsThreads + tid; };
-        auto fetch = [&](float (&x)[kBsVecs][4], int e0) {
+        float4 *const place = beam_smem + tid;
+        auto fetch = [&](int e0, int buf) {
+            const unsigned dst = (unsigned)__cvta_generic_to_shared(place + buf * kBsVecs * kBsThreads);
+            const float *const src = x0 + element(e0, 0, 0);
+            if (e0 + kBsBatch <= e1) {
 #pragma unroll
-            for (int i = 0; i < kBsVecs; ++i) {
-                if (WIDE && element(e0, i, 3) < e1) {
-                    const float4 y = __ldcs(reinterpret_cast<const float4 *>(x0 + element(e0, i, 0)));
-                    x[i][0] = y.x, x[i][1] = y.y, x[i][2] = y.z, x[i][3] = y.w;
-                } else {
+                for (int i = 0; i < kBsVecs; ++i) {
+                    if constexpr (WIDE) {
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + i * kBsThreads * 16), "l"(src + i * kBsThreads * 4) : "memory");
+                    } else {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x[i][j] = element(e0, i, j) < e1 ? __ldcs(x0 + element(e0, i, j)) : -INFINITY;
+                        for (int j = 0; j < 4; ++j)
+                            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + i * kBsThreads * 16 + 4 * j), "l"(src + (4 * i + j) * kBsThreads) : "memory");
+                    }
                 }
+            } else {
+#pragma unroll 1
+                for (int k = 0; k < 4 * kBsVecs; ++k)
+                    if (element(e0, k >> 2, k & 3) < e1)
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst + (k >> 2) * kBsThreads * 16 + 4 * (k & 3)),
+                                     "l"(x0 + element(e0, k >> 2, k & 3)) : "memory");
             }
+            asm volatile("cp.async.commit_group;" ::: "memory");
         };
+        fetch(split * part, 0);
 #pragma unroll 1
         for (int e0 = split * part; e0 < e1; e0 += kBsBatch) {
+            if (e0 + kBsBatch < e1) {
+                fetch(e0 + kBsBatch, (batch + 1) & 1);
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+            } else {
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+            }
             float x[kBsVecs][4];
-            fetch(x, e0);
+#pragma unroll
+            for (int i = 0; i < kBsVecs; ++i) {
+                const float4 y = place[((batch & 1) * kBsVecs + i) * kBsThreads];
+                x[i][0] = y.x, x[i][1] = y.y, x[i][2] = y.z, x[i][3] = y.w;
+            }
+            if (e0 + kBsBatch > e1) {
+#pragma unroll
+                for (int i = 0; i < kBsVecs; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (element(e0, i, j) >= e1) x[i][j] = -INFINITY;
+            }
             float tops[kBsVecs];
 #pragma unroll
             for (int i = 0; i < kBsVecs; ++i) tops[i] = bs_max_nan(x[i][0], x[i][1], bs_max_nan(x[i][2], x[i][3], x[i][3]));
             const float top = bs_max_nan(tops[0], tops[1], bs_max_nan(tops[2], tops[3], tops[3]));
-            bad |= __any_sync(0xffffffffu, !(top < INFINITY)); // nothing of the row counts any more
-            // `share` logits of every warp reach the least of the warps' bars, so the beams' last does; renewed at batches 1, 2,
-            // 4, ... (what another warp has not renewed yet holds as well)
+            const bool hit = __any_sync(0xffffffffu, !(top < limit));
             lane_top = fmaxf(lane_top, top);
             ++batch;
-            float most = m;
+            if (hit) {
+                bad |= __any_sync(0xffffffffu, !(top < INFINITY));             // nothing of the row counts any more
+                if (__any_sync(0xffffffffu, top > m + 20.f)) {
+                    float most = top;
+#pragma unroll
+                    for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+                    if (m > -INFINITY) sum *= exp((double)m - (double)most);
+                    m = most;
+                    minus_m = -most;
+                }
+            }
             if ((batch & (batch - 1)) == 0) {
-                const float in_order = bs_sorted(lane_top, lane), nth = __shfl_sync(0xffffffffu, in_order, share - 1);
-                most = __shfl_sync(0xffffffffu, in_order, 0);
-                if (lane == 0) *(volatile float *)&s_bars[warp] = nth;
+                // the bar, renewed at batches 1, 2, 4, ...: the `beams`-th of 32 of the part's logits, the largest four lanes' of every
+                // warp (what another warp has not renewed yet are logits of the part as well)
+                const float in_order = bs_sorted(lane_top, lane);
+                if (lane < 4) *(volatile float *)&s_bars[warp * 4 + lane] = in_order;
                 if (batch == 1) __syncthreads();
-                float least = INFINITY;
-#pragma unroll
-                for (int w = 0; w < kBsWarps; ++w) least = fminf(least, *(volatile float *)&s_bars[w]);
-                bar = fmaxf(bar, least);
-            } else if (__any_sync(0xffffffffu, top > m + 20.f)) {
-                most = lane_top;
-#pragma unroll
-                for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+                bar = fmaxf(bar, __shfl_sync(0xffffffffu, bs_sorted(*(volatile float *)&s_bars[lane], lane), W - 1));
             }
-            if (most > m + 20.f || m == -INFINITY) {
-                if (m > -INFINITY) sum *= exp((double)m - (double)most);
-                m = most;
-            }
-            if (bad || m == -INFINITY) continue;
+            limit = fminf(bar, m + 20.f);
             float2 add[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
             for (int i = 0; i < kBsVecs; ++i) {
-                bs_add_exp2(add[0], x[i][0], x[i][1], -m);
-                bs_add_exp2(add[1], x[i][2], x[i][3], -m);
+                bs_add_exp2(add[0], x[i][0], x[i][1], minus_m);
+                bs_add_exp2(add[1], x[i][2], x[i][3], minus_m);
             }
             sum += (double)((add[0].x + add[0].y) + (add[1].x + add[1].y));
-            if (!__any_sync(0xffffffffu, top >= bar)) continue;
+            if (!hit) continue;
 #pragma unroll
             for (int i = 0; i < kBsVecs; ++i) {
                 if (!__any_sync(0xffffffffu, tops[i] >= bar)) continue;
@@ -424,7 +456,9 @@ lookat_status launch_beam_select(Ctx *ctx, const BeamArgs &a)
     if (st != LOOKAT_OK) return st;
     const bool wide = (reinterpret_cast<uintptr_t>(a.logits) & 15) == 0 && a.stride % 4 == 0;
     auto kern = wide ? beam_select_kernel<true> : beam_select_kernel<false>;
-    kern<<<(unsigned)(rows * splits), kBsThreads, 0, ctx->stream>>>(a, (int)splits, per * kBsBatch, static_cast<BsPart *>(ctx->beam_parts.ptr),
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBsRing) != cudaSuccess)
+        return check_launch(ctx, "beam_select: shared-memory opt-in");
+    kern<<<(unsigned)(rows * splits), kBsThreads, kBsRing, ctx->stream>>>(a, (int)splits, per * kBsBatch, static_cast<BsPart *>(ctx->beam_parts.ptr),
                                                                     static_cast<unsigned *>(ctx->beam_tickets.ptr));
     return check_launch(ctx, "beam_select_kernel");
 }
