@@ -4,15 +4,18 @@
 // M lies kPackedLift below a line's largest score and moves only when the scores run ahead of it by more than kPuSlack: the
 // weights, fp16 numbers, use fp16's range (up to 2^15), and O in tensor memory is seldom rescaled.
 //
-// A line is one (token, query head) pair of a KV head, line = token * g + head.  A CTA works on two tiles of 128 lines of one
-// row against chunks of 128 tokens.  Tensor memory is full: per tile 128 columns of scores, over whose first half the
+// A line is one (token, query head) pair of a KV head, line = token * g + head.  An item is two tiles of 128 lines of one row,
+// against chunks of 128 tokens; a persistent CTA per SM goes through every 148th item of the list, which begins with those
+// that see the most tokens (packed_tile).  Tensor memory is full: per tile 128 columns of scores, over whose first half the
 // weights are written, and up to 128 of O.  So a tile's products alternate, S, O, S, O, and while the softmax threads work on
-// one tile the tensor pipe works on the other.  Roles (11 warps, one CTA per SM by tensor memory):
+// one tile the tensor pipe works on the other.  The roles run ahead of each other from item to item, so that an item's queries,
+// keys and first scores are there when the one before is written out (12 warps, one CTA per SM by tensor memory):
 //   warps 0-3 / 4-7  softmax of tile 0 / 1: thread r owns line r of its tile = tensor-memory lane r;
 //   warp 8      fetches keys and values by tiled bulk copies, 128 tokens x 64 dims with the 128-byte swizzle, through maps over
 //               the caller's strides; in the row's last chunk it zeroes the values behind the last token (a copy brings the next
 //               row's tokens along, whose infinities the weights of zero would not take away);
-//   warps 9, 10 one thread each issues the MMAs of tile 0 / 1 and commits them to mbarriers.
+//   warps 9, 10 one thread each issues the MMAs of tile 0 / 1 and commits them to mbarriers;
+//   warp 11     fetches the query lines (cp.async: any strides and groups).
 // Every mbarrier wait gives up after a bounded number of polls, raises the context's time-out flag and lets the CTA drain and
 // free its tensor memory.
 #include <cuda.h>           // CUtensorMap only
@@ -25,15 +28,16 @@ namespace lookat {
 namespace {
 
 constexpr int kPuRows = 128, kPuChunk = 128, kPuTiles = 2, kPuBoth = kPuTiles * kPuRows;
-constexpr int kPuSoftmax = kPuBoth, kPuThreads = kPuSoftmax + 96;
+constexpr int kPuSoftmax = kPuBoth, kPuThreads = kPuSoftmax + 128;
 constexpr float kPuSlack = 8.f;
 
 template <int DK, int DV>
 struct PuLayout {
-    static constexpr int kStages = DK == 64 && DV == 64 ? 3 : 2;
+    static constexpr int kStages = DK == 64 && DV == 64 ? 4 : 2;
     static constexpr int kKb = DK / 64, kVb = DV / 64, kBox = kPuChunk * 128;        // 64 dims of a chunk: 16 KB
-    static constexpr int kK = kKb * kBox, kV = kVb * kBox, kQ = kPuRows * 2 * (DK > DV ? DK : DV);
-    static constexpr int kOffK = 0, kOffV = kStages * kK, kOffQ = kOffV + kStages * kV, kOffBars = kOffQ + kPuTiles * kQ;
+    static constexpr int kK = kKb * kBox, kV = kVb * kBox, kQ = kPuRows * 2 * DK;
+    static constexpr int kOffK = 0, kOffV = kStages * kK, kOffQ = kOffV + kStages * kV;
+    static constexpr int kTurn = 4096, kOffTurn = kOffQ + kPuTiles * kQ, kOffBars = kOffTurn + kPuSoftmax / 32 * kTurn;     // turn: a warp's results on their way out
     static constexpr int kBytes = kOffBars + 256;
     static constexpr int kColO = kPuTiles * kPuChunk;
     // instruction descriptors: fp32 accumulate, fp16 operands, N >> 3 at bit 17, M >> 4 at bit 24; bit 16: B is MN-major
@@ -71,8 +75,8 @@ __device__ __forceinline__ void pu_copy(uint32_t dst, const CUtensorMap *map, in
 
 template <int DK, int DV>
 __global__ void __launch_bounds__(kPuThreads, 1)
-attend_packed_umma_kernel(PackedAttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, int k_order,
-                          int v_order, int *__restrict__ timeout_flag)
+attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+                          int k_order, int v_order, int *__restrict__ timeout_flag)
 {
     using Lay = PuLayout<DK, DV>;
     constexpr int kStages = Lay::kStages;
@@ -81,60 +85,36 @@ attend_packed_umma_kernel(PackedAttendArgs a, const __grid_constant__ CUtensorMa
     const uint32_t sm0 = um_smem(sm);
     uint64_t *const bars = reinterpret_cast<uint64_t *>(sm + Lay::kOffBars);
     uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(bars + 30);
-    // per stage: keys there, keys free, values there, values free; per tile: scores done (of each chunk), weights stored (of
-    // each chunk), O done; the values behind the row's end are zero
-    const uint32_t bar0 = um_smem(bars), bar_k = bar0, bar_kf = bar0 + 24, bar_v = bar0 + 48, bar_vf = bar0 + 72;
-    const uint32_t bar_s = bar0 + 96, bar_p = bar0 + 112, bar_o = bar0 + 128, bar_z = bar0 + 144;
+    // per stage: keys there, keys free, values there, values free; per tile: scores done and weights stored (of each of its
+    // chunks), queries there, queries free, O done, O read (of each of its items); copies of a row's last values there.  A phase of each
+    // ends only after every waiter of the one before has moved on.
+    const uint32_t bar0 = um_smem(bars), bar_k = bar0, bar_kf = bar0 + 32, bar_v = bar0 + 64, bar_vf = bar0 + 96;
+    const uint32_t bar_s = bar0 + 128, bar_p = bar0 + 144, bar_q = bar0 + 160, bar_qf = bar0 + 176, bar_o = bar0 + 192, bar_of = bar0 + 208;
+    const uint32_t bar_t = bar0 + 224;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int h = blockIdx.x % a.H_kv;
-    int b, place, first, n;
     if (blockIdx.x == 0) packed_check(a.rows, tid, kPuThreads);
-    if (!packed_tile(a.rows, a.g, kPuBoth, blockIdx.x / a.H_kv, lane, b, place, first, n)) return;
-    const int line0 = place * kPuBoth, lines = n * a.g;
-    const int tiles = lines - line0 > kPuRows ? 2 : 1;
-    auto chunks_of = [&](int t) { return (min(line0 + (t + 1) * kPuRows, lines) - 1) / a.g / kPuChunk + 1; };
-    const int n_chunks = chunks_of(tiles - 1);
-    const int tail = n - (n_chunks - 1) * kPuChunk;            // tokens of the row in the last chunk (more than a chunk: others follow)
-
     if (tid == 0) {
         for (int i = 0; i < kStages; ++i) {
             um_bar_init(bar_k + 8 * i, 1);
             um_bar_init(bar_v + 8 * i, 1);
-            um_bar_init(bar_kf + 8 * i, tiles);
-            um_bar_init(bar_vf + 8 * i, tiles);
+            um_bar_init(bar_kf + 8 * i, kPuTiles);
+            um_bar_init(bar_vf + 8 * i, kPuTiles);
         }
         for (int t = 0; t < kPuTiles; ++t) {
             um_bar_init(bar_s + 8 * t, 1);
             um_bar_init(bar_p + 8 * t, kPuRows);
+            um_bar_init(bar_q + 8 * t, 32);
+            um_bar_init(bar_qf + 8 * t, 1);
             um_bar_init(bar_o + 8 * t, 1);
+            um_bar_init(bar_of + 8 * t, kPuRows);
         }
-        um_bar_init(bar_z, 1);
+        um_bar_init(bar_t, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(um_smem(tmem_slot)), "n"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
-    // ---- the query lines, A operand of the scores: 64 dims each, 128-byte swizzle; a warp's 32 lines piece by piece ----
-    const int tile = warp >> 2, r = (warp & 3) * 32 + lane, line = line0 + tile * kPuRows + r;
-    const bool on = line < lines;
-    const int line_c = min(line, lines - 1), tok = line_c / a.g, head = h * a.g + line_c % a.g;      // lines beyond the last repeat it
-    if (warp < kPuSoftmax / 32) {
-        const unsigned long long at = reinterpret_cast<unsigned long long>(a.q.p + (first + tok) * a.q.ts + head * a.q.hs);
-        constexpr int kPieces = DK / 8;
-        uint4 x[kPieces];
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int idx = i * 32 + lane, row = idx / kPieces, piece = idx % kPieces;
-            x[i] = __ldg(reinterpret_cast<const uint4 *>(__shfl_sync(0xffffffffu, at, row)) + piece);
-        }
-#pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int idx = i * 32 + lane, row = (warp & 3) * 32 + idx / kPieces, piece = idx % kPieces;
-            *reinterpret_cast<uint4 *>(sm + Lay::kOffQ + tile * Lay::kQ + (piece >> 3) * (kPuRows * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4)) = x[i];
-        }
-        um_fence_async_smem();
     }
     um_fence_before();
     __syncthreads();
@@ -142,196 +122,282 @@ attend_packed_umma_kernel(PackedAttendArgs a, const __grid_constant__ CUtensorMa
     const uint32_t tmem = *tmem_slot;
     bool dead = (sm0 & 1023u) != 0;                            // a wait ran out (or the base is misaligned): leave, free, return
 
+    // ---- the CTA's items: two tiles of a row and KV head each; every role goes through them by itself ----
+    int at = blockIdx.x - gridDim.x, h = 0, b, place, first = 0, n = 0, line0 = 0, lines = 0, n_chunks = 0;
+    auto next = [&]() {
+        at += gridDim.x;
+        if (!packed_tile(a.rows, a.g, kPuBoth, at / a.H_kv, lane, b, place, first, n)) return false;
+        h = at % a.H_kv;
+        line0 = place * kPuBoth;
+        lines = n * a.g;
+        n_chunks = (min(line0 + kPuBoth, lines) - 1) / a.g / kPuChunk + 1;
+        return true;
+    };
+    auto chunks_of = [&](int t) { return line0 + t * kPuRows < lines ? (min(line0 + (t + 1) * kPuRows, lines) - 1) / a.g / kPuChunk + 1 : 0; };
+
     if (dead) {
         // misaligned shared-memory base: nothing runs
     } else if (warp == kPuSoftmax / 32) {
         // =================== the fetcher ===================
-        if (um_elect()) {
-            int k_sent = 0, v_sent = 0;
-            for (int ch = 0; ch < n_chunks && !dead; ++ch) {
-                const int st = ch % kStages, t0 = first + ch * kPuChunk;
-                const uint32_t done = (ch / kStages - 1) & 1;
-                if (ch >= kStages && !um_bar_wait(bar_kf + 8 * st, done)) { dead = true; break; }
-                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar_k + 8 * st), "r"(Lay::kK) : "memory");
+        // A row's last values, where it ends inside a chunk, come by a barrier of their own; with zeros behind them they are handed
+        // on.
+        int sent = 0, v_sent = 0, tails = 0;                   // chunks of keys, of values, of those with an end
+        while (!dead && next()) {
+            const int tail = n - (n_chunks - 1) * kPuChunk;
+            if (um_elect()) {
+                for (int ch = 0; ch < n_chunks; ++ch) {
+                    const int st = sent % kStages, t0 = first + ch * kPuChunk;
+                    const uint32_t done = (sent / kStages - 1) & 1, v_bar = ch == n_chunks - 1 && tail < kPuChunk ? bar_t : bar_v + 8 * st;
+                    if (sent >= kStages && !um_bar_wait(bar_kf + 8 * st, done)) { dead = true; break; }
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar_k + 8 * st), "r"(Lay::kK) : "memory");
 #pragma unroll
-                for (int i = 0; i < Lay::kKb; ++i) pu_copy(sm0 + Lay::kOffK + st * Lay::kK + i * Lay::kBox, &k_map, i * 64, h, t0, k_order, bar_k + 8 * st);
-                ++k_sent;
-                if (ch >= kStages && !um_bar_wait(bar_vf + 8 * st, done)) { dead = true; break; }
-                asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar_v + 8 * st), "r"(Lay::kV) : "memory");
+                    for (int i = 0; i < Lay::kKb; ++i) pu_copy(sm0 + Lay::kOffK + st * Lay::kK + i * Lay::kBox, &k_map, i * 64, h, t0, k_order, bar_k + 8 * st);
+                    ++sent;
+                    if (sent > kStages && !um_bar_wait(bar_vf + 8 * st, done)) { dead = true; break; }
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(v_bar), "r"(Lay::kV) : "memory");
 #pragma unroll
-                for (int i = 0; i < Lay::kVb; ++i) pu_copy(sm0 + Lay::kOffV + st * Lay::kV + i * Lay::kBox, &v_map, i * 64, h, t0, v_order, bar_v + 8 * st);
-                ++v_sent;
+                    for (int i = 0; i < Lay::kVb; ++i) pu_copy(sm0 + Lay::kOffV + st * Lay::kV + i * Lay::kBox, &v_map, i * 64, h, t0, v_order, v_bar);
+                    ++v_sent;
+                }
+                if (dead) {                                    // copies in flight end before the CTA does
+                    for (int i = max(0, sent - kStages); i < sent; ++i) um_bar_wait(bar_k + 8 * (i % kStages), (i / kStages) & 1);
+                    for (int i = max(0, v_sent - kStages); i < v_sent; ++i) um_bar_wait(bar_v + 8 * (i % kStages), (i / kStages) & 1);
+                }
             }
-            // copies in flight end before the CTA does
-            for (int i = max(0, k_sent - kStages); i < k_sent; ++i) dead |= !um_bar_wait(bar_k + 8 * (i % kStages), (i / kStages) & 1);
-            for (int i = max(0, v_sent - kStages); i < v_sent; ++i) dead |= !um_bar_wait(bar_v + 8 * (i % kStages), (i / kStages) & 1);
-        }
-        dead = __any_sync(0xffffffffu, dead);
-        const int last = (n_chunks - 1) % kStages;
-        dead = dead || !um_bar_wait(bar_v + 8 * last, ((n_chunks - 1) / kStages) & 1);         // (over already: for the other lanes' sake)
-        if (!dead && tail < kPuChunk) {
-            unsigned char *const rows = sm + Lay::kOffV + last * Lay::kV;
-            for (int i = tail * 8 + lane; i < kPuChunk * 8; i += 32)
+            dead = __any_sync(0xffffffffu, dead);
+            sent = __reduce_max_sync(0xffffffffu, sent);
+            v_sent = __reduce_max_sync(0xffffffffu, v_sent);
+            if (!dead && tail < kPuChunk) {
+                const int st = (v_sent - 1) % kStages;
+                if (!__all_sync(0xffffffffu, um_bar_wait(bar_t, tails & 1))) { dead = true; break; }
+                ++tails;
+                unsigned char *const rows = sm + Lay::kOffV + st * Lay::kV;
+                for (int i = tail * 8 + lane; i < kPuChunk * 8; i += 32)
 #pragma unroll
-                for (int j = 0; j < Lay::kVb; ++j) *reinterpret_cast<uint4 *>(rows + j * Lay::kBox + i * 16) = make_uint4(0u, 0u, 0u, 0u);
-            um_fence_async_smem();
-            __syncwarp();
-            if (lane == 0) um_bar_arrive(bar_z);
+                    for (int j = 0; j < Lay::kVb; ++j) *reinterpret_cast<uint4 *>(rows + j * Lay::kBox + i * 16) = make_uint4(0u, 0u, 0u, 0u);
+                um_fence_async_smem();
+                __syncwarp();
+                if (lane == 0) um_bar_arrive(bar_v + 8 * st);
+            }
         }
+    } else if (warp == kPuThreads / 32 - 1) {
+        // =================== the queries: A operand of the scores, 64 dims each, 128-byte swizzle ===================
+        constexpr int kPieces = DK / 8;
+        int seen[kPuTiles] = {0, 0};
+        bool started = false;
+        while (!dead && next()) {
+            const int tiles = lines - line0 > kPuRows ? 2 : 1;
+            for (int t = 0; t < tiles; ++t) {
+                if (seen[t] && !__all_sync(0xffffffffu, um_bar_wait(bar_qf + 8 * t, (seen[t] - 1) & 1))) { dead = true; break; }
+#pragma unroll 1
+                for (int part = 0; part < kPuRows / 32; ++part) {
+                    const int line = min(line0 + t * kPuRows + part * 32 + lane, lines - 1);       // lines beyond the last repeat it
+                    const unsigned long long src = reinterpret_cast<unsigned long long>(a.q.p + (first + line / a.g) * a.q.ts + (h * a.g + line % a.g) * a.q.hs);
+#pragma unroll
+                    for (int i = 0; i < kPieces; ++i) {
+                        const int idx = i * 32 + lane, row = part * 32 + idx / kPieces, piece = idx % kPieces;
+                        const unsigned long long from = __shfl_sync(0xffffffffu, src, idx / kPieces);
+                        um_cp_async16(sm0 + Lay::kOffQ + t * Lay::kQ + (piece >> 3) * (kPuRows * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4),
+                                      reinterpret_cast<const uint4 *>(from) + piece);
+                    }
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");
+                if (!started && tiles == 2) {                  // (both tiles of the first item at once)
+                    if (t == 0) continue;
+                    asm volatile("cp.async.wait_group 1;" ::: "memory");
+                    um_fence_async_smem();
+                    um_bar_arrive(bar_q);
+                    ++seen[0];
+                }
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                um_fence_async_smem();
+                um_bar_arrive(bar_q + 8 * t);
+                ++seen[t];
+            }
+            started = true;
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (warp > kPuSoftmax / 32) {
         // =================== the MMA thread of a tile ===================
         const int t = warp - kPuSoftmax / 32 - 1;
-        if (t < tiles && um_elect()) {
-            // descriptors: stride 1024 B, version 1, 128-byte swizzle in the high word; start address and leading offset in
-            // the low word
-            const uint32_t desc_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
-            const uint32_t k_lo = ((sm0 + Lay::kOffK) >> 4) | (1u << 16);                          // leading offset unused (16 B)
-            const uint32_t q_lo = ((sm0 + Lay::kOffQ + t * Lay::kQ) >> 4) | (1u << 16);
-            const uint32_t v_lo = ((sm0 + Lay::kOffV) >> 4) | ((uint32_t)(Lay::kBox / 16) << 16);  // between 64-column blocks
-            const uint32_t tm_s = tmem + t * kPuChunk, tm_o = tmem + Lay::kColO + t * DV;
+        // descriptors: stride 1024 B, version 1, 128-byte swizzle in the high word; start address and leading offset in
+        // the low word
+        const uint32_t desc_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+        const uint32_t k_lo = ((sm0 + Lay::kOffK) >> 4) | (1u << 16);                              // leading offset unused (16 B)
+        const uint32_t q_lo = ((sm0 + Lay::kOffQ + t * Lay::kQ) >> 4) | (1u << 16);
+        const uint32_t v_lo = ((sm0 + Lay::kOffV) >> 4) | ((uint32_t)(Lay::kBox / 16) << 16);      // between 64-column blocks
+        const uint32_t tm_s = tmem + t * kPuChunk, tm_o = tmem + Lay::kColO + t * DV;
+        int chunk0 = 0, mine0 = 0, items = 0;                  // chunks of all items so far, the tile's own, its items
+        while (!dead && next()) {
             const int mine = chunks_of(t);
-            auto score_mma = [&](int ch) {
-                const int st = ch % kStages;
-                if (!um_bar_wait(bar_k + 8 * st, (ch / kStages) & 1)) return false;
-                um_fence_after();
-                const uint32_t lo = k_lo + st * (Lay::kK >> 4);
+            if (um_elect()) {
+                auto score_mma = [&](int ch) {
+                    const int st = (chunk0 + ch) % kStages;
+                    if (!um_bar_wait(bar_k + 8 * st, ((chunk0 + ch) / kStages) & 1)) return false;
+                    um_fence_after();
+                    const uint32_t lo = k_lo + st * (Lay::kK >> 4);
 #pragma unroll
-                for (int ks = 0; ks < DK / 16; ++ks) {
-                    const uint32_t off = ((ks >> 2) * Lay::kBox + (ks & 3) * 32) >> 4;
-                    if (ks == 0) um_mma_ss<false>(tm_s, q_lo + off, desc_hi, lo + off, desc_hi, Lay::kIdescS);
-                    else um_mma_ss<true>(tm_s, q_lo + off, desc_hi, lo + off, desc_hi, Lay::kIdescS);
-                }
-                um_commit(bar_s + 8 * t);
-                um_commit(bar_kf + 8 * st);
-                return true;
-            };
-            auto value_mma = [&](int ch) {
-                const int st = ch % kStages;
-                if (!um_bar_wait(bar_p + 8 * t, ch & 1) || !um_bar_wait(bar_v + 8 * st, (ch / kStages) & 1)) return false;
-                if (ch == n_chunks - 1 && tail < kPuChunk && !um_bar_wait(bar_z, 0)) return false;
-                um_fence_after();
-                const uint32_t lo = v_lo + st * (Lay::kV >> 4);
+                    for (int ks = 0; ks < DK / 16; ++ks) {
+                        const uint32_t off = ((ks >> 2) * Lay::kBox + (ks & 3) * 32) >> 4;
+                        if (ks == 0) um_mma_ss<false>(tm_s, q_lo + off, desc_hi, lo + off, desc_hi, Lay::kIdescS);
+                        else um_mma_ss<true>(tm_s, q_lo + off, desc_hi, lo + off, desc_hi, Lay::kIdescS);
+                    }
+                    um_commit(bar_s + 8 * t);
+                    um_commit(bar_kf + 8 * st);
+                    if (ch == mine - 1) um_commit(bar_qf + 8 * t);
+                    return true;
+                };
+                auto value_mma = [&](int ch) {
+                    const int st = (chunk0 + ch) % kStages;
+                    if (!um_bar_wait(bar_p + 8 * t, (mine0 + ch) & 1) || !um_bar_wait(bar_v + 8 * st, ((chunk0 + ch) / kStages) & 1)) return false;
+                    if (ch == 0 && items && !um_bar_wait(bar_of + 8 * t, (items - 1) & 1)) return false;
+                    um_fence_after();
+                    const uint32_t lo = v_lo + st * (Lay::kV >> 4);
 #pragma unroll
-                for (int kt = 0; kt < kPuChunk / 16; ++kt) {
-                    if (kt == 0 && ch == 0) um_mma_ts<false>(tm_o, tm_s, lo, desc_hi, Lay::kIdescO);
-                    else um_mma_ts<true>(tm_o, tm_s + kt * 8, lo + kt * (2048 >> 4), desc_hi, Lay::kIdescO);
+                    for (int kt = 0; kt < kPuChunk / 16; ++kt) {
+                        if (kt == 0 && ch == 0) um_mma_ts<false>(tm_o, tm_s, lo, desc_hi, Lay::kIdescO);
+                        else um_mma_ts<true>(tm_o, tm_s + kt * 8, lo + kt * (2048 >> 4), desc_hi, Lay::kIdescO);
+                    }
+                    um_commit(bar_vf + 8 * st);
+                    return true;
+                };
+                bool ok = true;
+                if (mine) {
+                    ok = um_bar_wait(bar_q + 8 * t, items & 1) && score_mma(0);
+                    for (int ch = 0; ok && ch < mine; ++ch) ok = value_mma(ch) && (ch + 1 >= mine || score_mma(ch + 1));
+                    if (ok) um_commit(bar_o + 8 * t);
                 }
-                um_commit(bar_vf + 8 * st);
-                return true;
-            };
-            bool ok = score_mma(0);
-            for (int ch = 0; ok && ch < mine; ++ch) ok = value_mma(ch) && (ch + 1 >= mine || score_mma(ch + 1));
-            if (ok) um_commit(bar_o + 8 * t);
-            for (int ch = mine; ok && ch < n_chunks; ++ch) {   // chunks that only the other tile sees
-                const int st = ch % kStages;
-                ok = um_bar_wait(bar_k + 8 * st, (ch / kStages) & 1);
-                if (ok) um_bar_arrive(bar_kf + 8 * st);
-                ok = ok && um_bar_wait(bar_v + 8 * st, (ch / kStages) & 1);
-                if (ok) um_bar_arrive(bar_vf + 8 * st);
+                for (int ch = mine; ok && ch < n_chunks; ++ch) {               // chunks that only the other tile sees
+                    const int st = (chunk0 + ch) % kStages;
+                    ok = um_bar_wait(bar_k + 8 * st, ((chunk0 + ch) / kStages) & 1);
+                    if (ok) um_bar_arrive(bar_kf + 8 * st);
+                    ok = ok && um_bar_wait(bar_v + 8 * st, ((chunk0 + ch) / kStages) & 1);
+                    if (ok) um_bar_arrive(bar_vf + 8 * st);
+                }
+                dead = !ok;
             }
-            dead = !ok;
+            dead = __any_sync(0xffffffffu, dead);
+            chunk0 += n_chunks;
+            mine0 += mine;
+            items += mine > 0;
         }
-    } else if (tile < tiles) {
+    } else {
         // =================== softmax: thread r owns line r of its tile ===================
-        const int mine = chunks_of(tile);
+        const int tile = warp >> 2;
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tm_s = tmem + tile * kPuChunk + lane_base, tm_o = tmem + Lay::kColO + tile * DV + lane_base;
-        float m_run = 0.f, l_run = 0.f;
-        for (int ch = 0; ch < mine; ++ch) {
-            if (!__all_sync(0xffffffffu, um_bar_wait(bar_s + 8 * tile, ch & 1))) { dead = true; break; }     // warp-uniform
-            um_fence_after();
-            float2 y[kPuChunk / 2];
-            {
-                uint32_t s[kPuChunk / 32][32];
-#pragma unroll
-                for (int p = 0; p < kPuChunk / 32; ++p) um_ld32(s[p], tm_s + p * 32);
-                um_wait_ld();
-#pragma unroll
-                for (int i = 0; i < kPuChunk / 2; ++i) y[i] = make_float2(__uint_as_float(s[i / 16][2 * i % 32]), __uint_as_float(s[i / 16][2 * i % 32 + 1]));
+        unsigned char *const turn = sm + Lay::kOffTurn + warp * Lay::kTurn;
+        int mine0 = 0, items = 0;                              // the tile's chunks and items so far
+        bool more = next();
+        while (!dead && more) {
+            const int mine = chunks_of(tile), line = line0 + tile * kPuRows + (warp & 3) * 32 + lane, line_c = min(line, lines - 1);
+            if (!mine) {
+                more = next();
+                continue;
             }
-            const int sees = tok + 1 - ch * kPuChunk;          // tokens of the chunk that this line sees
-            if (__any_sync(0xffffffffu, sees < kPuChunk)) {
+            const int tok = line_c / a.g;                      // (lines beyond the last repeat it)
+            const unsigned long long out = line < lines ? reinterpret_cast<unsigned long long>(a.out.p + (first + tok) * a.out.ts + (h * a.g + line_c % a.g) * a.out.hs) : 0;
+            float m_run = 0.f, l_run = 0.f;
+            for (int ch = 0; ch < mine; ++ch) {
+                if (!__all_sync(0xffffffffu, um_bar_wait(bar_s + 8 * tile, (mine0 + ch) & 1))) { dead = true; break; }     // warp-uniform
+                um_fence_after();
+                float2 y[kPuChunk / 2];
+                {
+                    uint32_t s[kPuChunk / 32][32];
 #pragma unroll
-                for (int i = 0; i < kPuChunk / 2; ++i) {
-                    if (2 * i >= sees) y[i].x = -INFINITY;
-                    if (2 * i + 1 >= sees) y[i].y = -INFINITY;
-                }
-            }
-            float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int i = 0; i < kPuChunk / 2; ++i) tops[i & 3] = pu_max3(tops[i & 3], y[i].x, y[i].y);
-            const float top = fmaxf(pu_max3(tops[0], tops[1], tops[2]), tops[3]) * a.scale_log2;
-            // M moves only when the scores run ahead by more than kPuSlack (token 0 is in every line's first chunk)
-            float alpha = 1.f;
-            if (ch == 0) {
-                m_run = top - kPackedLift;
-            } else if (top > m_run + (kPackedLift + kPuSlack)) {
-                alpha = ex2_approx(m_run - (top - kPackedLift));
-                m_run = top - kPackedLift;
-            }
-            float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                uint32_t pk[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    const float2 e = pu_fma2(y[half * 32 + i], a.scale_log2, -m_run);
-                    const float2 w = make_float2(ex2_approx(e.x), ex2_approx(e.y));
-                    sum[i & 1] = pu_add2(sum[i & 1], w);
-                    const __half2 x = __floats2half2_rn(w.x, w.y);
-                    pk[i] = *reinterpret_cast<const uint32_t *>(&x);
-                }
-                um_st32(tm_s + half * 32, pk);
-            }
-            l_run = fmaf(l_run, alpha, (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
-            // O: this tile's value MMAs so far were over before these scores were (one thread issues both, in order)
-            if (__any_sync(0xffffffffu, alpha != 1.f)) {
-#pragma unroll 1
-                for (int p = 0; p < DV / 32; ++p) {
-                    uint32_t o[32];
-                    um_ld32(o, tm_o + p * 32);
+                    for (int p = 0; p < kPuChunk / 32; ++p) um_ld32(s[p], tm_s + p * 32);
                     um_wait_ld();
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                    um_st32(tm_o + p * 32, o);
+                    for (int i = 0; i < kPuChunk / 2; ++i) y[i] = make_float2(__uint_as_float(s[i / 16][2 * i % 32]), __uint_as_float(s[i / 16][2 * i % 32 + 1]));
                 }
+                const int sees = tok + 1 - ch * kPuChunk;      // tokens of the chunk that this line sees
+                if (__any_sync(0xffffffffu, sees < kPuChunk)) {
+#pragma unroll
+                    for (int i = 0; i < kPuChunk / 2; ++i) {
+                        if (2 * i >= sees) y[i].x = -INFINITY;
+                        if (2 * i + 1 >= sees) y[i].y = -INFINITY;
+                    }
+                }
+                float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int i = 0; i < kPuChunk / 2; ++i) tops[i & 3] = pu_max3(tops[i & 3], y[i].x, y[i].y);
+                const float top = fmaxf(pu_max3(tops[0], tops[1], tops[2]), tops[3]) * a.scale_log2;
+                // M moves only when the scores run ahead by more than kPuSlack (token 0 is in every line's first chunk)
+                float alpha = 1.f;
+                if (ch == 0) {
+                    m_run = top - kPackedLift;
+                } else if (top > m_run + (kPackedLift + kPuSlack)) {
+                    alpha = ex2_approx(m_run - (top - kPackedLift));
+                    m_run = top - kPackedLift;
+                }
+                float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t pk[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const float2 e = pu_fma2(y[half * 32 + i], a.scale_log2, -m_run);
+                        const float2 w = make_float2(ex2_approx(e.x), ex2_approx(e.y));
+                        sum[i & 1] = pu_add2(sum[i & 1], w);
+                        const __half2 x = __floats2half2_rn(w.x, w.y);
+                        pk[i] = *reinterpret_cast<const uint32_t *>(&x);
+                    }
+                    um_st32(tm_s + half * 32, pk);
+                }
+                l_run = fmaf(l_run, alpha, (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
+                // O: this tile's value MMAs so far were over before these scores were (one thread issues both, in order)
+                if (__any_sync(0xffffffffu, alpha != 1.f)) {
+#pragma unroll 1
+                    for (int p = 0; p < DV / 32; ++p) {
+                        uint32_t o[32];
+                        um_ld32(o, tm_o + p * 32);
+                        um_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                        um_st32(tm_o + p * 32, o);
+                    }
+                }
+                um_wait_st();
+                um_fence_before();
+                um_bar_arrive(bar_p + 8 * tile);
             }
-            um_wait_st();
-            um_fence_before();
-            um_bar_arrive(bar_p + 8 * tile);
-        }
-        if (!dead && __all_sync(0xffffffffu, um_bar_wait(bar_o + 8 * tile, 0))) {
-            // results by way of the tile's query rows, which nothing reads any more: whole lines of global memory
+            mine0 += mine;
+            const int parity = items++ & 1;
+            more = next();                                     // (found while the last products run)
+            if (dead || !__all_sync(0xffffffffu, um_bar_wait(bar_o + 8 * tile, parity))) { dead = true; break; }
+            // ---- results, 64 dims at a time by way of the warp's shared memory: whole lines of global memory ----
             um_fence_after();
             const float inv = 1.f / l_run;
-            constexpr int kPieces = DV / 8;
-            unsigned char *const rows = sm + Lay::kOffQ + tile * Lay::kQ + (warp & 3) * 32 * (DV * 2);
 #pragma unroll
-            for (int p = 0; p < DV / 32; ++p) {
-                uint32_t o[32];
-                um_ld32(o, tm_o + p * 32);
+            for (int part = 0; part < DV / 64; ++part) {
+                uint32_t o[2][32];
+                um_ld32(o[0], tm_o + part * 64);
+                um_ld32(o[1], tm_o + part * 64 + 32);
                 um_wait_ld();
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint4 x;
-                    x.x = q8_half2(__uint_as_float(o[8 * i]) * inv, __uint_as_float(o[8 * i + 1]) * inv);
-                    x.y = q8_half2(__uint_as_float(o[8 * i + 2]) * inv, __uint_as_float(o[8 * i + 3]) * inv);
-                    x.z = q8_half2(__uint_as_float(o[8 * i + 4]) * inv, __uint_as_float(o[8 * i + 5]) * inv);
-                    x.w = q8_half2(__uint_as_float(o[8 * i + 6]) * inv, __uint_as_float(o[8 * i + 7]) * inv);
-                    *reinterpret_cast<uint4 *>(rows + lane * (DV * 2) + (((p * 4 + i) ^ (lane & 7)) << 4)) = x;
+                if (part == DV / 64 - 1) {
+                    um_fence_before();
+                    um_bar_arrive(bar_of + 8 * tile);
                 }
-            }
-            __syncwarp();
-            const unsigned long long at = on ? reinterpret_cast<unsigned long long>(a.out.p + (first + tok) * a.out.ts + head * a.out.hs) : 0;
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                const int idx = i * 32 + lane, row = idx / kPieces, piece = idx % kPieces;
-                const uint4 x = *reinterpret_cast<const uint4 *>(rows + row * (DV * 2) + ((piece ^ (row & 7)) << 4));
-                const unsigned long long dst = __shfl_sync(0xffffffffu, at, row);
-                if (dst) *(reinterpret_cast<uint4 *>(dst) + piece) = x;
+                for (int i = 0; i < 8; ++i) {
+                    const uint32_t *const w = &o[i >> 2][(i & 3) * 8];
+                    uint4 x;
+                    x.x = q8_half2(__uint_as_float(w[0]) * inv, __uint_as_float(w[1]) * inv);
+                    x.y = q8_half2(__uint_as_float(w[2]) * inv, __uint_as_float(w[3]) * inv);
+                    x.z = q8_half2(__uint_as_float(w[4]) * inv, __uint_as_float(w[5]) * inv);
+                    x.w = q8_half2(__uint_as_float(w[6]) * inv, __uint_as_float(w[7]) * inv);
+                    *reinterpret_cast<uint4 *>(turn + lane * 128 + ((i ^ (lane & 7)) << 4)) = x;
+                }
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int row = i * 4 + (lane >> 3), piece = lane & 7;
+                    const uint4 x = *reinterpret_cast<const uint4 *>(turn + row * 128 + ((piece ^ (row & 7)) << 4));
+                    const unsigned long long dst = __shfl_sync(0xffffffffu, out, row);
+                    if (dst) *(reinterpret_cast<uint4 *>(dst) + part * 8 + piece) = x;
+                }
+                __syncwarp();
             }
-        } else {
-            dead = true;
         }
     }
 
@@ -355,8 +421,8 @@ lookat_status launch_pu(Ctx *ctx, const PackedAttendArgs &a)
         return set_error(ctx, LOOKAT_ERR_CUDA, "attend_packed: the driver refused a tensor map");
     // no more tiles than this, whatever the rows' lengths
     const long long ctas = ((long long)a.rows.n * a.g / kPuBoth + (a.rows.B < a.rows.n ? a.rows.B : a.rows.n)) * a.H_kv;
-    if (ctas > 0x7fffffffll) return set_error(ctx, LOOKAT_ERR_UNSUPPORTED, "attend_packed: too many tokens for one call");
-    kern<<<(unsigned)ctas, kPuThreads, Lay::kBytes, ctx->stream>>>(a, k_map, v_map, k_order, v_order, ctx->timeout_flag);
+    if (ctas > 0x3fffffffll) return set_error(ctx, LOOKAT_ERR_UNSUPPORTED, "attend_packed: too many tokens for one call");
+    kern<<<(unsigned)(ctas < ctx->sm_count ? ctas : ctx->sm_count), kPuThreads, Lay::kBytes, ctx->stream>>>(a, k_map, v_map, k_order, v_order, ctx->timeout_flag);
     return check_launch(ctx, "attend_packed_umma_kernel");
 }
 

@@ -53,7 +53,7 @@ __device__ __forceinline__ void packed_check(const Packed &p, int thread, int th
 // that the tiles with the most tokens to attend start first.  Called by a whole warp; false behind the last tile.
 //   With A(x) the number of tiles at place x or later (the sum over rows of tiles - x, where positive), the tile's place is the x
 // with A(x + 1) <= item < A(x), found by bisection, and it is row number item - A(x + 1) of those with more than x tiles.
-__device__ inline bool packed_tile(const Packed &p, int g, int per, long long item, int lane, int &b, int &place, int &first, int &n)
+__device__ inline bool packed_tile(const Packed &p, int g, int per, int item, int lane, int &b, int &place, int &first, int &n)
 {
     auto tiles_of = [&](int row, int &at, int &len) {
         len = row < p.B ? packed_row(p, row, at) : 0;
@@ -68,14 +68,12 @@ __device__ inline bool packed_tile(const Packed &p, int g, int per, long long it
     }
     most = __reduce_max_sync(0xffffffffu, most);
     auto later = [&](int x) {                                   // A(x)
-        long long sum = max(mine - x, 0);
+        int sum = max(mine - x, 0);
         for (int row = lane + 32; row < p.B; row += 32) {
             int t, l;
             sum += max(tiles_of(row, t, l) - x, 0);
         }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        return sum;
+        return __reduce_add_sync(0xffffffffu, sum);
     };
     int lo = 0, hi = most;                                      // A(lo) > item >= A(hi), if any
     if (later(0) <= item) return false;
@@ -84,14 +82,14 @@ __device__ inline bool packed_tile(const Packed &p, int g, int per, long long it
         (later(mid) > item ? lo : hi) = mid;
     }
     place = lo;
-    long long rank = item - later(lo + 1);
+    int rank = item - later(lo + 1);
     for (int row0 = 0; row0 < p.B; row0 += 32) {
         int t = at, l = len, tiles = mine;
         if (row0) tiles = tiles_of(row0 + lane, t, l);
         const unsigned who = __ballot_sync(0xffffffffu, tiles > lo);
         const int count = __popc(who);
         if (rank < count) {
-            const unsigned src = __fns(who, 0, (int)rank + 1);
+            const unsigned src = __fns(who, 0, rank + 1);
             b = row0 + (int)src;
             first = __shfl_sync(0xffffffffu, t, src);
             n = __shfl_sync(0xffffffffu, l, src);
