@@ -30,6 +30,7 @@ namespace {
 constexpr int kPuRows = 128, kPuChunk = 128, kPuTiles = 2, kPuBoth = kPuTiles * kPuRows;
 constexpr int kPuSoftmax = kPuBoth, kPuThreads = kPuSoftmax + 128;
 constexpr float kPuSlack = 8.f;
+constexpr int kPuListed = 128;                  // items that a CTA finds at its start, with all its warps; later ones every role finds by itself
 
 template <int DK, int DV>
 struct PuLayout {
@@ -38,7 +39,7 @@ struct PuLayout {
     static constexpr int kK = kKb * kBox, kV = kVb * kBox, kQ = kPuRows * 2 * DK;
     static constexpr int kOffK = 0, kOffV = kStages * kK, kOffQ = kOffV + kStages * kV;
     static constexpr int kTurn = 4096, kOffTurn = kOffQ + kPuTiles * kQ, kOffBars = kOffTurn + kPuSoftmax / 32 * kTurn;     // turn: a warp's results on their way out
-    static constexpr int kBytes = kOffBars + 256;
+    static constexpr int kOffItems = kOffBars + 256, kBytes = kOffItems + kPuListed * 16;
     static constexpr int kColO = kPuTiles * kPuChunk;
     // instruction descriptors: fp32 accumulate, fp16 operands, N >> 3 at bit 17, M >> 4 at bit 24; bit 16: B is MN-major
     static constexpr uint32_t kIdescS = (1u << 4) | ((uint32_t)(kPuChunk >> 3) << 17) | ((uint32_t)(kPuRows >> 4) << 24);
@@ -116,17 +117,33 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(um_smem(tmem_slot)), "n"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    // ---- the CTA's items: two tiles of a row and KV head each: {first token, tokens of the row, place of the tiles}, no tokens: the end ----
+    int4 *const listed = reinterpret_cast<int4 *>(sm + Lay::kOffItems);
+    for (int k = warp; k < kPuListed; k += kPuThreads / 32) {
+        int b, place, first, n;
+        const bool some = packed_tile(a.rows, a.g, kPuBoth, (blockIdx.x + k * gridDim.x) / a.H_kv, lane, b, place, first, n);
+        if (lane == 0) listed[k] = some ? make_int4(first, n, place, 0) : make_int4(0, 0, 0, 0);
+        if (!some) break;                                      // (a warp of an earlier place has met the end, too, or will)
+    }
     um_fence_before();
     __syncthreads();
     um_fence_after();
     const uint32_t tmem = *tmem_slot;
     bool dead = (sm0 & 1023u) != 0;                            // a wait ran out (or the base is misaligned): leave, free, return
 
-    // ---- the CTA's items: two tiles of a row and KV head each; every role goes through them by itself ----
-    int at = blockIdx.x - gridDim.x, h = 0, b, place, first = 0, n = 0, line0 = 0, lines = 0, n_chunks = 0;
+    // every role goes through the items by itself
+    int k = -1, h = 0, first = 0, n = 0, line0 = 0, lines = 0, n_chunks = 0;
     auto next = [&]() {
-        at += gridDim.x;
-        if (!packed_tile(a.rows, a.g, kPuBoth, at / a.H_kv, lane, b, place, first, n)) return false;
+        const int at = blockIdx.x + ++k * gridDim.x;
+        int place;
+        if (k < kPuListed) {
+            const int4 item = listed[k];
+            if (item.y == 0) return false;
+            first = item.x, n = item.y, place = item.z;
+        } else {
+            int b;
+            if (!packed_tile(a.rows, a.g, kPuBoth, at / a.H_kv, lane, b, place, first, n)) return false;
+        }
         h = at % a.H_kv;
         line0 = place * kPuBoth;
         lines = n * a.g;

@@ -89,8 +89,8 @@ __device__ inline bool packed_tile(const Packed &p, int g, int per, int item, in
         const unsigned who = __ballot_sync(0xffffffffu, tiles > lo);
         const int count = __popc(who);
         if (rank < count) {
-            const unsigned src = __fns(who, 0, rank + 1);
-            b = row0 + (int)src;
+            const int src = __ffs(__ballot_sync(0xffffffffu, tiles > lo && __popc(who & ((1u << lane) - 1)) == rank)) - 1;
+            b = row0 + src;
             first = __shfl_sync(0xffffffffu, t, src);
             n = __shfl_sync(0xffffffffu, l, src);
             return true;
