@@ -4,8 +4,8 @@
 // M lies kPackedLift below a line's largest score and moves only when the scores run ahead of it by more than kPuSlack: the
 // weights, fp16 numbers, use fp16's range (up to 2^15), and O in tensor memory is seldom rescaled.
 //
-// A line is one (token, query head) pair of a KV head, line = token * g + head.  An item is two tiles of 128 lines of one row,
-// against chunks of 128 tokens; a persistent CTA per SM goes through every 148th item of the list, which begins with those
+// A line is one (token, query head) pair of a KV head, line = token * g + head.  An item is two tiles of 128 lines of one row (`per`
+// lines: one tile where there are few items), against chunks of 128 tokens; a persistent CTA per SM goes through every 148th item of the list, which begins with those
 // that see the most tokens (packed_tile).  Tensor memory is full: per tile 128 columns of scores, over whose first half the
 // weights are written, and up to 128 of O.  So a tile's products alternate, S, O, S, O, and while the softmax threads work on
 // one tile the tensor pipe works on the other.  The roles run ahead of each other from item to item, so that an item's queries,
@@ -76,7 +76,7 @@ __device__ __forceinline__ void pu_copy(uint32_t dst, const CUtensorMap *map, in
 
 template <int DK, int DV>
 __global__ void __launch_bounds__(kPuThreads, 1)
-attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, int per,
                           int k_order, int v_order, int *__restrict__ timeout_flag)
 {
     using Lay = PuLayout<DK, DV>;
@@ -121,7 +121,7 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
     int4 *const listed = reinterpret_cast<int4 *>(sm + Lay::kOffItems);
     for (int k = warp; k < kPuListed; k += kPuThreads / 32) {
         int b, place, first, n;
-        const bool some = packed_tile(a.rows, a.g, kPuBoth, (blockIdx.x + k * gridDim.x) / a.H_kv, lane, b, place, first, n);
+        const bool some = packed_tile(a.rows, a.g, per, (blockIdx.x + k * gridDim.x) / a.H_kv, lane, b, place, first, n);
         if (lane == 0) listed[k] = some ? make_int4(first, n, place, 0) : make_int4(0, 0, 0, 0);
         if (!some) break;                                      // (a warp of an earlier place has met the end, too, or will)
     }
@@ -142,15 +142,15 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
             first = item.x, n = item.y, place = item.z;
         } else {
             int b;
-            if (!packed_tile(a.rows, a.g, kPuBoth, at / a.H_kv, lane, b, place, first, n)) return false;
+            if (!packed_tile(a.rows, a.g, per, at / a.H_kv, lane, b, place, first, n)) return false;
         }
         h = at % a.H_kv;
-        line0 = place * kPuBoth;
+        line0 = place * per;
         lines = n * a.g;
-        n_chunks = (min(line0 + kPuBoth, lines) - 1) / a.g / kPuChunk + 1;
+        n_chunks = (min(line0 + per, lines) - 1) / a.g / kPuChunk + 1;
         return true;
     };
-    auto chunks_of = [&](int t) { return line0 + t * kPuRows < lines ? (min(line0 + (t + 1) * kPuRows, lines) - 1) / a.g / kPuChunk + 1 : 0; };
+    auto chunks_of = [&](int t) { return t * kPuRows < per && line0 + t * kPuRows < lines ? (min(line0 + (t + 1) * kPuRows, lines) - 1) / a.g / kPuChunk + 1 : 0; };
 
     if (dead) {
         // misaligned shared-memory base: nothing runs
@@ -203,7 +203,7 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
         int seen[kPuTiles] = {0, 0};
         bool started = false;
         while (!dead && next()) {
-            const int tiles = lines - line0 > kPuRows ? 2 : 1;
+            const int tiles = chunks_of(1) ? 2 : 1;
             for (int t = 0; t < tiles; ++t) {
                 if (seen[t] && !__all_sync(0xffffffffu, um_bar_wait(bar_qf + 8 * t, (seen[t] - 1) & 1))) { dead = true; break; }
 #pragma unroll 1
@@ -437,9 +437,12 @@ lookat_status launch_pu(Ctx *ctx, const PackedAttendArgs &a)
         !make_rows_map_f16(&v_map, a.v.p, DV, a.H_kv, a.rows.n, a.v.hs, a.v.ts, kPuChunk, &v_order))
         return set_error(ctx, LOOKAT_ERR_CUDA, "attend_packed: the driver refused a tensor map");
     // no more tiles than this, whatever the rows' lengths
-    const long long ctas = ((long long)a.rows.n * a.g / kPuBoth + (a.rows.B < a.rows.n ? a.rows.B : a.rows.n)) * a.H_kv;
+    auto items = [&](int per) { return ((long long)a.rows.n * a.g / per + (a.rows.B < a.rows.n ? a.rows.B : a.rows.n)) * a.H_kv; };
+    // items of one tile where two leave SMs without any (2048 tokens, 12 heads of 64: PERS)
+    const int per = items(kPuBoth) <= ctx->sm_count ? kPuRows : kPuBoth;
+    const long long ctas = items(per);
     if (ctas > 0x3fffffffll) return set_error(ctx, LOOKAT_ERR_UNSUPPORTED, "attend_packed: too many tokens for one call");
-    kern<<<(unsigned)(ctas < ctx->sm_count ? ctas : ctx->sm_count), kPuThreads, Lay::kBytes, ctx->stream>>>(a, k_map, v_map, k_order, v_order, ctx->timeout_flag);
+    kern<<<(unsigned)(ctas < ctx->sm_count ? ctas : ctx->sm_count), kPuThreads, Lay::kBytes, ctx->stream>>>(a, k_map, v_map, per, k_order, v_order, ctx->timeout_flag);
     return check_launch(ctx, "attend_packed_umma_kernel");
 }
 
