@@ -104,11 +104,11 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
         }
         for (int t = 0; t < kPuTiles; ++t) {
             um_bar_init(bar_s + 8 * t, 1);
-            um_bar_init(bar_p + 8 * t, kPuRows);
-            um_bar_init(bar_q + 8 * t, 32);
+            um_bar_init(bar_p + 8 * t, kPuRows / 32);
+            um_bar_init(bar_q + 8 * t, 1);
             um_bar_init(bar_qf + 8 * t, 1);
             um_bar_init(bar_o + 8 * t, 1);
-            um_bar_init(bar_of + 8 * t, kPuRows);
+            um_bar_init(bar_of + 8 * t, kPuRows / 32);
         }
         um_bar_init(bar_t, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -223,12 +223,14 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
                     if (t == 0) continue;
                     asm volatile("cp.async.wait_group 1;" ::: "memory");
                     um_fence_async_smem();
-                    um_bar_arrive(bar_q);
+                    __syncwarp();
+                    if (lane == 0) um_bar_arrive(bar_q);
                     ++seen[0];
                 }
                 asm volatile("cp.async.wait_group 0;" ::: "memory");
                 um_fence_async_smem();
-                um_bar_arrive(bar_q + 8 * t);
+                __syncwarp();
+                if (lane == 0) um_bar_arrive(bar_q + 8 * t);
                 ++seen[t];
             }
             started = true;
@@ -376,7 +378,8 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
                 }
                 um_wait_st();
                 um_fence_before();
-                um_bar_arrive(bar_p + 8 * tile);
+                __syncwarp();
+                if (lane == 0) um_bar_arrive(bar_p + 8 * tile);         // (one of a warp: 128 arrivals at a barrier take their time)
             }
             mine0 += mine;
             const int parity = items++ & 1;
@@ -393,7 +396,8 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
                 um_wait_ld();
                 if (part == DV / 64 - 1) {
                     um_fence_before();
-                    um_bar_arrive(bar_of + 8 * tile);
+                    __syncwarp();
+                    if (lane == 0) um_bar_arrive(bar_of + 8 * tile);
                 }
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
