@@ -8,7 +8,8 @@
 // lines: one tile where there are few items), against chunks of 128 tokens; a persistent CTA per SM goes through every 148th item of the list, which begins with those
 // that see the most tokens (packed_tile).  Tensor memory is full: per tile 128 columns of scores, over whose first half the
 // weights are written, and up to 128 of O.  So a tile's products alternate, S, O, S, O, and while the softmax threads work on
-// one tile the tensor pipe works on the other.  The roles run ahead of each other from item to item, so that an item's queries,
+// one tile the tensor pipe works on the other.  With values of 64 dims there is room for the weights of their own (kApart), and a
+// chunk's scores are made while the softmax threads work on the one before.  The roles run ahead of each other from item to item, so that an item's queries,
 // keys and first scores are there when the one before is written out (12 warps, one CTA per SM by tensor memory):
 //   warps 0-3 / 4-7  softmax of tile 0 / 1: thread r owns line r of its tile = tensor-memory lane r;
 //   warp 8      fetches keys and values by tiled bulk copies, 128 tokens x 64 dims with the 128-byte swizzle, through maps over
@@ -39,8 +40,10 @@ struct PuLayout {
     static constexpr int kK = kKb * kBox, kV = kVb * kBox, kQ = kPuRows * 2 * DK;
     static constexpr int kOffK = 0, kOffV = kStages * kK, kOffQ = kOffV + kStages * kV;
     static constexpr int kTurn = 4096, kOffTurn = kOffQ + kPuTiles * kQ, kOffBars = kOffTurn + kPuSoftmax / 32 * kTurn;     // turn: a warp's results on their way out
-    static constexpr int kOffItems = kOffBars + 256, kBytes = kOffItems + kPuListed * 16;
-    static constexpr int kColO = kPuTiles * kPuChunk;
+    static constexpr int kOffItems = kOffBars + 512, kBytes = kOffItems + kPuListed * 16;
+    // tensor memory: scores of both tiles, O of both, and where that leaves room (kApart) the weights of both beside the scores
+    static constexpr bool kApart = DV == 64;
+    static constexpr int kColO = kPuTiles * kPuChunk, kColP = kColO + kPuTiles * DV;
     // instruction descriptors: fp32 accumulate, fp16 operands, N >> 3 at bit 17, M >> 4 at bit 24; bit 16: B is MN-major
     static constexpr uint32_t kIdescS = (1u << 4) | ((uint32_t)(kPuChunk >> 3) << 17) | ((uint32_t)(kPuRows >> 4) << 24);
     static constexpr uint32_t kIdescO = (1u << 4) | (1u << 16) | ((uint32_t)(DV >> 3) << 17) | ((uint32_t)(kPuRows >> 4) << 24);
@@ -87,11 +90,11 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
     uint64_t *const bars = reinterpret_cast<uint64_t *>(sm + Lay::kOffBars);
     uint32_t *const tmem_slot = reinterpret_cast<uint32_t *>(bars + 30);
     // per stage: keys there, keys free, values there, values free; per tile: scores done and weights stored (of each of its
-    // chunks), queries there, queries free, O done, O read (of each of its items); copies of a row's last values there.  A phase of each
+    // chunks; with kApart also scores read, value MMAs done), queries there, queries free, O done, O read (of each of its items); copies of a row's last values there.  A phase of each
     // ends only after every waiter of the one before has moved on.
     const uint32_t bar0 = um_smem(bars), bar_k = bar0, bar_kf = bar0 + 32, bar_v = bar0 + 64, bar_vf = bar0 + 96;
     const uint32_t bar_s = bar0 + 128, bar_p = bar0 + 144, bar_q = bar0 + 160, bar_qf = bar0 + 176, bar_o = bar0 + 192, bar_of = bar0 + 208;
-    const uint32_t bar_t = bar0 + 224;
+    const uint32_t bar_t = bar0 + 224, bar_sf = bar0 + 256, bar_pv = bar0 + 272;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (blockIdx.x == 0) packed_check(a.rows, tid, kPuThreads);
@@ -106,6 +109,8 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
             um_bar_init(bar_s + 8 * t, 1);
             um_bar_init(bar_p + 8 * t, kPuRows / 32);
             um_bar_init(bar_q + 8 * t, 1);
+            um_bar_init(bar_sf + 8 * t, kPuRows / 32);
+            um_bar_init(bar_pv + 8 * t, 1);
             um_bar_init(bar_qf + 8 * t, 1);
             um_bar_init(bar_o + 8 * t, 1);
             um_bar_init(bar_of + 8 * t, kPuRows / 32);
@@ -245,15 +250,16 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
         const uint32_t k_lo = ((sm0 + Lay::kOffK) >> 4) | (1u << 16);                              // leading offset unused (16 B)
         const uint32_t q_lo = ((sm0 + Lay::kOffQ + t * Lay::kQ) >> 4) | (1u << 16);
         const uint32_t v_lo = ((sm0 + Lay::kOffV) >> 4) | ((uint32_t)(Lay::kBox / 16) << 16);      // between 64-column blocks
-        const uint32_t tm_s = tmem + t * kPuChunk, tm_o = tmem + Lay::kColO + t * DV;
+        const uint32_t tm_s = tmem + t * kPuChunk, tm_o = tmem + Lay::kColO + t * DV, tm_p = Lay::kApart ? tmem + Lay::kColP + t * (kPuChunk / 2) : tm_s;
         int chunk0 = 0, mine0 = 0, items = 0;                  // chunks of all items so far, the tile's own, its items
         while (!dead && next()) {
             const int mine = chunks_of(t);
             if (um_elect()) {
+                // (waits that are over already go first: between a tile's weights and its next scores there is nothing but the MMAs)
+                auto keys_there = [&](int ch) { return um_bar_wait(bar_k + 8 * ((chunk0 + ch) % kStages), ((chunk0 + ch) / kStages) & 1); };
+                auto values_there = [&](int ch) { return um_bar_wait(bar_v + 8 * ((chunk0 + ch) % kStages), ((chunk0 + ch) / kStages) & 1); };
                 auto score_mma = [&](int ch) {
                     const int st = (chunk0 + ch) % kStages;
-                    if (!um_bar_wait(bar_k + 8 * st, ((chunk0 + ch) / kStages) & 1)) return false;
-                    um_fence_after();
                     const uint32_t lo = k_lo + st * (Lay::kK >> 4);
 #pragma unroll
                     for (int ks = 0; ks < DK / 16; ++ks) {
@@ -264,26 +270,40 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
                     um_commit(bar_s + 8 * t);
                     um_commit(bar_kf + 8 * st);
                     if (ch == mine - 1) um_commit(bar_qf + 8 * t);
-                    return true;
                 };
                 auto value_mma = [&](int ch) {
                     const int st = (chunk0 + ch) % kStages;
-                    if (!um_bar_wait(bar_p + 8 * t, (mine0 + ch) & 1) || !um_bar_wait(bar_v + 8 * st, ((chunk0 + ch) / kStages) & 1)) return false;
-                    if (ch == 0 && items && !um_bar_wait(bar_of + 8 * t, (items - 1) & 1)) return false;
-                    um_fence_after();
                     const uint32_t lo = v_lo + st * (Lay::kV >> 4);
 #pragma unroll
                     for (int kt = 0; kt < kPuChunk / 16; ++kt) {
-                        if (kt == 0 && ch == 0) um_mma_ts<false>(tm_o, tm_s, lo, desc_hi, Lay::kIdescO);
-                        else um_mma_ts<true>(tm_o, tm_s + kt * 8, lo + kt * (2048 >> 4), desc_hi, Lay::kIdescO);
+                        if (kt == 0 && ch == 0) um_mma_ts<false>(tm_o, tm_p, lo, desc_hi, Lay::kIdescO);
+                        else um_mma_ts<true>(tm_o, tm_p + kt * 8, lo + kt * (2048 >> 4), desc_hi, Lay::kIdescO);
                     }
+                    if (Lay::kApart) um_commit(bar_pv + 8 * t);
                     um_commit(bar_vf + 8 * st);
-                    return true;
                 };
                 bool ok = true;
                 if (mine) {
-                    ok = um_bar_wait(bar_q + 8 * t, items & 1) && score_mma(0);
-                    for (int ch = 0; ok && ch < mine; ++ch) ok = value_mma(ch) && (ch + 1 >= mine || score_mma(ch + 1));
+                    ok = keys_there(0) && um_bar_wait(bar_q + 8 * t, items & 1) && (!Lay::kApart || !mine0 || um_bar_wait(bar_sf + 8 * t, (mine0 - 1) & 1));
+                    if (ok) {
+                        um_fence_after();
+                        score_mma(0);
+                    }
+                    ok = ok && (!items || um_bar_wait(bar_of + 8 * t, (items - 1) & 1));
+                    for (int ch = 0; ok && ch < mine; ++ch) {
+                        const bool last = ch + 1 >= mine;
+                        if (Lay::kApart && !last) {            // the next scores while the softmax threads work on these
+                            ok = keys_there(ch + 1) && um_bar_wait(bar_sf + 8 * t, (mine0 + ch) & 1);
+                            if (!ok) break;
+                            um_fence_after();
+                            score_mma(ch + 1);
+                        }
+                        ok = values_there(ch) && (Lay::kApart || last || keys_there(ch + 1)) && um_bar_wait(bar_p + 8 * t, (mine0 + ch) & 1);
+                        if (!ok) break;
+                        um_fence_after();
+                        value_mma(ch);
+                        if (!Lay::kApart && !last) score_mma(ch + 1);
+                    }
                     if (ok) um_commit(bar_o + 8 * t);
                 }
                 for (int ch = mine; ok && ch < n_chunks; ++ch) {               // chunks that only the other tile sees
@@ -305,6 +325,7 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
         const int tile = warp >> 2;
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
         const uint32_t tm_s = tmem + tile * kPuChunk + lane_base, tm_o = tmem + Lay::kColO + tile * DV + lane_base;
+        const uint32_t tm_p = Lay::kApart ? tmem + Lay::kColP + tile * (kPuChunk / 2) + lane_base : tm_s;
         unsigned char *const turn = sm + Lay::kOffTurn + warp * Lay::kTurn;
         int mine0 = 0, items = 0;                              // the tile's chunks and items so far
         bool more = next();
@@ -329,6 +350,11 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
 #pragma unroll
                     for (int i = 0; i < kPuChunk / 2; ++i) y[i] = make_float2(__uint_as_float(s[i / 16][2 * i % 32]), __uint_as_float(s[i / 16][2 * i % 32 + 1]));
                 }
+                if (Lay::kApart) {
+                    um_fence_before();
+                    __syncwarp();
+                    if (lane == 0) um_bar_arrive(bar_sf + 8 * tile);
+                }
                 const int sees = tok + 1 - ch * kPuChunk;      // tokens of the chunk that this line sees
                 if (__any_sync(0xffffffffu, sees < kPuChunk)) {
 #pragma unroll
@@ -349,6 +375,9 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
                     alpha = ex2_approx(m_run - (top - kPackedLift));
                     m_run = top - kPackedLift;
                 }
+                // the value MMAs of the chunk before are over: with kApart asked for here, else known by these scores, which the same
+                // thread issued after them
+                if (Lay::kApart && mine0 + ch && !__all_sync(0xffffffffu, um_bar_wait(bar_pv + 8 * tile, (mine0 + ch - 1) & 1))) { dead = true; break; }
                 float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
@@ -361,11 +390,11 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
                         const __half2 x = __floats2half2_rn(w.x, w.y);
                         pk[i] = *reinterpret_cast<const uint32_t *>(&x);
                     }
-                    um_st32(tm_s + half * 32, pk);
+                    um_st32(tm_p + half * 32, pk);
                 }
                 l_run = fmaf(l_run, alpha, (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y));
-                // O: this tile's value MMAs so far were over before these scores were (one thread issues both, in order)
                 if (__any_sync(0xffffffffu, alpha != 1.f)) {
+                    um_fence_after();
 #pragma unroll 1
                     for (int p = 0; p < DV / 32; ++p) {
                         uint32_t o[32];
