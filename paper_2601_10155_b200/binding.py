@@ -244,20 +244,21 @@ def _on(t, dtype, name, device, shape=None):
     return p
 
 
-def _rows(t, name, device, shape):
-    """fp16 [tokens][heads][d] with dense vectors, as the library takes packed rows; a view of a wider tensor will do."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA tensor (the library has no CPU path)")
-    if t.dtype is not torch.float16:
-        raise TypeError(f"{name} must have dtype torch.float16, got {t.dtype}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    if t.device != device:
+def _fill(rows, t, name, device, shape):
+    """fp16 [tokens][heads][d] with dense vectors into a lookat_rows; a view of a wider tensor will do."""
+    if not (isinstance(t, torch.Tensor) and t.get_device() == device.index and t.dtype is torch.float16 and t.shape == shape):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda:
+            raise TypeError(f"{name} must be a CUDA tensor (the library has no CPU path)")
+        if t.dtype is not torch.float16:
+            raise TypeError(f"{name} must have dtype torch.float16, got {t.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
         raise ValueError(f"{name} is on {t.device}, the context on {device}")
-    ts, hs, one = t.stride()
+    rows.data = t.data_ptr()
+    rows.token_stride, rows.head_stride, one = t.stride()
     if one != 1 and shape[2] > 1:
         raise ValueError(f"{name}: a vector's elements must lie next to each other")
-    return lookat_rows(t.data_ptr(), ts, hs)
+    return rows
 
 
 class RopeTable:
@@ -277,6 +278,7 @@ class RopeTable:
         self.rotary_dim, self.amplitude = rotary_dim, amplitude.value
         self.host = list(turns)                                 # fractions of 2^64
         self.turns = torch.tensor([t - (1 << 64) if t >> 63 else t for t in self.host], dtype=torch.int64, device=device)
+        self.pointer, self.device = self.turns.data_ptr(), self.turns.device
 
 
 class BeamState:
@@ -290,7 +292,7 @@ class BeamState:
         if tokens is not None and tokens.dim() != 3:
             raise ValueError("tokens must have shape [groups][beams][max_len]")
         self.scores, self.lengths, self.finished, self.tokens = scores, lengths, finished, tokens
-        self.groups, self.beams, self.device = *shape, dev
+        self.groups, self.beams, self.rows, self.device = *shape, shape[0] * shape[1], dev
         max_len = 0 if tokens is None else tokens.shape[2]
         self.c = lookat_beam_state(_dev(scores, torch.float32, "scores"), _on(lengths, i32, "lengths", dev, shape), _on(finished, i32, "finished", dev, shape),
                                    None if max_len == 0 else _on(tokens, i32, "tokens", dev, (*shape, max_len)), *shape, max_len)
@@ -402,6 +404,7 @@ class Lookat:
         self._h = h
         self._shape, self._kv_shape = (n_q_heads, n_kv_heads, d_k, d_v), (n_kv_heads, d_k, d_v)
         self._raw_stream = stream.cuda_stream
+        self._row_args = [lookat_rows() for _ in range(4)]      # filled by every call that takes packed rows
         self.scale = scale if scale > 0 else 1.0 / math.sqrt(d_k)
 
     # -- helpers ---------------------------------------------------------------
@@ -646,8 +649,8 @@ class Lookat:
                                                    _on(remap, torch.int32, "remap", self.device, (state.n_pages,))))
 
     # -- what runs around it (include/lookat_serve.h) --------------------------------
-    def _empty(self, shape, dtype):
-        out = torch.empty(shape, dtype=dtype, device=self.device)
+    def _empty(self, shape, strides, dtype):
+        out = torch.empty_strided(shape, strides, dtype=dtype, device=self.device)     # (takes half the time of empty)
         if torch._C._cuda_getCurrentRawStream(self.device.index) != self._raw_stream:
             out.record_stream(self.stream)                      # allocated for another stream than the one that writes it
         return out
@@ -658,57 +661,73 @@ class Lookat:
         H, H_kv, d, _ = self._shape
         dev = self.device
         T = (k if q is None else q).shape[0]
-        if table.turns.device != dev:
-            raise ValueError(f"the table is on {table.turns.device}, the context on {dev}")
-        args = []
-        for x, heads, name in ((q, H, "q"), (k, H_kv, "k")):
-            args.append(None if x is None else _rows(x, name, dev, (T, heads, d)))
-        if q is not None and q_out is None:
-            q_out = self._empty((T, H, d), torch.float16)
-        if k is not None and k_out is None:
-            k_out = self._empty((T, H_kv, d), torch.float16)
-        outs = [None if x is None else _rows(x, name, dev, (T, heads, d)) for x, heads, name in ((q_out, H, "q_out"), (k_out, H_kv, "k_out"))]
-        self._check(self._lib.lookat_rope(self._h, *args, T, _on(positions, torch.int32, "positions", dev, (T,)), table.turns.data_ptr(), table.rotary_dim,
-                                          1 if interleaved else 0, table.amplitude, *outs))
+        if table.device != dev:
+            raise ValueError(f"the table is on {table.device}, the context on {dev}")
+        r = self._row_args
+        in_q = in_k = to_q = to_k = None
+        if q is not None:
+            shape = (T, H, d)
+            if q_out is None:
+                q_out = self._empty(shape, (H * d, d, 1), torch.float16)
+            in_q, to_q = _fill(r[0], q, "q", dev, shape), _fill(r[1], q_out, "q_out", dev, shape)
+        if k is not None:
+            shape = (T, H_kv, d)
+            if k_out is None:
+                k_out = self._empty(shape, (H_kv * d, d, 1), torch.float16)
+            in_k, to_k = _fill(r[2], k, "k", dev, shape), _fill(r[3], k_out, "k_out", dev, shape)
+        st = self._lib.lookat_rope(self._h, in_q, in_k, T, _on(positions, torch.int32, "positions", dev, (T,)), table.pointer, table.rotary_dim,
+                                   1 if interleaved else 0, table.amplitude, to_q, to_k)
+        if st:
+            self._check(st)
         return q_out, k_out
 
     def lookat_attend_packed(self, q, k, v, starts, out=None):
         """Exact causal attention of packed prompts: q [tokens][H_q][d_k], k [tokens][H_kv][d_k], v [tokens][H_kv][d_v], row b the
         tokens starts[b] .. starts[b + 1] - 1; tokens of no row keep what `out` held."""
         H, H_kv, d_k, d_v = self._shape
-        dev = self.device
-        T, B = q.shape[0], starts.shape[0] - 1
+        dev, r = self.device, self._row_args
+        T, n = q.shape[0], starts.shape[0]
+        shape = (T, H, d_v)
         if out is None:
-            out = self._empty((T, H, d_v), torch.float16)
-        self._check(self._lib.lookat_attend_packed(self._h, _rows(q, "q", dev, (T, H, d_k)), _rows(k, "k", dev, (T, H_kv, d_k)),
-                                                   _rows(v, "v", dev, (T, H_kv, d_v)), T, B, _on(starts, torch.int32, "starts", dev, (B + 1,)),
-                                                   _rows(out, "out", dev, (T, H, d_v))))
+            out = self._empty(shape, (H * d_v, d_v, 1), torch.float16)
+        st = self._lib.lookat_attend_packed(self._h, _fill(r[0], q, "q", dev, (T, H, d_k)), _fill(r[1], k, "k", dev, (T, H_kv, d_k)),
+                                            _fill(r[2], v, "v", dev, (T, H_kv, d_v)), T, n - 1, _on(starts, torch.int32, "starts", dev, (n,)),
+                                            _fill(r[3], out, "out", dev, shape))
+        if st:
+            self._check(st)
         return out
 
     def lookat_q8_append_packed(self, cache, k, v, starts, tables, seq_lens):
         """Quantises the packed tokens starts[b] .. starts[b + 1] - 1 as the newest of row b; k [tokens][H_kv][d_k]."""
         _, H, d_k, d_v = self._shape
-        dev = self.device
+        dev, r = self.device, self._row_args
         B, max_pages, tb, sl = self._q8(cache, tables, seq_lens)
         T = k.shape[0]
-        self._check(self._lib.lookat_q8_append_packed(self._h, cache.c, _rows(k, "k", dev, (T, H, d_k)), _rows(v, "v", dev, (T, H, d_v)), T, B,
-                                                      _on(starts, torch.int32, "starts", dev, (B + 1,)), tb, max_pages, sl))
+        st = self._lib.lookat_q8_append_packed(self._h, cache.c, _fill(r[0], k, "k", dev, (T, H, d_k)), _fill(r[1], v, "v", dev, (T, H, d_v)), T, B,
+                                               _on(starts, torch.int32, "starts", dev, (B + 1,)), tb, max_pages, sl)
+        if st:
+            self._check(st)
 
     def lookat_beam_select(self, state, logits, eos=-1, length_penalty=0.0, next_ids=None, parents=None):
         """One step of beam search over logits [groups * beams][vocab] (rows may lie further apart); the state moves in place.
         Returns (next_ids, parents), int32 [groups * beams]."""
-        dev, rows = self.device, state.groups * state.beams
+        dev, rows, i32 = self.device, state.rows, torch.int32
         if state.device != dev:
             raise ValueError(f"the beams are on {state.device}, the context on {dev}")
         if not isinstance(logits, torch.Tensor) or not logits.is_cuda or logits.dtype is not torch.float32:
             raise TypeError("logits must be a CUDA tensor of dtype torch.float32")
-        if logits.device != dev or logits.dim() != 2 or logits.shape[0] != rows or logits.shape[1] < 1 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        if logits.get_device() != dev.index or logits.dim() != 2 or logits.shape[0] != rows or logits.shape[1] < 1 or \
+                (logits.shape[1] > 1 and logits.stride(1) != 1):
             raise ValueError(f"logits must have shape [{rows}][vocab] with dense rows on {dev}")
         vocab = logits.shape[1]
-        next_ids = self._empty((rows,), torch.int32) if next_ids is None else next_ids
-        parents = self._empty((rows,), torch.int32) if parents is None else parents
-        self._check(self._lib.lookat_beam_select(self._h, state.c, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, vocab, eos, length_penalty,
-                                                 _on(next_ids, torch.int32, "next_ids", dev, (rows,)), _on(parents, torch.int32, "parents", dev, (rows,))))
+        if next_ids is None:
+            next_ids = self._empty((rows,), (1,), i32)
+        if parents is None:
+            parents = self._empty((rows,), (1,), i32)
+        st = self._lib.lookat_beam_select(self._h, state.c, logits.data_ptr(), logits.stride(0) if rows > 1 else vocab, vocab, eos, length_penalty,
+                                          _on(next_ids, i32, "next_ids", dev, (rows,)), _on(parents, i32, "parents", dev, (rows,)))
+        if st:
+            self._check(st)
         return next_ids, parents
 
     def lookat_kernel_launches(self) -> int:
