@@ -660,6 +660,8 @@ class Lookat:
         given, which may be q and k themselves."""
         H, H_kv, d, _ = self._shape
         dev = self.device
+        if q is None and k is None:
+            raise ValueError("q and k are both None")
         T = (k if q is None else q).shape[0]
         if table.device != dev:
             raise ValueError(f"the table is on {table.device}, the context on {dev}")

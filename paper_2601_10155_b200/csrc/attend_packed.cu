@@ -28,9 +28,9 @@ __global__ void __launch_bounds__(kPaThreads) attend_packed_kernel(PackedAttendA
     __half *const qs = pa_smem, *const ks = qs + kPaLines * kPitch, *const vs = ks + kPaBlock * kPitch;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, r = lane >> 2, t = lane & 3;
     const int h = blockIdx.x % a.H_kv;
-    int b, place, first, n;
+    int place, first, n;
     if (blockIdx.x == 0) packed_check(a.rows, tid, kPaThreads);
-    if (!packed_tile(a.rows, a.g, kPaLines, blockIdx.x / a.H_kv, lane, b, place, first, n)) return;
+    if (packed_tile(a.rows, a.g, kPaLines, blockIdx.x / a.H_kv, lane, place, first, n) != kTile) return;
     const int line0 = place * kPaLines, lines = n * a.g;       // (the host sees to it that lines fit 31 bits)
     const __half *const kg = a.k.p + first * a.k.ts + h * a.k.hs, *const vg = a.v.p + first * a.v.ts + h * a.v.hs;
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
@@ -140,8 +140,7 @@ lookat_status launch_pa(Ctx *ctx, const PackedAttendArgs &a)
     auto kern = attend_packed_kernel<DIM>;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes) != cudaSuccess)
         return check_launch(ctx, "attend_packed: shared-memory opt-in");
-    // no more tiles than this, whatever the rows' lengths
-    const long long ctas = ((long long)a.rows.n * a.g / kPaLines + (a.rows.B < a.rows.n ? a.rows.B : a.rows.n)) * a.H_kv;
+    const long long ctas = packed_tiles(a.rows, a.g, kPaLines) * a.H_kv;
     if (ctas > 0x7fffffffll) return set_error(ctx, LOOKAT_ERR_UNSUPPORTED, "attend_packed: too many tokens for one call");
     kern<<<(unsigned)ctas, kPaThreads, kBytes, ctx->stream>>>(a);
     return check_launch(ctx, "attend_packed_kernel");

@@ -122,13 +122,13 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(um_smem(tmem_slot)), "n"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    // ---- the CTA's items: two tiles of a row and KV head each: {first token, tokens of the row, place of the tiles}, no tokens: the end ----
+    // ---- the CTA's items: up to two tiles of a row and KV head each: {first token, tokens of the row, place of the tiles, what packed_tile said} ----
     int4 *const listed = reinterpret_cast<int4 *>(sm + Lay::kOffItems);
     for (int k = warp; k < kPuListed; k += kPuThreads / 32) {
-        int b, place, first, n;
-        const bool some = packed_tile(a.rows, a.g, per, (blockIdx.x + k * gridDim.x) / a.H_kv, lane, b, place, first, n);
-        if (lane == 0) listed[k] = some ? make_int4(first, n, place, 0) : make_int4(0, 0, 0, 0);
-        if (!some) break;                                      // (a warp of an earlier place has met the end, too, or will)
+        int4 item = make_int4(0, 0, 0, 0);
+        item.w = packed_tile(a.rows, a.g, per, (blockIdx.x + k * gridDim.x) / a.H_kv, lane, item.z, item.x, item.y);
+        if (lane == 0) listed[k] = item;
+        if (item.w == kNoMore) break;                          // (a warp of an earlier place has met the end, too, or will)
     }
     um_fence_before();
     __syncthreads();
@@ -139,18 +139,16 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
     // every role goes through the items by itself
     int k = -1, h = 0, first = 0, n = 0, line0 = 0, lines = 0, n_chunks = 0;
     auto next = [&]() {
-        const int at = blockIdx.x + ++k * gridDim.x;
-        int place;
-        if (k < kPuListed) {
-            const int4 item = listed[k];
-            if (item.y == 0) return false;
-            first = item.x, n = item.y, place = item.z;
-        } else {
-            int b;
-            if (!packed_tile(a.rows, a.g, per, at / a.H_kv, lane, b, place, first, n)) return false;
-        }
-        h = at % a.H_kv;
-        line0 = place * per;
+        int4 item;
+        do {
+            ++k;
+            if (k < kPuListed) item = listed[k];
+            else item.w = packed_tile(a.rows, a.g, per, (blockIdx.x + k * gridDim.x) / a.H_kv, lane, item.z, item.x, item.y);
+            if (item.w == kNoMore) return false;
+        } while (item.w == kNoTile);
+        first = item.x, n = item.y;
+        h = (blockIdx.x + k * gridDim.x) % a.H_kv;
+        line0 = item.z * per;
         lines = n * a.g;
         n_chunks = (min(line0 + per, lines) - 1) / a.g / kPuChunk + 1;
         return true;
@@ -205,12 +203,14 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
     } else if (warp == kPuThreads / 32 - 1) {
         // =================== the queries: A operand of the scores, 64 dims each, 128-byte swizzle ===================
         constexpr int kPieces = DK / 8;
-        int seen[kPuTiles] = {0, 0};
+        int seen[kPuTiles] = {0, 0}, chunks = 0;               // chunks: of the item before, all of whose scores this waits for
         bool started = false;
         while (!dead && next()) {
             const int tiles = chunks_of(1) ? 2 : 1;
             for (int t = 0; t < tiles; ++t) {
-                if (seen[t] && !__all_sync(0xffffffffu, um_bar_wait(bar_qf + 8 * t, (seen[t] - 1) & 1))) { dead = true; break; }
+                bool there = seen[t] == 0;
+                for (int i = 0; i <= chunks && !there; ++i) there = __all_sync(0xffffffffu, um_bar_wait(bar_qf + 8 * t, (seen[t] - 1) & 1));
+                if (!there) { dead = true; break; }
 #pragma unroll 1
                 for (int part = 0; part < kPuRows / 32; ++part) {
                     const int line = min(line0 + t * kPuRows + part * 32 + lane, lines - 1);       // lines beyond the last repeat it
@@ -239,6 +239,7 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
                 ++seen[t];
             }
             started = true;
+            chunks = n_chunks;
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
     } else if (warp > kPuSoftmax / 32) {
@@ -470,9 +471,10 @@ lookat_status launch_pu(Ctx *ctx, const PackedAttendArgs &a)
         !make_rows_map_f16(&v_map, a.v.p, DV, a.H_kv, a.rows.n, a.v.hs, a.v.ts, kPuChunk, &v_order))
         return set_error(ctx, LOOKAT_ERR_CUDA, "attend_packed: the driver refused a tensor map");
     // no more tiles than this, whatever the rows' lengths
-    auto items = [&](int per) { return ((long long)a.rows.n * a.g / per + (a.rows.B < a.rows.n ? a.rows.B : a.rows.n)) * a.H_kv; };
-    // items of one tile where two leave SMs without any (2048 tokens, 12 heads of 64: PERS)
-    const int per = items(kPuBoth) <= ctx->sm_count ? kPuRows : kPuBoth;
+    auto items = [&](int per) { return packed_tiles(a.rows, a.g, per) * a.H_kv; };
+    // items of one tile where there is an SM for each (2048 tokens, 8 and 2 heads of 128: 38 us, and 46 with two; 1000 tokens, 32 and 8
+    // heads, where there is not, 34 and 32)
+    const int per = items(kPuRows) <= ctx->sm_count ? kPuRows : kPuBoth;
     const long long ctas = items(per);
     if (ctas > 0x3fffffffll) return set_error(ctx, LOOKAT_ERR_UNSUPPORTED, "attend_packed: too many tokens for one call");
     kern<<<(unsigned)(ctas < ctx->sm_count ? ctas : ctx->sm_count), kPuThreads, Lay::kBytes, ctx->stream>>>(a, k_map, v_map, per, k_order, v_order, ctx->timeout_flag);
@@ -483,8 +485,11 @@ lookat_status launch_pu(Ctx *ctx, const PackedAttendArgs &a)
 
 bool attend_packed_umma_covers(const Ctx *ctx, const PackedAttendArgs &a)
 {
+    // Rows of more than 64 lines (one tile of attend_packed_kernel) on average, as far as the host knows: shorter ones leave most of
+    // two tiles of 128 empty.  16384 tokens, 12 heads of 64: rows of 32 tokens 202 us here and 97 there, of 64 109 and 69, of 128 62
+    // and 77; 32 and 8 heads of 128: rows of 16 306 and 259, of 32 160 and 249.
     const bool dims = (a.d_k == 64 || a.d_k == 128) && (a.d_v == 64 || a.d_v == 128);
-    return dims && ctx->timeout_flag && tile_maps_available();
+    return dims && (long long)a.rows.n * a.g > 64ll * a.rows.B && ctx->timeout_flag && tile_maps_available();
 }
 
 lookat_status launch_attend_packed_umma(Ctx *ctx, const PackedAttendArgs &a)

@@ -49,16 +49,33 @@ __device__ __forceinline__ void packed_check(const Packed &p, int thread, int th
     }
 }
 
-// Tile `item` of all rows' tiles of `per` lines each, a row of n tokens having n * g lines: by falling place within their rows, so
-// that the tiles with the most tokens to attend start first.  Called by a whole warp; false behind the last tile.
-//   With A(x) the number of tiles at place x or later (the sum over rows of tiles - x, where positive), the tile's place is the x
-// with A(x + 1) <= item < A(x), found by bisection, and it is row number item - A(x + 1) of those with more than x tiles.
-__device__ inline bool packed_tile(const Packed &p, int g, int per, int item, int lane, int &b, int &place, int &first, int &n)
+// Tile `item` of all rows' tiles of `per` lines each, a row of n tokens having n * g lines.  Called by a whole warp; kTile, or kNoTile
+// (this number has none, later ones may), or kNoMore.  There are at most n_tokens * g / per + B numbers.
+//   Up to kSortedRows rows: by falling place within their rows, so that the tiles with the most tokens to attend start first.  With
+// A(x) the number of tiles at place x or later (the sum over rows of tiles - x, where positive; below 2^31, as lines are), the tile's
+// place is the x with A(x + 1) <= item < A(x), found by bisection, and it is row number item - A(x + 1) of those with more than x.
+//   More rows: in their order, a row's tiles from number starts * g / per + row on, which a bisection over the rows finds.  (Looking
+// through all rows takes longer than what the order gains: 256 rows of up to 500 tokens, 32 and 8 heads of 128, 622 us by place, 531
+// in their order; 64 rows of up to 1500 698 and 690; 33 rows of up to 2000, 12 heads of 64, 180 and 204.)
+enum { kNoMore = -1, kNoTile = 0, kTile = 1 };
+constexpr int kSortedRows = 64;
+__device__ inline int packed_tile(const Packed &p, int g, int per, int item, int lane, int &place, int &first, int &n)
 {
     auto tiles_of = [&](int row, int &at, int &len) {
         len = row < p.B ? packed_row(p, row, at) : 0;
         return (int)(((long long)len * g + per - 1) / per);
     };
+    if (p.B > kSortedRows) {
+        if (item >= (long long)p.n * g / per + p.B) return kNoMore;
+        auto number0 = [&](int row) { return (long long)min(max(p.starts[row], 0), p.n) * g / per + row; };
+        int lo = 0, hi = p.B;                                   // the last row whose first number is not behind this one
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            (number0(mid) <= item ? lo : hi) = mid;
+        }
+        place = (int)(item - number0(lo));
+        return place >= 0 && place < tiles_of(lo, first, n) ? kTile : kNoTile;
+    }
     int at, len;
     const int mine = tiles_of(lane, at, len);                   // (all there is for up to 32 rows)
     int most = mine;
@@ -76,7 +93,7 @@ __device__ inline bool packed_tile(const Packed &p, int g, int per, int item, in
         return __reduce_add_sync(0xffffffffu, sum);
     };
     int lo = 0, hi = most;                                      // A(lo) > item >= A(hi), if any
-    if (later(0) <= item) return false;
+    if (later(0) <= item) return kNoMore;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         (later(mid) > item ? lo : hi) = mid;
@@ -90,14 +107,19 @@ __device__ inline bool packed_tile(const Packed &p, int g, int per, int item, in
         const int count = __popc(who);
         if (rank < count) {
             const int src = __ffs(__ballot_sync(0xffffffffu, tiles > lo && __popc(who & ((1u << lane) - 1)) == rank)) - 1;
-            b = row0 + src;
             first = __shfl_sync(0xffffffffu, t, src);
             n = __shfl_sync(0xffffffffu, l, src);
-            return true;
+            return kTile;
         }
         rank -= count;
     }
-    return false;
+    return kNoMore;
+}
+
+// numbers that packed_tile is to be asked for, whatever the rows' lengths (by place, there are no tiles of empty rows between)
+inline long long packed_tiles(const Packed &p, int g, int per)
+{
+    return (long long)p.n * g / per + (p.B > kSortedRows || p.B < p.n ? p.B : p.n);
 }
 
 struct PackedAttendArgs {

@@ -37,7 +37,8 @@ def rope_bound(x, amplitude):
 
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("H,H_kv,d,r,scaling", [(12, 12, 64, 64, "none"), (32, 8, 128, 128, "ramp"), (4, 2, 64, 32, "linear"), (5, 1, 48, 20, "base"), (3, 3, 16, 2, "none"),
-                                                (6, 3, 128, 24, "bands"), (2, 2, 256, 256, "none"), (1, 1, 8, 8, "none")])
+                                                (6, 3, 128, 24, "bands"), (2, 2, 256, 256, "none"), (1, 1, 8, 8, "none"), (2, 1, 48, 48, "none"), (4, 2, 24, 16, "none"),
+                                                (6, 2, 112, 96, "linear")])
 @pytest.mark.parametrize("T", [1, 3, 70])
 def test_rope(H, H_kv, d, r, scaling, interleaved, T):
     rng = np.random.default_rng(T + d)
@@ -174,9 +175,25 @@ def test_attend_packed(lens, H, H_kv, d_k, d_v, layout):
 
 @pytest.mark.parametrize("H,H_kv,d", [(3, 1, 64), (32, 8, 128), (2, 2, 32)])
 def test_attend_packed_long_and_many_rows(H, H_kv, d):
+    """Few rows and many, whose tiles are found in different ways; more tiles than a CTA lists; rows short enough for the other form,
+    some of them among long ones."""
     rng = np.random.default_rng(d)
     check_attend(rng, [5000, 2, 700], H, H_kv, d, d)
     check_attend(rng, [int(n) for n in rng.integers(0, 9, 400)], H, H_kv, d, d)
+    check_attend(rng, [int(n) for n in rng.integers(0, 200, 65)], H, H_kv, d, d)
+    check_attend(rng, [0] * 70 + [900] + [1] * 30 + [400, 0], H, H_kv, d, d)
+
+
+def test_attend_packed_more_items_than_a_cta_lists():
+    rng = np.random.default_rng(1)
+    (q, k, v), starts = packed_inputs(rng, [150] * 400, 64, 64, 64, 64, first=0, behind=0)      # 400 * 64 items on at most 148 SMs
+    lk = Lookat(64, 64, 64, 64, 1, 16)
+    out = lk.lookat_attend_packed(q, k, v, i32(starts))
+    assert finding(lk) == ""
+    for b in (0, 7, 199, 399):
+        lo, hi = int(starts[b]), int(starts[b + 1])
+        want, mag, reach = attend_reference(q[lo:hi], k[lo:hi], v[lo:hi], [0, 150], lk.scale)
+        assert bool(((out[lo:hi].double() - want).abs() <= attend_bound(want, mag, reach, 64, 150, float(v.abs().max()))).all())
 
 
 def test_attend_packed_of_the_plain_oracle():
