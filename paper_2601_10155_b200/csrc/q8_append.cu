@@ -33,12 +33,42 @@ struct ApUnit {                                 // 16 new elements
 __device__ __forceinline__ ApUnit ap_load(const uint4 *src)
 {
     const uint4 a = __ldg(src), b = __ldg(src + 1);
-    return {{ap_finite2(a.x), ap_finite2(a.y), ap_finite2(a.z), ap_finite2(a.w), ap_finite2(b.x), ap_finite2(b.y), ap_finite2(b.z), ap_finite2(b.w)}};
+    return {{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
 }
-__device__ __forceinline__ void ap_max(__half2 &top, const ApUnit &u)
+__device__ __forceinline__ void ap_finite(ApUnit &u)
 {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = __hmax2(top, __habs2(*reinterpret_cast<const __half2 *>(&u.w[i])));
+    for (int i = 0; i < 8; ++i) u.w[i] = ap_finite2(u.w[i]);
+}
+// magnitudes as whole numbers, which go in the same order; infinities are 0x7c00, NaN more
+__device__ __forceinline__ void ap_max(uint32_t &top, const ApUnit &u)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = __vmaxu2(top, u.w[i] & 0x7fff7fffu);
+}
+__device__ __forceinline__ uint32_t ap_higher(uint32_t top) { return max(top & 0xffffu, top >> 16); }
+
+__device__ __forceinline__ unsigned long long ap_two(float x, float y)
+{
+    unsigned long long p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(x), "f"(y));
+    return p;
+}
+__device__ __forceinline__ float2 ap_each(unsigned long long p)
+{
+    float2 x;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x.x), "=f"(x.y) : "l"(p));
+    return x;
+}
+__device__ __forceinline__ unsigned long long ap_mul(unsigned long long a, unsigned long long b)
+{
+    asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(a) : "l"(b));
+    return a;
+}
+__device__ __forceinline__ unsigned long long ap_fma(unsigned long long a, unsigned long long b, unsigned long long c)
+{
+    asm("fma.rn.f32x2 %0, %0, %1, %2;" : "+l"(a) : "l"(b), "l"(c));
+    return a;
 }
 
 // 16 new elements to 16 bytes; amax > 0, scale = R / amax rounded
@@ -51,34 +81,40 @@ __device__ __forceinline__ uint4 ap_round16(const ApUnit &u, float amax, float s
     if constexpr (FORMAT == LOOKAT_Q8_INT8) {
         constexpr float kMagic = 12582912.f;    // 1.5 * 2^23: the sum's low bits are the rounded number
         const float half = 0.5f * amax;
+        const unsigned long long scale2 = ap_two(scale, scale), magic2 = ap_two(kMagic, kMagic), minus2 = ap_two(-1.f, -1.f),
+                                 amax2 = ap_two(amax, amax), R2 = ap_two(R, R);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             uint32_t t[4];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&u.w[2 * i + j]));
-                const float a = fmaf(x.x, scale, kMagic), b = fmaf(x.y, scale, kMagic);
+                const float2 xf = __half22float2(*reinterpret_cast<const __half2 *>(&u.w[2 * i + j]));
+                const unsigned long long x = ap_two(xf.x, xf.y), a = ap_fma(x, scale2, magic2);
                 // what is left of R x, exactly: half of amax or more only at a tie
-                tie |= fabsf(fmaf(kMagic - a, amax, R * x.x)) >= half || fabsf(fmaf(kMagic - b, amax, R * x.y)) >= half;
-                t[2 * j] = __float_as_uint(a);
-                t[2 * j + 1] = __float_as_uint(b);
+                const float2 left = ap_each(ap_fma(ap_fma(a, minus2, magic2), amax2, ap_mul(x, R2))), n = ap_each(a);
+                tie |= fmaxf(fabsf(left.x), fabsf(left.y)) >= half;
+                t[2 * j] = __float_as_uint(n.x);
+                t[2 * j + 1] = __float_as_uint(n.y);
             }
             o[i] = __byte_perm(__byte_perm(t[0], t[1], 0x0040), __byte_perm(t[2], t[3], 0x0040), 0x5410);
         }
     } else {
-        constexpr float kUp = 1.f + 0x1p-21f, kDown = 1.f - 0x1p-21f;
+        const float up = scale * (1.f + 0x1p-21f), down = scale * (1.f - 0x1p-21f);
+        const unsigned long long up2 = ap_two(up, up), down2 = ap_two(down, down);
+        uint32_t differ = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             uint32_t t[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&u.w[2 * i + j]));
-                const float2 r = make_float2(x.x * scale, x.y * scale);
-                t[j] = __nv_cvt_float2_to_fp8x2(make_float2(r.x * kUp, r.y * kUp), __NV_SATFINITE, __NV_E4M3);
-                tie |= t[j] != __nv_cvt_float2_to_fp8x2(make_float2(r.x * kDown, r.y * kDown), __NV_SATFINITE, __NV_E4M3);
+                const float2 xf = __half22float2(*reinterpret_cast<const __half2 *>(&u.w[2 * i + j]));
+                const unsigned long long x = ap_two(xf.x, xf.y);
+                t[j] = __nv_cvt_float2_to_fp8x2(ap_each(ap_mul(x, up2)), __NV_SATFINITE, __NV_E4M3);
+                differ |= t[j] ^ __nv_cvt_float2_to_fp8x2(ap_each(ap_mul(x, down2)), __NV_SATFINITE, __NV_E4M3);
             }
             o[i] = t[0] | t[1] << 16;
         }
+        tie = differ != 0;
     }
     if (tie) {
 #pragma unroll
@@ -126,18 +162,19 @@ __global__ void __launch_bounds__(THREADS == 32 ? 128 : THREADS, THREADS == 256 
     int j, which, b, h, start = 0;
     long long bh = 0;
     if constexpr (PACKED) {                                     // [slot][head][K or V]
+        const unsigned pair = (unsigned)item >> 1;              // (fewer than 2^31 items)
         which = (int)(item & 1);
-        h = (int)((item >> 1) % c.H_kv);
-        const long long slot = (item >> 1) / c.H_kv;
+        h = (int)(pair % (unsigned)c.H_kv);
+        const int slot = (int)(pair / (unsigned)c.H_kv);
         if (slot >= blocks_per_row) return;                     // (here the number of slots; whole groups leave)
-        auto slot0 = [&](int row) { return (long long)(min(max(__ldg(a.starts + row), 0), a.n) >> c.page_shift) + 2ll * row; };
+        auto slot0 = [&](int row) { return (min(max(__ldg(a.starts + row), 0), a.n) >> c.page_shift) + 2 * row; };
         int lo = 0, hi = a.B;                                   // the last row whose first slot is not behind this one
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             (slot0(mid) <= slot ? lo : hi) = mid;
         }
         b = lo;
-        j = (int)(slot - slot0(b));
+        j = slot - slot0(b);
         if (j < 0) return;
     } else {
         j = (int)(item % blocks_per_row), which = (int)(item / blocks_per_row & 1);
@@ -184,7 +221,7 @@ __global__ void __launch_bounds__(THREADS == 32 ? 128 : THREADS, THREADS == 256 
     };
 
     ApUnit keep[kApKeep];
-    __half2 tops2 = __halves2half2(__ushort_as_half(0), __ushort_as_half(0));
+    uint32_t tops2 = 0;
 #pragma unroll
     for (int i = 0; i < kApKeep; ++i) {
         const int u = lane + i * THREADS;
@@ -194,7 +231,7 @@ __global__ void __launch_bounds__(THREADS == 32 ? 128 : THREADS, THREADS == 256 
         }
     }
     for (int u = lane + kApKeep * THREADS; u < units; u += THREADS) ap_max(tops2, load(u));
-    float top = fmaxf(__low2float(tops2), __high2float(tops2));
+    uint32_t top = ap_higher(tops2);
     if (pid < 0 || pid >= c.n_pages) {                          // (the same for the whole group)
         if (lane == 0) q8_report(c.status, kStatusBadPage);
         return;
@@ -204,16 +241,36 @@ __global__ void __launch_bounds__(THREADS == 32 ? 128 : THREADS, THREADS == 256 
     float *amax_at = (which ? c.v_amax : c.k_amax) + block;
     float was = 0.f;
     if (old > 0) was = fmaxf(*amax_at, 0.f);
+    // the group's largest; where that is an infinity or a NaN, the numbers are made finite and it is taken again
+    __shared__ uint32_t tops[2][THREADS / 32];
+    auto of_group = [&](uint32_t mine, int round) {
+        mine = __reduce_max_sync(0xffffffffu, mine);
+        if constexpr (THREADS > 32) {
+            if ((threadIdx.x & 31) == 0) tops[round][threadIdx.x >> 5] = mine;
+            __syncthreads();                                    // (also: everyone has read *amax_at)
 #pragma unroll
-    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if constexpr (THREADS > 32) {
-        __shared__ float tops[THREADS / 32];
-        if ((threadIdx.x & 31) == 0) tops[threadIdx.x >> 5] = top;
-        __syncthreads();                                        // (also: everyone has read *amax_at)
+            for (int i = 0; i < THREADS / 32; ++i) mine = max(mine, tops[round][i]);
+        }
+        return mine;
+    };
+    top = of_group(top, 0);
+    const bool odd = top >= 0x7c00u;                            // (the same for the whole group)
+    if (odd) {
+        tops2 = 0;
 #pragma unroll
-        for (int i = 0; i < THREADS / 32; ++i) top = fmaxf(top, tops[i]);
+        for (int i = 0; i < kApKeep; ++i)
+            if (lane + i * THREADS < units) {
+                ap_finite(keep[i]);
+                ap_max(tops2, keep[i]);
+            }
+        for (int u = lane + kApKeep * THREADS; u < units; u += THREADS) {
+            ApUnit more = load(u);
+            ap_finite(more);
+            ap_max(tops2, more);
+        }
+        top = of_group(ap_higher(tops2), 1);
     }
-    const float now = fmaxf(was, top);
+    const float now = fmaxf(was, __half2float(__ushort_as_half((unsigned short)top)));
 
     if (now > was && old > 0 && was > 0.f) {                    // (with was = 0 the earlier numbers are all 0)
         uint4 *o = reinterpret_cast<uint4 *>(base);
@@ -226,8 +283,11 @@ __global__ void __launch_bounds__(THREADS == 32 ? 128 : THREADS, THREADS == 256 
         const int u = lane + i * THREADS;
         if (u < units) dst[u] = now > 0.f ? ap_round16<FORMAT>(keep[i], now, scale) : make_uint4(0u, 0u, 0u, 0u);
     }
-    for (int u = lane + kApKeep * THREADS; u < units; u += THREADS)
-        dst[u] = now > 0.f ? ap_round16<FORMAT>(load(u), now, scale) : make_uint4(0u, 0u, 0u, 0u);
+    for (int u = lane + kApKeep * THREADS; u < units; u += THREADS) {
+        ApUnit more = load(u);
+        if (odd) ap_finite(more);
+        dst[u] = now > 0.f ? ap_round16<FORMAT>(more, now, scale) : make_uint4(0u, 0u, 0u, 0u);
+    }
     if constexpr (THREADS == 32) __syncwarp();
     if (lane == 0) *amax_at = now;
 }
@@ -243,7 +303,7 @@ lookat_status launch_q8_append(Ctx *ctx, const Q8AppendArgs &a)
     const int d = a.c.d_k > a.c.d_v ? a.c.d_k : a.c.d_v, units = (a.n < page ? a.n : page) * d / 16;     // of the largest group
     const int threads = units <= 32 * kApKeep ? 32 : units <= 128 * kApKeep ? 128 : 256;
     const long long ctas = threads == 32 ? (items + 3) / 4 : items;
-    if (ctas > 0x7fffffffll) return set_error(ctx, LOOKAT_ERR_UNSUPPORTED, "q8_append: too many blocks for one call");
+    if (ctas > 0x7fffffffll || (a.starts && items > 0x7fffffffll)) return set_error(ctx, LOOKAT_ERR_UNSUPPORTED, "q8_append: too many blocks for one call");
     auto launch = [&](auto kern) { kern<<<(unsigned)ctas, threads == 32 ? 128 : threads, 0, ctx->stream>>>(a, blocks); };
     auto sized = [&](auto format, auto packed) {
         constexpr int F = decltype(format)::value;
