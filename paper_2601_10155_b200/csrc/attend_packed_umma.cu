@@ -16,7 +16,8 @@
 //               the caller's strides; in the row's last chunk it zeroes the values behind the last token (a copy brings the next
 //               row's tokens along, whose infinities the weights of zero would not take away);
 //   warps 9, 10 one thread each issues the MMAs of tile 0 / 1 and commits them to mbarriers;
-//   warp 11     fetches the query lines (cp.async: any strides and groups).
+//   warp 11     fetches the query lines: by tiled bulk copies where a tile's lines are whole tokens of [tokens][heads][dims], else
+//               by cp.async (any strides and groups).
 // Every mbarrier wait gives up after a bounded number of polls, raises the context's time-out flag and lets the CTA drain and
 // free its tensor memory.
 #include <cuda.h>           // CUtensorMap only
@@ -79,8 +80,9 @@ __device__ __forceinline__ void pu_copy(uint32_t dst, const CUtensorMap *map, in
 
 template <int DK, int DV>
 __global__ void __launch_bounds__(kPuThreads, 1)
-attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, int per,
-                          int k_order, int v_order, int *__restrict__ timeout_flag)
+attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+                          const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap out_map,
+                          int q_boxes, int out_boxes /* 0: none, 2: map over [heads][tokens] */, int per, int k_order, int v_order, int *__restrict__ timeout_flag)
 {
     using Lay = PuLayout<DK, DV>;
     constexpr int kStages = Lay::kStages;
@@ -211,6 +213,17 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
                 bool there = seen[t] == 0;
                 for (int i = 0; i <= chunks && !there; ++i) there = __all_sync(0xffffffffu, um_bar_wait(bar_qf + 8 * t, (seen[t] - 1) & 1));
                 if (!there) { dead = true; break; }
+                if (q_boxes) {                                 // (tokens behind the row's end are lines that are not written)
+                    if (um_elect()) {
+                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar_q + 8 * t), "r"(Lay::kQ) : "memory");
+#pragma unroll
+                        for (int i = 0; i < Lay::kKb; ++i)
+                            pu_copy(sm0 + Lay::kOffQ + t * Lay::kQ + i * (kPuRows * 128), &q_map, i * 64, h * a.g, first + (line0 + t * kPuRows) / a.g, q_boxes == 2, bar_q + 8 * t);
+                    }
+                    __syncwarp();
+                    ++seen[t];
+                    continue;
+                }
 #pragma unroll 1
                 for (int part = 0; part < kPuRows / 32; ++part) {
                     const int line = min(line0 + t * kPuRows + part * 32 + lane, lines - 1);       // lines beyond the last repeat it
@@ -241,7 +254,11 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
             started = true;
             chunks = n_chunks;
         }
+        // copies in flight end before the CTA does
         asm volatile("cp.async.wait_all;" ::: "memory");
+        if (q_boxes && dead)
+            for (int t = 0; t < kPuTiles; ++t)
+                if (seen[t]) um_bar_wait(bar_q + 8 * t, (seen[t] - 1) & 1);
     } else if (warp > kPuSoftmax / 32) {
         // =================== the MMA thread of a tile ===================
         const int t = warp - kPuSoftmax / 32 - 1;
@@ -338,6 +355,9 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
             }
             const int tok = line_c / a.g;                      // (lines beyond the last repeat it)
             const unsigned long long out = line < lines ? reinterpret_cast<unsigned long long>(a.out.p + (first + tok) * a.out.ts + (h * a.g + line_c % a.g) * a.out.hs) : 0;
+            // (all of the warp's lines are the row's, and in one box)
+            const int line_w = line0 + tile * kPuRows + (warp & 3) * 32, box_head = h * a.g, box_token = first + line_w / a.g;
+            const bool boxed = out_boxes && line_w + 32 <= lines;
             float m_run = 0.f, l_run = 0.f;
             for (int ch = 0; ch < mine; ++ch) {
                 if (!__all_sync(0xffffffffu, um_bar_wait(bar_s + 8 * tile, (mine0 + ch) & 1))) { dead = true; break; }     // warp-uniform
@@ -429,6 +449,8 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
                     __syncwarp();
                     if (lane == 0) um_bar_arrive(bar_of + 8 * tile);
                 }
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");         // the copy before has read them
+                __syncwarp();
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const uint32_t *const w = &o[i >> 2][(i & 3) * 8];
@@ -438,6 +460,17 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
                     x.z = q8_half2(__uint_as_float(w[4]) * inv, __uint_as_float(w[5]) * inv);
                     x.w = q8_half2(__uint_as_float(w[6]) * inv, __uint_as_float(w[7]) * inv);
                     *reinterpret_cast<uint4 *>(turn + lane * 128 + ((i ^ (lane & 7)) << 4)) = x;
+                }
+                if (boxed) {
+                    um_fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) {
+                        asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(&out_map), "r"(part * 64),
+                                     "r"(out_boxes == 2 ? box_token : box_head), "r"(out_boxes == 2 ? box_head : box_token), "r"(um_smem(turn))
+                                     : "memory");
+                        asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                    }
+                    continue;
                 }
                 __syncwarp();
 #pragma unroll
@@ -450,6 +483,7 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
                 __syncwarp();
             }
         }
+        if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");      // (results on their way out)
     }
 
     if (dead) atomicExch(timeout_flag, 1);
@@ -465,19 +499,30 @@ lookat_status launch_pu(Ctx *ctx, const PackedAttendArgs &a)
     auto kern = attend_packed_umma_kernel<DK, DV>;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kBytes) != cudaSuccess)
         return check_launch(ctx, "attend_packed (tcgen05 form): shared-memory opt-in");
-    CUtensorMap k_map, v_map;
-    int k_order, v_order;
-    if (!make_rows_map_f16(&k_map, a.k.p, DK, a.H_kv, a.rows.n, a.k.hs, a.k.ts, kPuChunk, &k_order) ||
-        !make_rows_map_f16(&v_map, a.v.p, DV, a.H_kv, a.rows.n, a.v.hs, a.v.ts, kPuChunk, &v_order))
+    CUtensorMap k_map, v_map, q_map, out_map;
+    int k_order, v_order, q_order = 0, out_order = 0;
+    if (!make_rows_map_f16(&k_map, a.k.p, DK, a.H_kv, a.rows.n, a.k.hs, a.k.ts, 1, kPuChunk, &k_order) ||
+        !make_rows_map_f16(&v_map, a.v.p, DV, a.H_kv, a.rows.n, a.v.hs, a.v.ts, 1, kPuChunk, &v_order))
         return set_error(ctx, LOOKAT_ERR_CUDA, "attend_packed: the driver refused a tensor map");
     // no more tiles than this, whatever the rows' lengths
+    // a tile's lines in one box: g heads of 128 / g tokens, heads innermost
+    const bool whole = kPuRows % a.g == 0 &&
+                       make_rows_map_f16(&q_map, a.q.p, DK, a.H_q, a.rows.n, a.q.hs, a.q.ts, a.g, kPuRows / a.g, &q_order);
+    const int q_boxes = whole && (!q_order || a.g == 1);
+    if (!q_boxes) q_map = k_map;                               // (not used)
+    // a warp's lines of results, 64 dims, likewise
+    const bool out_whole = 32 % a.g == 0 &&
+                           make_rows_map_f16(&out_map, a.out.p, DV, a.H_q, a.rows.n, a.out.hs, a.out.ts, a.g, 32 / a.g, &out_order);
+    const int out_boxes = out_whole && (!out_order || a.g == 1);
+    if (!out_boxes) out_map = k_map;
     auto items = [&](int per) { return packed_tiles(a.rows, a.g, per) * a.H_kv; };
     // items of one tile where there is an SM for each (2048 tokens, 8 and 2 heads of 128: 38 us, and 46 with two; 1000 tokens, 32 and 8
     // heads, where there is not, 34 and 32)
     const int per = items(kPuRows) <= ctx->sm_count ? kPuRows : kPuBoth;
     const long long ctas = items(per);
     if (ctas > 0x3fffffffll) return set_error(ctx, LOOKAT_ERR_UNSUPPORTED, "attend_packed: too many tokens for one call");
-    kern<<<(unsigned)(ctas < ctx->sm_count ? ctas : ctx->sm_count), kPuThreads, Lay::kBytes, ctx->stream>>>(a, k_map, v_map, per, k_order, v_order, ctx->timeout_flag);
+    kern<<<(unsigned)(ctas < ctx->sm_count ? ctas : ctx->sm_count), kPuThreads, Lay::kBytes, ctx->stream>>>(a, k_map, v_map, q_map, out_map, q_boxes ? 1 + q_order : 0,
+                                                                                                   out_boxes ? 1 + out_order : 0, per, k_order, v_order, ctx->timeout_flag);
     return check_launch(ctx, "attend_packed_umma_kernel");
 }
 

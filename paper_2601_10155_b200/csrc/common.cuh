@@ -203,10 +203,10 @@ struct LinearArgs {
 bool tile_maps_available();
 bool make_tile_map_f16(void *map, const void *base, unsigned long long inner, unsigned long long rows, unsigned box_inner,
                        unsigned box_rows);
-// the same over packed rows: vectors of d halfs at strides (in halfs) by head and by token, boxes of box_tokens tokens x 64 halfs of
-// one head.  Coordinates are (dim, head, token), or (dim, token, head) where *heads_last says so.
+// the same over packed rows: vectors of d halfs at strides (in halfs) by head and by token, boxes of box_tokens tokens x
+// box_heads heads x 64 halfs.  Coordinates are (dim, head, token), or (dim, token, head) where *heads_last says so.
 bool make_rows_map_f16(void *map, const void *base, int d, int heads, long long tokens, long long head_stride, long long token_stride,
-                       int box_tokens, int *heads_last);
+                       int box_heads, int box_tokens, int *heads_last);
 lookat_status launch_linear(Ctx *ctx, const void *x, int x_fp32, const __half *w_t, LinearArgs p);
 lookat_status launch_embed(Ctx *ctx, const int32_t *ids, const __half *wte, const __half *wpe, float *x, long long rows, int T,
                            int pos0, int d, int vocab);

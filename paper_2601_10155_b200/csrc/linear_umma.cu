@@ -417,7 +417,7 @@ bool make_tile_map_f16(void *map, const void *base, unsigned long long inner, un
 }
 
 bool make_rows_map_f16(void *map, const void *base, int d, int heads, long long tokens, long long head_stride, long long token_stride,
-                       int box_tokens, int *heads_last)
+                       int box_heads, int box_tokens, int *heads_last)
 {
     tensor_map_encode_fn encode = tensor_map_encoder();
     if (!encode) return false;
@@ -428,7 +428,7 @@ bool make_rows_map_f16(void *map, const void *base, int d, int heads, long long 
     dims[h] = (cuuint64_t)heads, dims[t] = (cuuint64_t)tokens;
     strides[h - 1] = hs, strides[t - 1] = ts;
     cuuint32_t box[3] = {64, 1, 1}, estr[3] = {1, 1, 1};
-    box[t] = (cuuint32_t)box_tokens;
+    box[h] = (cuuint32_t)box_heads, box[t] = (cuuint32_t)box_tokens;
     return encode(static_cast<CUtensorMap *>(map), CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr,
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
