@@ -32,6 +32,10 @@ namespace {
 constexpr int kPuRows = 128, kPuChunk = 128, kPuTiles = 2, kPuBoth = kPuTiles * kPuRows;
 constexpr int kPuSoftmax = kPuBoth, kPuThreads = kPuSoftmax + 128;
 constexpr float kPuSlack = 8.f;
+// Registers: the softmax threads hold 128 scores each.  The launch's 168 of each thread are split anew (2 x 128 x 208 + 128 x 88 is what
+// 384 x 168 is): 4 x 4096 tokens, 32 and 8 heads of 128, 524 -> 500 us, 23 ragged rows 215 -> 198.
+constexpr int kPuLaunchRegs = 168, kPuSoftmaxRegs = 208, kPuOtherRegs = 88;
+static_assert(kPuSoftmax * kPuSoftmaxRegs + (kPuThreads - kPuSoftmax) * kPuOtherRegs <= kPuThreads * kPuLaunchRegs, "register split");
 constexpr int kPuListed = 128;                  // items that a CTA finds at its start, with all its warps; later ones every role finds by itself
 
 template <int DK, int DV>
@@ -159,186 +163,190 @@ attend_packed_umma_kernel(const __grid_constant__ PackedAttendArgs a, const __gr
 
     if (dead) {
         // misaligned shared-memory base: nothing runs
-    } else if (warp == kPuSoftmax / 32) {
-        // =================== the fetcher ===================
-        // A row's last values, where it ends inside a chunk, come by a barrier of their own; with zeros behind them they are handed
-        // on.
-        int sent = 0, v_sent = 0, tails = 0;                   // chunks of keys, of values, of those with an end
-        while (!dead && next()) {
-            const int tail = n - (n_chunks - 1) * kPuChunk;
-            if (um_elect()) {
-                for (int ch = 0; ch < n_chunks; ++ch) {
-                    const int st = sent % kStages, t0 = first + ch * kPuChunk;
-                    const uint32_t done = (sent / kStages - 1) & 1, v_bar = ch == n_chunks - 1 && tail < kPuChunk ? bar_t : bar_v + 8 * st;
-                    if (sent >= kStages && !um_bar_wait(bar_kf + 8 * st, done)) { dead = true; break; }
-                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar_k + 8 * st), "r"(Lay::kK) : "memory");
+    } else if (warp >= kPuSoftmax / 32) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPuOtherRegs));
+        if (warp == kPuSoftmax / 32) {
+            // =================== the fetcher ===================
+            // A row's last values, where it ends inside a chunk, come by a barrier of their own; with zeros behind them they are handed
+            // on.
+            int sent = 0, v_sent = 0, tails = 0;                   // chunks of keys, of values, of those with an end
+            while (!dead && next()) {
+                const int tail = n - (n_chunks - 1) * kPuChunk;
+                if (um_elect()) {
+                    for (int ch = 0; ch < n_chunks; ++ch) {
+                        const int st = sent % kStages, t0 = first + ch * kPuChunk;
+                        const uint32_t done = (sent / kStages - 1) & 1, v_bar = ch == n_chunks - 1 && tail < kPuChunk ? bar_t : bar_v + 8 * st;
+                        if (sent >= kStages && !um_bar_wait(bar_kf + 8 * st, done)) { dead = true; break; }
+                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar_k + 8 * st), "r"(Lay::kK) : "memory");
 #pragma unroll
-                    for (int i = 0; i < Lay::kKb; ++i) pu_copy(sm0 + Lay::kOffK + st * Lay::kK + i * Lay::kBox, &k_map, i * 64, h, t0, k_order, bar_k + 8 * st);
-                    ++sent;
-                    if (sent > kStages && !um_bar_wait(bar_vf + 8 * st, done)) { dead = true; break; }
-                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(v_bar), "r"(Lay::kV) : "memory");
+                        for (int i = 0; i < Lay::kKb; ++i) pu_copy(sm0 + Lay::kOffK + st * Lay::kK + i * Lay::kBox, &k_map, i * 64, h, t0, k_order, bar_k + 8 * st);
+                        ++sent;
+                        if (sent > kStages && !um_bar_wait(bar_vf + 8 * st, done)) { dead = true; break; }
+                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(v_bar), "r"(Lay::kV) : "memory");
 #pragma unroll
-                    for (int i = 0; i < Lay::kVb; ++i) pu_copy(sm0 + Lay::kOffV + st * Lay::kV + i * Lay::kBox, &v_map, i * 64, h, t0, v_order, v_bar);
-                    ++v_sent;
-                }
-                if (dead) {                                    // copies in flight end before the CTA does
-                    for (int i = max(0, sent - kStages); i < sent; ++i) um_bar_wait(bar_k + 8 * (i % kStages), (i / kStages) & 1);
-                    for (int i = max(0, v_sent - kStages); i < v_sent; ++i) um_bar_wait(bar_v + 8 * (i % kStages), (i / kStages) & 1);
-                }
-            }
-            dead = __any_sync(0xffffffffu, dead);
-            sent = __reduce_max_sync(0xffffffffu, sent);
-            v_sent = __reduce_max_sync(0xffffffffu, v_sent);
-            if (!dead && tail < kPuChunk) {
-                const int st = (v_sent - 1) % kStages;
-                if (!__all_sync(0xffffffffu, um_bar_wait(bar_t, tails & 1))) { dead = true; break; }
-                ++tails;
-                unsigned char *const rows = sm + Lay::kOffV + st * Lay::kV;
-                for (int i = tail * 8 + lane; i < kPuChunk * 8; i += 32)
-#pragma unroll
-                    for (int j = 0; j < Lay::kVb; ++j) *reinterpret_cast<uint4 *>(rows + j * Lay::kBox + i * 16) = make_uint4(0u, 0u, 0u, 0u);
-                um_fence_async_smem();
-                __syncwarp();
-                if (lane == 0) um_bar_arrive(bar_v + 8 * st);
-            }
-        }
-    } else if (warp == kPuThreads / 32 - 1) {
-        // =================== the queries: A operand of the scores, 64 dims each, 128-byte swizzle ===================
-        constexpr int kPieces = DK / 8;
-        int seen[kPuTiles] = {0, 0}, chunks = 0;               // chunks: of the item before, all of whose scores this waits for
-        bool started = false;
-        while (!dead && next()) {
-            const int tiles = chunks_of(1) ? 2 : 1;
-            for (int t = 0; t < tiles; ++t) {
-                bool there = seen[t] == 0;
-                for (int i = 0; i <= chunks && !there; ++i) there = __all_sync(0xffffffffu, um_bar_wait(bar_qf + 8 * t, (seen[t] - 1) & 1));
-                if (!there) { dead = true; break; }
-                if (q_boxes) {                                 // (tokens behind the row's end are lines that are not written)
-                    if (um_elect()) {
-                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar_q + 8 * t), "r"(Lay::kQ) : "memory");
-#pragma unroll
-                        for (int i = 0; i < Lay::kKb; ++i)
-                            pu_copy(sm0 + Lay::kOffQ + t * Lay::kQ + i * (kPuRows * 128), &q_map, i * 64, h * a.g, first + (line0 + t * kPuRows) / a.g, q_boxes == 2, bar_q + 8 * t);
+                        for (int i = 0; i < Lay::kVb; ++i) pu_copy(sm0 + Lay::kOffV + st * Lay::kV + i * Lay::kBox, &v_map, i * 64, h, t0, v_order, v_bar);
+                        ++v_sent;
                     }
-                    __syncwarp();
-                    ++seen[t];
-                    continue;
-                }
-#pragma unroll 1
-                for (int part = 0; part < kPuRows / 32; ++part) {
-                    const int line = min(line0 + t * kPuRows + part * 32 + lane, lines - 1);       // lines beyond the last repeat it
-                    const unsigned long long src = reinterpret_cast<unsigned long long>(a.q.p + (first + line / a.g) * a.q.ts + (h * a.g + line % a.g) * a.q.hs);
-#pragma unroll
-                    for (int i = 0; i < kPieces; ++i) {
-                        const int idx = i * 32 + lane, row = part * 32 + idx / kPieces, piece = idx % kPieces;
-                        const unsigned long long from = __shfl_sync(0xffffffffu, src, idx / kPieces);
-                        um_cp_async16(sm0 + Lay::kOffQ + t * Lay::kQ + (piece >> 3) * (kPuRows * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4),
-                                      reinterpret_cast<const uint4 *>(from) + piece);
+                    if (dead) {                                    // copies in flight end before the CTA does
+                        for (int i = max(0, sent - kStages); i < sent; ++i) um_bar_wait(bar_k + 8 * (i % kStages), (i / kStages) & 1);
+                        for (int i = max(0, v_sent - kStages); i < v_sent; ++i) um_bar_wait(bar_v + 8 * (i % kStages), (i / kStages) & 1);
                     }
                 }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                if (!started && tiles == 2) {                  // (both tiles of the first item at once)
-                    if (t == 0) continue;
-                    asm volatile("cp.async.wait_group 1;" ::: "memory");
+                dead = __any_sync(0xffffffffu, dead);
+                sent = __reduce_max_sync(0xffffffffu, sent);
+                v_sent = __reduce_max_sync(0xffffffffu, v_sent);
+                if (!dead && tail < kPuChunk) {
+                    const int st = (v_sent - 1) % kStages;
+                    if (!__all_sync(0xffffffffu, um_bar_wait(bar_t, tails & 1))) { dead = true; break; }
+                    ++tails;
+                    unsigned char *const rows = sm + Lay::kOffV + st * Lay::kV;
+                    for (int i = tail * 8 + lane; i < kPuChunk * 8; i += 32)
+#pragma unroll
+                        for (int j = 0; j < Lay::kVb; ++j) *reinterpret_cast<uint4 *>(rows + j * Lay::kBox + i * 16) = make_uint4(0u, 0u, 0u, 0u);
                     um_fence_async_smem();
                     __syncwarp();
-                    if (lane == 0) um_bar_arrive(bar_q);
-                    ++seen[0];
+                    if (lane == 0) um_bar_arrive(bar_v + 8 * st);
                 }
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
-                um_fence_async_smem();
-                __syncwarp();
-                if (lane == 0) um_bar_arrive(bar_q + 8 * t);
-                ++seen[t];
             }
-            started = true;
-            chunks = n_chunks;
-        }
-        // copies in flight end before the CTA does
-        asm volatile("cp.async.wait_all;" ::: "memory");
-        if (q_boxes && dead)
-            for (int t = 0; t < kPuTiles; ++t)
-                if (seen[t]) um_bar_wait(bar_q + 8 * t, (seen[t] - 1) & 1);
-    } else if (warp > kPuSoftmax / 32) {
-        // =================== the MMA thread of a tile ===================
-        const int t = warp - kPuSoftmax / 32 - 1;
-        // descriptors: stride 1024 B, version 1, 128-byte swizzle in the high word; start address and leading offset in
-        // the low word
-        const uint32_t desc_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
-        const uint32_t k_lo = ((sm0 + Lay::kOffK) >> 4) | (1u << 16);                              // leading offset unused (16 B)
-        const uint32_t q_lo = ((sm0 + Lay::kOffQ + t * Lay::kQ) >> 4) | (1u << 16);
-        const uint32_t v_lo = ((sm0 + Lay::kOffV) >> 4) | ((uint32_t)(Lay::kBox / 16) << 16);      // between 64-column blocks
-        const uint32_t tm_s = tmem + t * kPuChunk, tm_o = tmem + Lay::kColO + t * DV, tm_p = Lay::kApart ? tmem + Lay::kColP + t * (kPuChunk / 2) : tm_s;
-        int chunk0 = 0, mine0 = 0, items = 0;                  // chunks of all items so far, the tile's own, its items
-        while (!dead && next()) {
-            const int mine = chunks_of(t);
-            if (um_elect()) {
-                // (waits that are over already go first: between a tile's weights and its next scores there is nothing but the MMAs)
-                auto keys_there = [&](int ch) { return um_bar_wait(bar_k + 8 * ((chunk0 + ch) % kStages), ((chunk0 + ch) / kStages) & 1); };
-                auto values_there = [&](int ch) { return um_bar_wait(bar_v + 8 * ((chunk0 + ch) % kStages), ((chunk0 + ch) / kStages) & 1); };
-                auto score_mma = [&](int ch) {
-                    const int st = (chunk0 + ch) % kStages;
-                    const uint32_t lo = k_lo + st * (Lay::kK >> 4);
+        } else if (warp == kPuThreads / 32 - 1) {
+            // =================== the queries: A operand of the scores, 64 dims each, 128-byte swizzle ===================
+            constexpr int kPieces = DK / 8;
+            int seen[kPuTiles] = {0, 0}, chunks = 0;               // chunks: of the item before, all of whose scores this waits for
+            bool started = false;
+            while (!dead && next()) {
+                const int tiles = chunks_of(1) ? 2 : 1;
+                for (int t = 0; t < tiles; ++t) {
+                    bool there = seen[t] == 0;
+                    for (int i = 0; i <= chunks && !there; ++i) there = __all_sync(0xffffffffu, um_bar_wait(bar_qf + 8 * t, (seen[t] - 1) & 1));
+                    if (!there) { dead = true; break; }
+                    if (q_boxes) {                                 // (tokens behind the row's end are lines that are not written)
+                        if (um_elect()) {
+                            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar_q + 8 * t), "r"(Lay::kQ) : "memory");
 #pragma unroll
-                    for (int ks = 0; ks < DK / 16; ++ks) {
-                        const uint32_t off = ((ks >> 2) * Lay::kBox + (ks & 3) * 32) >> 4;
-                        if (ks == 0) um_mma_ss<false>(tm_s, q_lo + off, desc_hi, lo + off, desc_hi, Lay::kIdescS);
-                        else um_mma_ss<true>(tm_s, q_lo + off, desc_hi, lo + off, desc_hi, Lay::kIdescS);
+                            for (int i = 0; i < Lay::kKb; ++i)
+                                pu_copy(sm0 + Lay::kOffQ + t * Lay::kQ + i * (kPuRows * 128), &q_map, i * 64, h * a.g, first + (line0 + t * kPuRows) / a.g, q_boxes == 2, bar_q + 8 * t);
+                        }
+                        __syncwarp();
+                        ++seen[t];
+                        continue;
                     }
-                    um_commit(bar_s + 8 * t);
-                    um_commit(bar_kf + 8 * st);
-                    if (ch == mine - 1) um_commit(bar_qf + 8 * t);
-                };
-                auto value_mma = [&](int ch) {
-                    const int st = (chunk0 + ch) % kStages;
-                    const uint32_t lo = v_lo + st * (Lay::kV >> 4);
+#pragma unroll 1
+                    for (int part = 0; part < kPuRows / 32; ++part) {
+                        const int line = min(line0 + t * kPuRows + part * 32 + lane, lines - 1);       // lines beyond the last repeat it
+                        const unsigned long long src = reinterpret_cast<unsigned long long>(a.q.p + (first + line / a.g) * a.q.ts + (h * a.g + line % a.g) * a.q.hs);
 #pragma unroll
-                    for (int kt = 0; kt < kPuChunk / 16; ++kt) {
-                        if (kt == 0 && ch == 0) um_mma_ts<false>(tm_o, tm_p, lo, desc_hi, Lay::kIdescO);
-                        else um_mma_ts<true>(tm_o, tm_p + kt * 8, lo + kt * (2048 >> 4), desc_hi, Lay::kIdescO);
+                        for (int i = 0; i < kPieces; ++i) {
+                            const int idx = i * 32 + lane, row = part * 32 + idx / kPieces, piece = idx % kPieces;
+                            const unsigned long long from = __shfl_sync(0xffffffffu, src, idx / kPieces);
+                            um_cp_async16(sm0 + Lay::kOffQ + t * Lay::kQ + (piece >> 3) * (kPuRows * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4),
+                                          reinterpret_cast<const uint4 *>(from) + piece);
+                        }
                     }
-                    if (Lay::kApart) um_commit(bar_pv + 8 * t);
-                    um_commit(bar_vf + 8 * st);
-                };
-                bool ok = true;
-                if (mine) {
-                    ok = keys_there(0) && um_bar_wait(bar_q + 8 * t, items & 1) && (!Lay::kApart || !mine0 || um_bar_wait(bar_sf + 8 * t, (mine0 - 1) & 1));
-                    if (ok) {
-                        um_fence_after();
-                        score_mma(0);
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                    if (!started && tiles == 2) {                  // (both tiles of the first item at once)
+                        if (t == 0) continue;
+                        asm volatile("cp.async.wait_group 1;" ::: "memory");
+                        um_fence_async_smem();
+                        __syncwarp();
+                        if (lane == 0) um_bar_arrive(bar_q);
+                        ++seen[0];
                     }
-                    ok = ok && (!items || um_bar_wait(bar_of + 8 * t, (items - 1) & 1));
-                    for (int ch = 0; ok && ch < mine; ++ch) {
-                        const bool last = ch + 1 >= mine;
-                        if (Lay::kApart && !last) {            // the next scores while the softmax threads work on these
-                            ok = keys_there(ch + 1) && um_bar_wait(bar_sf + 8 * t, (mine0 + ch) & 1);
+                    asm volatile("cp.async.wait_group 0;" ::: "memory");
+                    um_fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) um_bar_arrive(bar_q + 8 * t);
+                    ++seen[t];
+                }
+                started = true;
+                chunks = n_chunks;
+            }
+            // copies in flight end before the CTA does
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            if (q_boxes && dead)
+                for (int t = 0; t < kPuTiles; ++t)
+                    if (seen[t]) um_bar_wait(bar_q + 8 * t, (seen[t] - 1) & 1);
+        } else if (warp > kPuSoftmax / 32) {
+            // =================== the MMA thread of a tile ===================
+            const int t = warp - kPuSoftmax / 32 - 1;
+            // descriptors: stride 1024 B, version 1, 128-byte swizzle in the high word; start address and leading offset in
+            // the low word
+            const uint32_t desc_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+            const uint32_t k_lo = ((sm0 + Lay::kOffK) >> 4) | (1u << 16);                              // leading offset unused (16 B)
+            const uint32_t q_lo = ((sm0 + Lay::kOffQ + t * Lay::kQ) >> 4) | (1u << 16);
+            const uint32_t v_lo = ((sm0 + Lay::kOffV) >> 4) | ((uint32_t)(Lay::kBox / 16) << 16);      // between 64-column blocks
+            const uint32_t tm_s = tmem + t * kPuChunk, tm_o = tmem + Lay::kColO + t * DV, tm_p = Lay::kApart ? tmem + Lay::kColP + t * (kPuChunk / 2) : tm_s;
+            int chunk0 = 0, mine0 = 0, items = 0;                  // chunks of all items so far, the tile's own, its items
+            while (!dead && next()) {
+                const int mine = chunks_of(t);
+                if (um_elect()) {
+                    // (waits that are over already go first: between a tile's weights and its next scores there is nothing but the MMAs)
+                    auto keys_there = [&](int ch) { return um_bar_wait(bar_k + 8 * ((chunk0 + ch) % kStages), ((chunk0 + ch) / kStages) & 1); };
+                    auto values_there = [&](int ch) { return um_bar_wait(bar_v + 8 * ((chunk0 + ch) % kStages), ((chunk0 + ch) / kStages) & 1); };
+                    auto score_mma = [&](int ch) {
+                        const int st = (chunk0 + ch) % kStages;
+                        const uint32_t lo = k_lo + st * (Lay::kK >> 4);
+#pragma unroll
+                        for (int ks = 0; ks < DK / 16; ++ks) {
+                            const uint32_t off = ((ks >> 2) * Lay::kBox + (ks & 3) * 32) >> 4;
+                            if (ks == 0) um_mma_ss<false>(tm_s, q_lo + off, desc_hi, lo + off, desc_hi, Lay::kIdescS);
+                            else um_mma_ss<true>(tm_s, q_lo + off, desc_hi, lo + off, desc_hi, Lay::kIdescS);
+                        }
+                        um_commit(bar_s + 8 * t);
+                        um_commit(bar_kf + 8 * st);
+                        if (ch == mine - 1) um_commit(bar_qf + 8 * t);
+                    };
+                    auto value_mma = [&](int ch) {
+                        const int st = (chunk0 + ch) % kStages;
+                        const uint32_t lo = v_lo + st * (Lay::kV >> 4);
+#pragma unroll
+                        for (int kt = 0; kt < kPuChunk / 16; ++kt) {
+                            if (kt == 0 && ch == 0) um_mma_ts<false>(tm_o, tm_p, lo, desc_hi, Lay::kIdescO);
+                            else um_mma_ts<true>(tm_o, tm_p + kt * 8, lo + kt * (2048 >> 4), desc_hi, Lay::kIdescO);
+                        }
+                        if (Lay::kApart) um_commit(bar_pv + 8 * t);
+                        um_commit(bar_vf + 8 * st);
+                    };
+                    bool ok = true;
+                    if (mine) {
+                        ok = keys_there(0) && um_bar_wait(bar_q + 8 * t, items & 1) && (!Lay::kApart || !mine0 || um_bar_wait(bar_sf + 8 * t, (mine0 - 1) & 1));
+                        if (ok) {
+                            um_fence_after();
+                            score_mma(0);
+                        }
+                        ok = ok && (!items || um_bar_wait(bar_of + 8 * t, (items - 1) & 1));
+                        for (int ch = 0; ok && ch < mine; ++ch) {
+                            const bool last = ch + 1 >= mine;
+                            if (Lay::kApart && !last) {            // the next scores while the softmax threads work on these
+                                ok = keys_there(ch + 1) && um_bar_wait(bar_sf + 8 * t, (mine0 + ch) & 1);
+                                if (!ok) break;
+                                um_fence_after();
+                                score_mma(ch + 1);
+                            }
+                            ok = values_there(ch) && (Lay::kApart || last || keys_there(ch + 1)) && um_bar_wait(bar_p + 8 * t, (mine0 + ch) & 1);
                             if (!ok) break;
                             um_fence_after();
-                            score_mma(ch + 1);
+                            value_mma(ch);
+                            if (!Lay::kApart && !last) score_mma(ch + 1);
                         }
-                        ok = values_there(ch) && (Lay::kApart || last || keys_there(ch + 1)) && um_bar_wait(bar_p + 8 * t, (mine0 + ch) & 1);
-                        if (!ok) break;
-                        um_fence_after();
-                        value_mma(ch);
-                        if (!Lay::kApart && !last) score_mma(ch + 1);
+                        if (ok) um_commit(bar_o + 8 * t);
                     }
-                    if (ok) um_commit(bar_o + 8 * t);
+                    for (int ch = mine; ok && ch < n_chunks; ++ch) {               // chunks that only the other tile sees
+                        const int st = (chunk0 + ch) % kStages;
+                        ok = um_bar_wait(bar_k + 8 * st, ((chunk0 + ch) / kStages) & 1);
+                        if (ok) um_bar_arrive(bar_kf + 8 * st);
+                        ok = ok && um_bar_wait(bar_v + 8 * st, ((chunk0 + ch) / kStages) & 1);
+                        if (ok) um_bar_arrive(bar_vf + 8 * st);
+                    }
+                    dead = !ok;
                 }
-                for (int ch = mine; ok && ch < n_chunks; ++ch) {               // chunks that only the other tile sees
-                    const int st = (chunk0 + ch) % kStages;
-                    ok = um_bar_wait(bar_k + 8 * st, ((chunk0 + ch) / kStages) & 1);
-                    if (ok) um_bar_arrive(bar_kf + 8 * st);
-                    ok = ok && um_bar_wait(bar_v + 8 * st, ((chunk0 + ch) / kStages) & 1);
-                    if (ok) um_bar_arrive(bar_vf + 8 * st);
-                }
-                dead = !ok;
+                dead = __any_sync(0xffffffffu, dead);
+                chunk0 += n_chunks;
+                mine0 += mine;
+                items += mine > 0;
             }
-            dead = __any_sync(0xffffffffu, dead);
-            chunk0 += n_chunks;
-            mine0 += mine;
-            items += mine > 0;
         }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPuSoftmaxRegs));
         // =================== softmax: thread r owns line r of its tile ===================
         const int tile = warp >> 2;
         const uint32_t lane_base = (uint32_t)((warp & 3) * 32) << 16;
@@ -499,6 +507,12 @@ lookat_status launch_pu(Ctx *ctx, const PackedAttendArgs &a)
     auto kern = attend_packed_umma_kernel<DK, DV>;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kBytes) != cudaSuccess)
         return check_launch(ctx, "attend_packed (tcgen05 form): shared-memory opt-in");
+    // (with fewer registers than it was written for, the split would wait for ever)
+    static const int regs = [&] {
+        cudaFuncAttributes attributes;
+        return cudaFuncGetAttributes(&attributes, kern) == cudaSuccess ? attributes.numRegs : 0;
+    }();
+    if (regs < kPuLaunchRegs) return set_error(ctx, LOOKAT_ERR_CUDA, "attend_packed: the kernel was compiled to %d registers, not %d", regs, kPuLaunchRegs);
     CUtensorMap k_map, v_map, q_map, out_map;
     int k_order, v_order, q_order = 0, out_order = 0;
     if (!make_rows_map_f16(&k_map, a.k.p, DK, a.H_kv, a.rows.n, a.k.hs, a.k.ts, 1, kPuChunk, &k_order) ||
