@@ -148,12 +148,16 @@ lookat_status launch_pa(Ctx *ctx, const PackedAttendArgs &a)
 
 }  // namespace
 
+lookat_status launch_attend_packed_any(Ctx *ctx, const PackedAttendArgs &a)
+{
+    const int dim = a.d_k > a.d_v ? a.d_k : a.d_v;
+    return dim <= 64 ? launch_pa<64>(ctx, a) : dim <= 128 ? launch_pa<128>(ctx, a) : launch_pa<256>(ctx, a);
+}
+
 lookat_status launch_attend_packed(Ctx *ctx, const PackedAttendArgs &a)
 {
     if ((long long)a.rows.n * a.g >= (1ll << 31) - 1024) return set_error(ctx, LOOKAT_ERR_UNSUPPORTED, "attend_packed: too many tokens for one call");
-    if (attend_packed_umma_covers(ctx, a)) return launch_attend_packed_umma(ctx, a);
-    const int dim = a.d_k > a.d_v ? a.d_k : a.d_v;
-    return dim <= 64 ? launch_pa<64>(ctx, a) : dim <= 128 ? launch_pa<128>(ctx, a) : launch_pa<256>(ctx, a);
+    return attend_packed_umma_covers(ctx, a) ? launch_attend_packed_umma(ctx, a) : launch_attend_packed_any(ctx, a);
 }
 
 }  // namespace lookat

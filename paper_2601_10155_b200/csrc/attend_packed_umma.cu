@@ -517,7 +517,7 @@ lookat_status launch_pu(Ctx *ctx, const PackedAttendArgs &a)
     int k_order, v_order, q_order = 0, out_order = 0;
     if (!make_rows_map_f16(&k_map, a.k.p, DK, a.H_kv, a.rows.n, a.k.hs, a.k.ts, 1, kPuChunk, &k_order) ||
         !make_rows_map_f16(&v_map, a.v.p, DV, a.H_kv, a.rows.n, a.v.hs, a.v.ts, 1, kPuChunk, &v_order))
-        return set_error(ctx, LOOKAT_ERR_CUDA, "attend_packed: the driver refused a tensor map");
+        return launch_attend_packed_any(ctx, a);               // (strides that the driver makes no map of)
     // no more tiles than this, whatever the rows' lengths
     // a tile's lines in one box: g heads of 128 / g tokens, heads innermost
     const bool whole = kPuRows % a.g == 0 &&

@@ -129,6 +129,7 @@ struct PackedAttendArgs {
     float scale_log2;               // softmax scale * log2(e)
 };
 lookat_status launch_attend_packed(Ctx *ctx, const PackedAttendArgs &a);
+lookat_status launch_attend_packed_any(Ctx *ctx, const PackedAttendArgs &a);       // any dims, on mma.sync
 // on tcgen05 (attend_packed_umma.cu)
 bool attend_packed_umma_covers(const Ctx *ctx, const PackedAttendArgs &a);
 lookat_status launch_attend_packed_umma(Ctx *ctx, const PackedAttendArgs &a);

@@ -196,6 +196,29 @@ def test_attend_packed_more_items_than_a_cta_lists():
         assert bool(((out[lo:hi].double() - want).abs() <= attend_bound(want, mag, reach, 64, 150, float(v.abs().max()))).all())
 
 
+@pytest.mark.parametrize("layout", ["fused", "heads"])
+@pytest.mark.parametrize("H,H_kv", [(64, 1), (128, 1), (32, 1), (96, 2), (256, 2)])
+def test_attend_packed_large_groups(H, H_kv, layout):
+    """Groups of 32 to 128 query heads: a tile is a few tokens, or one; a warp's lines are part of a token's."""
+    check_attend(np.random.default_rng(H), [40, 1, 9], H, H_kv, 64, 64, layout)
+    check_attend(np.random.default_rng(H), [70, 200], H, H_kv, 128, 128, layout)
+
+
+def test_attend_packed_windows_and_an_output_among_other_things():
+    """Keys whose vectors overlap each other (heads 8 elements apart), and results into the middle of wider rows."""
+    T, H, d = 300, 4, 64
+    buf = torch.randn(T * 128 + 64, device="cuda").half()
+    k = buf.as_strided((T, H, d), (128, 8, 1))
+    q, v = torch.randn(T, H, d, device="cuda").half(), torch.randn(T, H, d, device="cuda").half()
+    wide = torch.full((T, 3 * H, d), 7.0, dtype=torch.float16, device="cuda")
+    out = wide[:, H:2 * H]
+    lk = Lookat(H, H, d, d, 1, 16)
+    lk.lookat_attend_packed(q, k, v, i32([0, 120, T]), out=out)
+    want = lk.lookat_attend_packed(q, k.contiguous(), v, i32([0, 120, T]))
+    assert finding(lk) == "" and torch.equal(out, want)
+    assert (wide[:, :H] == 7).all() and (wide[:, 2 * H:] == 7).all()
+
+
 def test_attend_packed_of_the_plain_oracle():
     """A small case against the oracle that is written one query at a time."""
     (q, k, v), starts = packed_inputs(np.random.default_rng(2), [9, 0, 33], 4, 2, 64, 64)
