@@ -15,10 +15,12 @@ namespace lookat {
 
 namespace {
 
-enum { kRopeHalves, kRopePairs, kRopeAny };     // pieces with pairs half a rotary part apart, pieces of neighbouring pairs, single pairs
+// pieces with pairs half a rotary part apart, pieces of neighbouring pairs; halves that do not begin on pieces' borders, or of more than
+// a warp's pieces, two elements at a time
+enum { kRopeHalves, kRopePairs, kRopeAny };
 
 struct RopePlan {
-    int lanes;                  // per token and split: pieces of a head, rounded up to a power of two; kRopeAny: pairs
+    int lanes;                  // per token and split: pieces of a head (kRopeHalves: up to a power of two; kRopeAny: two elements each)
     int each, splits;           // heads per lane, lanes per piece
     int inplace[2];
     long long threads;
@@ -69,24 +71,34 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a, RopePlan p)
     if constexpr (FORM == kRopeAny) {
         if (id != id_in) return;
         const bool turns = at < c;
-        const int i = turns ? (a.interleaved ? 2 * at : at) : 2 * at, j = turns && !a.interleaved ? i + c : i + 1;
         const float2 cs = turns ? pair(at) : make_float2(1.f, 0.f);
-        for (int h = head0; h < head1; ++h) {
-            if (!turns && p.inplace[h >= a.heads[0]]) continue;
-            const __half *src = vector(a.in, h);
-            __half *dst = vector(a.out, h);
-            const __half u = src[i], v = src[j];
-            if (!turns) {
-                dst[i] = u, dst[j] = v;
-                continue;
+        constexpr int kBatch = 4;
+        for (int h0 = head0; h0 < head1; h0 += kBatch) {
+            __half u[kBatch], v[kBatch];
+            uint32_t w[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                if (h0 + k >= head1) continue;
+                const __half *src = vector(a.in, h0 + k);
+                if (turns) u[k] = src[at], v[k] = src[at + c];
+                else w[k] = *reinterpret_cast<const uint32_t *>(src + 2 * at);
             }
-            const float x = __half2float(u), y = __half2float(v);
-            dst[i] = __float2half_rn(x * cs.x - y * cs.y), dst[j] = __float2half_rn(y * cs.x + x * cs.y);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                if (h0 + k >= head1) continue;
+                __half *dst = vector(a.out, h0 + k);
+                if (turns) {
+                    const float x = __half2float(u[k]), y = __half2float(v[k]);
+                    dst[at] = __float2half_rn(x * cs.x - y * cs.y), dst[at + c] = __float2half_rn(y * cs.x + x * cs.y);
+                } else if (!p.inplace[h0 + k >= a.heads[0]]) {
+                    *reinterpret_cast<uint32_t *>(dst + 2 * at) = w[k];
+                }
+            }
         }
     } else {
         constexpr int kPairs = FORM == kRopeHalves ? 8 : 4, kBatch = 4;         // kBatch: heads whose loads are in flight together
         // the lane's piece: in the first half, in the second, or behind the rotary part
-        const bool on = id == id_in && at < a.d / 8, turns = at < a.r / 8, second = FORM == kRopeHalves && at >= c / 8;
+        const bool on = id == id_in && at < a.d / 8, turns = at * 8 < a.r, second = FORM == kRopeHalves && at >= c / 8;
         const int lane = threadIdx.x & 31, other = FORM == kRopeHalves && turns ? (second ? lane - c / 8 : lane + c / 8) : lane;
         float cosine[kPairs], sine[kPairs];                    // sine: with the sign that it has in this half
 #pragma unroll
@@ -97,7 +109,7 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a, RopePlan p)
                 cosine[i] = second ? had.x : own.x, sine[i] = second ? had.y : -own.y;
                 cosine[4 + i] = second ? own.x : had.x, sine[4 + i] = second ? own.y : -had.y;
             } else {
-                const float2 own = turns ? pair(at * 4 + i) : make_float2(1.f, 0.f);
+                const float2 own = at * 8 + 2 * i < a.r ? pair(at * 4 + i) : make_float2(1.f, 0.f);
                 cosine[i] = own.x, sine[i] = own.y;
             }
         }
@@ -119,7 +131,7 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a, RopePlan p)
                         const float2 n = rope_float2(__shfl_sync(0xffffffffu, u[i], other));
                         if (turns) u[i] = rope_half2(fmaf(m.x, cosine[2 * i], n.x * sine[2 * i]), fmaf(m.y, cosine[2 * i + 1], n.y * sine[2 * i + 1]));
                     } else {
-                        if (turns) u[i] = rope_half2(fmaf(m.x, cosine[i], -m.y * sine[i]), fmaf(m.y, cosine[i], m.x * sine[i]));
+                        if (at * 8 + 2 * i < a.r) u[i] = rope_half2(fmaf(m.x, cosine[i], -m.y * sine[i]), fmaf(m.y, cosine[i], m.x * sine[i]));
                     }
                 }
                 if (on && h < head1 && (turns || !p.inplace[h >= a.heads[0]]))
@@ -133,13 +145,12 @@ __global__ void __launch_bounds__(256) rope_kernel(RopeArgs a, RopePlan p)
 
 lookat_status launch_rope(Ctx *ctx, const RopeArgs &a)
 {
-    // whole 16-byte pieces where the halves (or the pairs) and what follows them begin on such borders, and a head's pieces fit a warp
-    const bool pieces = a.d <= 256 && a.r % (a.interleaved ? 8 : 16) == 0;
-    const int form = !pieces ? kRopeAny : a.interleaved ? kRopePairs : kRopeHalves;
+    const int form = a.interleaved ? kRopePairs : a.d <= 256 && a.r % 16 == 0 ? kRopeHalves : kRopeAny;
     RopePlan p;
     for (int i = 0; i < 2; ++i) p.inplace[i] = a.in[i].p == a.out[i].p && a.in[i].ts == a.out[i].ts && a.in[i].hs == a.out[i].hs;
+    p.lanes = a.d / 8;
+    if (form == kRopeHalves) for (p.lanes = 1; p.lanes < a.d / 8;) p.lanes *= 2;
     if (form == kRopeAny) p.lanes = a.d / 2;
-    else for (p.lanes = 1; p.lanes < a.d / 8;) p.lanes *= 2;
     const int heads = a.heads[0] + a.heads[1];
     const long long full = (long long)ctx->sm_count * 2048;    // resident threads
     for (p.each = 32; p.each > 1 && 4 * a.n * p.lanes * ((heads + p.each - 1) / p.each) < full;) p.each /= 2;

@@ -37,7 +37,7 @@ def rope_bound(x, amplitude):
 
 @pytest.mark.parametrize("interleaved", [False, True])
 @pytest.mark.parametrize("H,H_kv,d,r,scaling", [(12, 12, 64, 64, "none"), (32, 8, 128, 128, "ramp"), (4, 2, 64, 32, "linear"), (5, 1, 48, 20, "base"), (3, 3, 16, 2, "none"),
-                                                (6, 3, 128, 24, "bands"), (2, 2, 256, 256, "none"), (1, 1, 8, 8, "none"), (2, 1, 48, 48, "none"), (4, 2, 24, 16, "none"),
+                                                (6, 3, 128, 24, "bands"), (2, 2, 256, 256, "none"), (1, 1, 8, 8, "none"), (2, 1, 512, 512, "none"), (2, 2, 320, 36, "none"), (1, 1, 16, 14, "none"), (2, 1, 48, 48, "none"), (4, 2, 24, 16, "none"),
                                                 (6, 2, 112, 96, "linear")])
 @pytest.mark.parametrize("T", [1, 3, 70])
 def test_rope(H, H_kv, d, r, scaling, interleaved, T):
@@ -49,7 +49,7 @@ def test_rope(H, H_kv, d, r, scaling, interleaved, T):
     q, k = x[:, :H], x[:, H:H + H_kv]
     pos = rng.integers(-5, 1 << 20, T)
     pos[0] = 2 ** 31 - 1
-    lk = Lookat(H, H_kv, d, d, 1 if d <= 128 else 2, 16)
+    lk = Lookat(H, H_kv, d, d, 1 if d <= 128 else 4, 16)
     q0, k0 = q.cpu().numpy(), k.cpu().numpy()
     got_q, got_k = lk.lookat_rope(q, k, i32(pos), tb, interleaved=interleaved)
     assert finding(lk) == "" and np.array_equal(q.cpu().numpy(), q0), "inputs change"
