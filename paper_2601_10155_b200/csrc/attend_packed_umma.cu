@@ -18,6 +18,9 @@
 //   warps 9, 10 one thread each issues the MMAs of tile 0 / 1 and commits them to mbarriers;
 //   warp 11     fetches the query lines: by tiled bulk copies where a tile's lines are whole tokens of [tokens][heads][dims], else
 //               by cp.async (any strides and groups).
+//   4 x 4096 tokens, 32 and 8 heads of 128: 500 to 530 us, 1.04 to 1.1 PFLOP/s; one row of 16384 1.8 ms (1.2), 2.0 under the power cap.
+// Softmax alone (the MMAs cut to one each) and MMAs alone (no exponentials, maxima, sums) take about three quarters of that each:
+// the rest is that a tile's scores wait for its weights.  Short rows pay 3 to 4 us per item for its first scores and its way out.
 // Every mbarrier wait gives up after a bounded number of polls, raises the context's time-out flag and lets the CTA drain and
 // free its tensor memory.
 #include <cuda.h>           // CUtensorMap only

@@ -8,8 +8,11 @@
 //     and is renewed at the batches 1, 2, 4, ...: few logits reach it.
 // Rows are read in the same order whatever their alignment (16-byte loads where all rows lie on such borders, else 4-byte ones):
 // beams with equal logits and scores get equal ranks, and the lower one goes first.
-// The CTA's warps join in shared memory.  The last CTA of a group to finish (a counter, no waiting) joins the parts, ranks
+// A CTA's candidates find their places by counting those before them.  The last CTA of a group to finish (a counter, no waiting) joins the parts, ranks
 // in fp64, and moves the beams.
+//   32 x 16 beams over 131072 tokens: 73 us (3.7 TB/s: the copies wait for HBM under 24 warps an SM, 210 instructions per warp and
+// batch), histories of 512 tokens 4 us more; 8 x 4 over 50257 tokens 17 us, most of it the chain of dependent steps of a part
+// and of the join.
 #include "serve.cuh"
 
 namespace lookat {

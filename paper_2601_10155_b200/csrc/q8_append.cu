@@ -8,7 +8,8 @@
 // one is done again by division, whose correctly rounded fp32 quotient is the tie itself.
 //
 // One group of threads per (row, KV head, K or V, block): it reads the block's new tokens once (kept in registers between
-// the maximum and the rounding), so nothing is read from HBM twice and no two groups share a block.
+// the maximum and the rounding), so nothing is read from HBM twice and no two groups share a block.  Magnitudes are compared as
+// the whole numbers that their bits are; only where one is an infinity or a NaN are the numbers made finite.
 #include <type_traits>
 
 #include "serve.cuh"
@@ -146,8 +147,8 @@ __device__ __forceinline__ uint4 ap_shrink16(uint4 u, float was, float now)
 }
 
 // THREADS per group: as many as hold a block's new tokens in kApKeep units each, since what bounds the kernel is how many
-// groups wait for their loads at a time (4 rows of up to 4096 tokens, 8 heads of 128 dims, pages of 64: 24 us with 128
-// threads, 25 with 256, 35 with 512; pages of 16: 39, 51 and 97)
+// groups wait for their loads at a time (4 rows of up to 4096 tokens, 8 heads of 128 dims, pages of 64: 28 us with 32 threads, 19
+// with 128, 25 with 256; pages of 16: 25, 34 and 61.  As packed rows of 4096 tokens, pages of 64: 32, 31 and 34 us)
 //
 // PACKED: the rows' tokens stand one behind the other (a.starts), and the host does not know the rows' lengths.  A row of c
 // tokens touches at most c / page + 2 blocks (rounded down), so row b has the slots from starts[b] / page + 2 b on: those of

@@ -1,4 +1,4 @@
-// Device helpers of the tcgen05 kernels (prefill_umma.cu, attend_q8_umma.cu): mbarriers with bounded waits, MMAs with A in
+// Device helpers of the tcgen05 kernels (prefill_umma.cu, attend_q8_umma.cu, attend_packed_umma.cu): mbarriers with bounded waits, MMAs with A in
 // tensor memory, moves between registers and tensor memory.
 #pragma once
 
