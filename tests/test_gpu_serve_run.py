@@ -131,3 +131,19 @@ def test_beam_search_with_the_gpt2_harness():
         total += torch.log_softmax(logits.double(), dim=1).gather(1, feed.long()[:, None])[:, 0]
     # the same kernels on the same rows, the scores rounded once a step (2^-24 of at most 100) over sums good to 2^-20
     assert float((total - scores.double()).abs().max()) <= steps * (100 * 2.0 ** -24 + 2.0 ** -20)
+
+
+def test_the_debug_build_serves_as_well():
+    """The same calls in the library that checks codes."""
+    x = torch.randn(300, 12, 64, device="cuda").half()
+    q, k, v = x.split([8, 2, 2], dim=1)
+    got = []
+    for debug in (False, True):
+        lk = Lookat(8, 2, 64, 64, 4, 16, debug=debug)
+        a, b = lk.lookat_rope(q, k, torch.arange(300, dtype=torch.int32, device="cuda"), RopeTable(64))
+        st = BeamState.empty(2, 2, 4)
+        ids, _ = lk.lookat_beam_select(st, x.view(300, -1)[:4].float())
+        got.append((a, b, lk.lookat_attend_packed(a, b, v, i32([0, 170, 300])), ids, st.scores))
+        torch.cuda.synchronize()
+        assert lk.lookat_last_error() == ""
+    assert all(torch.equal(y, z) for y, z in zip(*got))
