@@ -160,9 +160,11 @@ __global__ void __launch_bounds__(THREADS == 32 ? 128 : THREADS, THREADS == 256 
     const int lane = THREADS == 32 ? (threadIdx.x & 31) : threadIdx.x;
     const long long item = (long long)blockIdx.x * kGroups + (THREADS == 32 ? threadIdx.x >> 5 : 0);
     const Q8View &c = a.c;
+    [[maybe_unused]] const Packed rows = {a.starts, a.B, a.n, c.status};
     int j, which, b, h, start = 0;
     long long bh = 0;
     if constexpr (PACKED) {                                     // [slot][head][K or V]
+        if (item == 0) packed_check(rows, lane, THREADS);       // (slot 0 may be no row's)
         const unsigned pair = (unsigned)item >> 1;              // (fewer than 2^31 items)
         which = (int)(item & 1);
         h = (int)(pair % (unsigned)c.H_kv);
@@ -188,8 +190,6 @@ __global__ void __launch_bounds__(THREADS == 32 ? 128 : THREADS, THREADS == 256 
     const int len_in = c.seq_lens[b];
     int count_in;
     if constexpr (PACKED) {
-        const Packed rows = {a.starts, a.B, a.n, c.status};
-        if (item == 0) packed_check(rows, lane, THREADS);
         count_in = packed_row(rows, b, start);
         if (count_in == 0) return;
     } else {

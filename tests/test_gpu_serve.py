@@ -438,6 +438,20 @@ def test_append_packed_findings_and_refusals():
         lk.lookat_q8_append_packed(cache, x, x[:30], i32([0, 20, 40]), tables, lens)
 
 
+@pytest.mark.parametrize("d,page", [(64, 16), (128, 64)])
+def test_append_packed_finds_bad_starts_behind_tokens_of_no_row(d, page):
+    """Tokens of more than a page before the first row: nothing is appended for the first places."""
+    cache = Q8Cache.empty(6, 2, page, d, d)
+    x = torch.randn(page + 40, 2, d, device="cuda").half()
+    tables, lens = i32([[0, 1], [2, 3]]), i32([20, 20])
+    for starts, message in (([page, page + 20, page + 40], ""), ([page, page + 20, page + 41], "out of range or order"),
+                            ([page + 20, page + 40, page], "out of range or order")):
+        lk = Lookat(2, 2, d, d, 1, 16)
+        lk.lookat_q8_append_packed(cache, x, x, i32(starts), tables, lens)
+        found = finding(lk)
+        assert message in found and bool(found) == bool(message)
+
+
 # ------------------------------------------------------------------------------------------------ beam selection
 GAP = 2e-5          # ranks closer than this are not asked to be told apart: fp32 exponentials and the differences in them, 2^-20 each at most
 
