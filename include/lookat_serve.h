@@ -12,8 +12,9 @@
  *   A context serves one attention shape: its n_q_heads, n_kv_heads, d_k, d_v and scale.
  *
  * DEVICE-SIDE FINDINGS.  The host does not see starts: a row for which 0 <= starts[b] <= starts[b + 1] <= n_tokens does not hold is
- * taken as empty, and lookat_last_error reports it as lookat_q8.h describes.  Rows that overlap (a later start before an earlier
- * row's end) are the caller's error: tokens of theirs may keep their former results.
+ * taken as empty, and lookat_last_error reports it as lookat_q8.h describes.  A row's tokens are found by bisection, for which starts
+ * must not fall: with an entry below an earlier one (rows that overlap, a list that ends in zeros) tokens of other rows may keep
+ * their former results.  A batch of fewer rows than B ends in repeats of its last entry, which are empty rows.
  *
  * Work is enqueued on the context's stream; scratch and captures are as in lookat_q8.h.
  */
