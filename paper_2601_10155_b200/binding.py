@@ -10,6 +10,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import threading
 
 import torch
 
@@ -261,6 +262,13 @@ def _fill(rows, t, name, device, shape):
     return rows
 
 
+class _RowArgs(threading.local):
+    """What calls that take packed rows fill in: each thread has its own, since a call gives others way."""
+
+    def __init__(self):
+        self.r = [lookat_rows() for _ in range(4)]
+
+
 class RopeTable:
     """The speeds of rotary positions (include/lookat_serve.h): turns per position of each pair on the device, and the factor on
     cosines and sines.  scaling: none, linear, base, bands or ramp."""
@@ -404,7 +412,7 @@ class Lookat:
         self._h = h
         self._shape, self._kv_shape = (n_q_heads, n_kv_heads, d_k, d_v), (n_kv_heads, d_k, d_v)
         self._raw_stream = stream.cuda_stream
-        self._row_args = [lookat_rows() for _ in range(4)]      # filled by every call that takes packed rows
+        self._row_args = _RowArgs()
         self.scale = scale if scale > 0 else 1.0 / math.sqrt(d_k)
 
     # -- helpers ---------------------------------------------------------------
@@ -665,7 +673,7 @@ class Lookat:
         T = (k if q is None else q).shape[0]
         if table.device != dev:
             raise ValueError(f"the table is on {table.device}, the context on {dev}")
-        r = self._row_args
+        r = self._row_args.r
         in_q = in_k = to_q = to_k = None
         if q is not None:
             shape = (T, H, d)
@@ -687,7 +695,7 @@ class Lookat:
         """Exact causal attention of packed prompts: q [tokens][H_q][d_k], k [tokens][H_kv][d_k], v [tokens][H_kv][d_v], row b the
         tokens starts[b] .. starts[b + 1] - 1; tokens of no row keep what `out` held."""
         H, H_kv, d_k, d_v = self._shape
-        dev, r = self.device, self._row_args
+        dev, r = self.device, self._row_args.r
         T, n = q.shape[0], starts.shape[0]
         shape = (T, H, d_v)
         if out is None:
@@ -702,7 +710,7 @@ class Lookat:
     def lookat_q8_append_packed(self, cache, k, v, starts, tables, seq_lens):
         """Quantises the packed tokens starts[b] .. starts[b + 1] - 1 as the newest of row b; k [tokens][H_kv][d_k]."""
         _, H, d_k, d_v = self._shape
-        dev, r = self.device, self._row_args
+        dev, r = self.device, self._row_args.r
         B, max_pages, tb, sl = self._q8(cache, tables, seq_lens)
         T = k.shape[0]
         st = self._lib.lookat_q8_append_packed(self._h, cache.c, _fill(r[0], k, "k", dev, (T, H, d_k)), _fill(r[1], v, "v", dev, (T, H, d_v)), T, B,

@@ -1,6 +1,8 @@
 """Rotary positions, attention of packed prompts, packed appends and beam selection on the GPU against their oracle
 (oracle/serve.py), within bounds that are derived below."""
 import math
+import sys
+import threading
 
 import numpy as np
 import pytest
@@ -79,6 +81,33 @@ def test_rope_of_many_tokens_is_that_of_few():
         assert torch.equal(a, q[lo:lo + 10]) and torch.equal(b, k[lo:lo + 10])
     e, _ = lk.lookat_rope(x[:0, :32], None, pos[:0], tb)
     assert e.shape == (0, 32, 128)
+
+
+def test_rope_from_two_threads_on_one_context():
+    """Each call has its own rows, whatever another thread calls meanwhile."""
+    lk, tb = Lookat(4, 2, 64, 64, 1, 16), RopeTable(64)
+    pos = torch.arange(16, dtype=torch.int32, device="cuda")
+    x = torch.randn(2, 16, 4, 64, device="cuda").half()
+    want = [lk.lookat_rope(x[i], None, pos, tb)[0] for i in range(2)]
+    out = torch.zeros(2, 400, 16, 4, 64, dtype=torch.float16, device="cuda")
+    torch.cuda.synchronize()
+
+    def run(i):
+        for j in range(400):
+            lk.lookat_rope(x[i], None, pos, tb, q_out=out[i, j])
+
+    threads, interval = [threading.Thread(target=run, args=(i,)) for i in range(2)], sys.getswitchinterval()
+    sys.setswitchinterval(1e-6)
+    try:
+        for t in threads:
+            t.start()
+        for t in threads:
+            t.join()
+    finally:
+        sys.setswitchinterval(interval)
+    assert finding(lk) == ""
+    for i in range(2):
+        assert (out[i] == want[i]).all()
 
 
 def test_rope_refuses():
