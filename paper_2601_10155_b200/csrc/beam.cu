@@ -8,11 +8,11 @@
 //     and is renewed at the batches 1, 2, 4, ...: few logits reach it.
 // Rows are read in the same order whatever their alignment (16-byte loads where all rows lie on such borders, else 4-byte ones):
 // beams with equal logits and scores get equal ranks, and the lower one goes first.
-// A CTA's candidates find their places by counting those before them.  The last CTA of a group to finish (a counter, no waiting) joins the parts, ranks
-// in fp64, and moves the beams.
-//   32 x 16 beams over 131072 tokens: 73 us (3.7 TB/s: the copies wait for HBM under 24 warps an SM, 210 instructions per warp and
-// batch), histories of 512 tokens 4 us more; 8 x 4 over 50257 tokens 17 us, most of it the chain of dependent steps of a part
-// and of the join.
+// A CTA's candidates find their places by counting those before them.  The last CTA of a group to finish (a counter, no waiting)
+// joins the parts, ranks in fp64, and moves the beams.
+//   32 x 16 beams over 131072 tokens: 71 us (3.8 TB/s: 24 warps an SM, 210 instructions per warp and batch; a batch more on its way
+// changes nothing), histories of 512 tokens 3 us more; 8 x 4 over 50257 tokens 13 us, most of it the chain of dependent steps of
+// a part and of the join.
 #include "serve.cuh"
 
 namespace lookat {
@@ -22,6 +22,7 @@ namespace {
 constexpr int kBsThreads = 256, kBsWarps = kBsThreads / 32, kBsVecs = 4, kBsMost = 32;
 constexpr int kBsBatch = kBsThreads * kBsVecs * 4;            // logits that a CTA has in flight
 constexpr int kBsRing = 2 * kBsBatch * 4;                      // bytes of the batches in shared memory
+constexpr int kBsSplits = 64;                                  // most parts of a row
 constexpr int kBsHold = 32;                                    // candidates that a warp collects before it sorts them in
 
 struct BsPart {                     // of a row: its best logits, sum exp(x - m) and m
@@ -89,14 +90,41 @@ __device__ __forceinline__ float bs_sorted(float v, int lane)
     return v;
 }
 
+// the 32 largest of the lanes' numbers, in falling order, and of others in rising order: in falling order
+__device__ __forceinline__ float bs_merged(float v, float others, int lane)
+{
+    v = fmaxf(v, others);
+#pragma unroll
+    for (int j = 16; j; j >>= 1) {
+        const float o = __shfl_xor_sync(0xffffffffu, v, j);
+        v = (lane & j) == 0 ? fmaxf(v, o) : fminf(v, o);
+    }
+    return v;
+}
+// Ranks as whole numbers that go in the same order (as which they are compared faster; -0 and 0 are one)
+constexpr long long kBsNone = (long long)0x800fffffffffffffull;         // -inf
+__device__ __forceinline__ double bs_rank(long long key) { return __longlong_as_double(key ^ ((key >> 63) & 0x7fffffffffffffffll)); }
+__device__ __forceinline__ long long bs_key(double rank)
+{
+    const long long bits = __double_as_longlong(rank + 0.0);
+    return bits ^ ((bits >> 63) & 0x7fffffffffffffffll);
+}
+
 // What a group's beams were before the call, and where its rows' candidates stand.
 struct BsGroup {
     float score[kBsMost];
     int len[kBsMost], fin[kBsMost];
-    double base[kBsMost], norm[kBsMost], rank[kBsWarps][kBsMost];                   // rank = (base + (x - m)) / norm
+    double base[kBsMost], norm[kBsMost];                       // rank = (base + (x - m)) / norm
     float m[kBsMost];
-    int at[kBsWarps][kBsMost], parent[kBsMost], slot[kBsMost], token[kBsMost];
+    int parent[kBsMost], slot[kBsMost], token[kBsMost];
 };
+struct BsBest {                     // the warps' best of it, and the parts to look through
+    long long key[kBsWarps][kBsMost];
+    int at[kBsWarps][kBsMost];
+    float firsts[kBsWarps][kBsMost];
+    int count, list[kBsMost * kBsSplits];
+};
+static_assert(kBsThreads * 8 + sizeof(BsBest) <= kBsRing, "what lies over the batches once they are read");
 
 // Columns of the histories, of up to MOST beams each: all are read before the first is written.
 template <int MOST, class T>
@@ -114,89 +142,129 @@ __device__ __forceinline__ void beam_move(T *rows, int columns, int beams, const
 }
 
 // The group's parts joined and ranked, its beams moved.
-__device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const BsPart *__restrict__ parts, int group, BsGroup &g)
+__device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const BsPart *__restrict__ parts, int group, BsGroup &g, BsBest &warps)
 {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, W = a.beams;
     const int g0 = group * W;
     const BsPart *const p0 = parts + (size_t)g0 * splits;
-    // ---- the rows' sums ----
-    for (int w = warp; w < W; w += kBsWarps) {
-        const float sc = g.score[w];
-        const bool counts = sc > -INFINITY && sc < INFINITY;
-        const int grown = max(g.len[w] + (g.fin[w] ? 0 : 1), 1);
-        double base = counts ? (double)sc : -INFINITY;
-        float top = 0.f;
-        if (counts && !g.fin[w]) {
-            const BsPart *p = p0 + (size_t)w * splits, &q = p[min(lane, splits - 1)];
-            const float m0 = __ldcg(&q.m);                     // (up to 32 parts: all asked for at once)
-            const double sum0 = __ldcg(&q.sum);
-            bool bad = __ldcg(&q.bad) != 0;
-            top = m0;
-            for (int i = lane + 32; i < splits; i += 32) top = fmaxf(top, __ldcg(&p[i].m)), bad |= __ldcg(&p[i].bad) != 0;
-#pragma unroll
-            for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            bad = __any_sync(0xffffffffu, bad) || top == -INFINITY;
-            double total = 0.0;
-            if (lane < splits && m0 > -INFINITY) total = sum0 * exp((double)m0 - (double)top);
-            for (int i = lane + 32; i < splits; i += 32)
-                if (__ldcg(&p[i].m) > -INFINITY) total += __ldcg(&p[i].sum) * exp((double)__ldcg(&p[i].m) - (double)top);
-#pragma unroll
-            for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-            base = bad ? -INFINITY : base - log(total);
+    // A group of many parts looks through those only whose first is not behind the W-th of the threads' best firsts: about W of them,
+    // which takes as long to find as a warp takes for three more parts (8 x 4 beams over 50257 tokens, 52 parts a group, 12.9 us, 16.6
+    // through all of them; one group of 32 beams over 131072, 512 parts, 29 and 60; with 13 parts for one beam 13.8 and 11).
+    const int items = W * splits;
+    const bool chosen = items > W + 24;
+    const float head = chosen && tid < items ? __ldcg(&p0[tid].best[0]) : -INFINITY;
+    // ---- the rows' sums, as many lanes per row as there are ----
+    {
+        const int lanes = W <= 8 ? 32 : W <= 16 ? 16 : 8, w = tid / lanes, sub = tid % lanes;
+        const bool row = w < W;
+        const float sc = row ? g.score[w] : -INFINITY;
+        const bool counts = sc > -INFINITY && sc < INFINITY, goes_on = counts && !g.fin[w];
+        const BsPart *const p = p0 + (size_t)(row ? w : 0) * splits;
+        float top = -INFINITY;                                 // a lane's parts: sum exp(x - top)
+        double total = 0.0;
+        bool bad = false;
+        if (goes_on && sub < splits) {
+            top = __ldcg(&p[sub].m);
+            total = __ldcg(&p[sub].sum);
+            bad = __ldcg(&p[sub].bad) != 0;
         }
-        if (lane == 0) g.base[w] = base, g.norm[w] = a.penalty == 0.0 ? 1.0 : pow((double)grown, a.penalty), g.m[w] = top;
+#pragma unroll 1
+        for (int i = sub + lanes; goes_on && i < splits; i += lanes) {
+            const float m = __ldcg(&p[i].m);
+            const double sum = __ldcg(&p[i].sum);
+            bad |= __ldcg(&p[i].bad) != 0;
+            if (!(m > -INFINITY)) continue;
+            const double k = exp(-fabs((double)m - (double)top));              // (0 where there was none)
+            total = m > top ? fma(total, k, sum) : fma(sum, k, total);
+            top = fmaxf(top, m);
+        }
+        float most = top;
+        for (int o = lanes / 2; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        total = top > -INFINITY ? total * exp((double)top - (double)most) : 0.0;
+        for (int o = lanes / 2; o; o >>= 1) {
+            total += __shfl_xor_sync(0xffffffffu, total, o);
+            bad |= __shfl_xor_sync(0xffffffffu, (int)bad, o) != 0;
+        }
+        if (row && sub == 0) {
+            const int grown = max(g.len[w] + (g.fin[w] ? 0 : 1), 1);
+            g.base[w] = !counts || (goes_on && (bad || most == -INFINITY)) ? -INFINITY : goes_on ? (double)sc - log(total) : (double)sc;
+            g.norm[w] = a.penalty == 0.0 ? 1.0 : pow((double)grown, a.penalty);
+            g.m[w] = goes_on ? most : 0.f;
+        }
     }
     __syncthreads();
     // ---- the best of all parts' candidates, which stand first to last there: read last to first ----
-    BsBlock<double> best = {-INFINITY, 0x7fffffff};
+    auto rank_of = [&](int item, float x, bool first) {        // of a part's candidate
+        const int w = item / splits;
+        const double base = g.base[w], norm = g.norm[w];
+        if (!(base > -INFINITY) || (g.fin[w] ? item != w * splits || !first : !(x > -INFINITY))) return (double)-INFINITY;    // (finished: itself, once)
+        const double score = g.fin[w] ? base : base + ((double)x - (double)g.m[w]);
+        return norm == 1.0 ? score : score / norm;
+    };
+    int count = items;
+    if (chosen) {
+        // (fp32, rounded up: in the same order)
+        const float mine = tid < items ? __double2float_ru(rank_of(tid, head, true)) : -INFINITY;
+        float top = mine;
+        for (int item = tid + kBsThreads; item < items; item += kBsThreads) top = fmaxf(top, __double2float_ru(rank_of(item, __ldcg(&p0[item].best[0]), true)));
+        if (tid == 0) warps.count = 0;
+        top = bs_sorted(top, lane);
+        warps.firsts[warp][lane] = top;
+#pragma unroll 1
+        for (int half = kBsWarps / 2; half; half >>= 1) {
+            __syncthreads();
+            if (warp < half) warps.firsts[warp][lane] = top = bs_merged(top, warps.firsts[warp + half][31 - lane], lane);
+        }
+        __syncthreads();
+        const float bar = warps.firsts[0][W - 1];
+        if (mine > -INFINITY && mine >= bar) warps.list[atomicAdd(&warps.count, 1)] = tid;
+        for (int item = tid + kBsThreads; item < items; item += kBsThreads) {
+            const float first = __double2float_ru(rank_of(item, __ldcg(&p0[item].best[0]), true));
+            if (first > -INFINITY && first >= bar) warps.list[atomicAdd(&warps.count, 1)] = item;
+        }
+        __syncthreads();
+        count = warps.count;
+    }
+    BsBlock<long long> best = {kBsNone, 0x7fffffff};
     constexpr int kAhead = 4;
 #pragma unroll 1
-    for (int i0 = warp; i0 < W * splits; i0 += kBsWarps * kAhead) {
+    for (int i0 = warp; i0 < count; i0 += kBsWarps * kAhead) {
         float x[kAhead];
-        int at[kAhead];
+        int at[kAhead], item[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const BsPart &q = p0[min(i0 + i * kBsWarps, W * splits - 1)];
-            x[i] = __ldcg(&q.best[31 - lane]);
-            at[i] = __ldcg(&q.at[31 - lane]);
+            const int k = min(i0 + i * kBsWarps, count - 1);
+            item[i] = chosen ? warps.list[k] : k;
+            x[i] = __ldcg(&p0[item[i]].best[31 - lane]);
+            at[i] = __ldcg(&p0[item[i]].at[31 - lane]);
         }
 #pragma unroll 1
-        for (int i = 0; i < kAhead; ++i) {
-            const int item = i0 + i * kBsWarps, w = min(item, W * splits - 1) / splits;
+        for (int i = 0; i < kAhead && i0 + i * kBsWarps < count; ++i) {
             const float xi = i == 0 ? x[0] : i == 1 ? x[1] : i == 2 ? x[2] : x[3];
-            const int ai = i == 0 ? at[0] : i == 1 ? at[1] : i == 2 ? at[2] : at[3];
-            const double base = g.base[w], norm = g.norm[w];
-            bool on = item < W * splits && base > -INFINITY;
-            double score = base + ((double)xi - (double)g.m[w]);
-            int where = w * a.vocab + ai;
-            if (g.fin[w]) {                                    // itself, once
-                on = on && item == w * splits && lane == 31;
-                score = base;
-                where = w * a.vocab + max(a.eos, 0);
-            } else {
-                on = on && xi > -INFINITY;
-            }
-            const double rank = !on ? -INFINITY : norm == 1.0 ? score : score / norm, bar = __shfl_sync(0xffffffffu, best.key, W - 1);
-            if (__any_sync(0xffffffffu, on && rank >= bar)) best.join(rank, on ? where : 0x7fffffff, lane);
+            const int ai = i == 0 ? at[0] : i == 1 ? at[1] : i == 2 ? at[2] : at[3], it = i == 0 ? item[0] : i == 1 ? item[1] : i == 2 ? item[2] : item[3];
+            const int w = it / splits;
+            const long long key = bs_key(rank_of(it, xi, lane == 31)), bar = __shfl_sync(0xffffffffu, best.key, W - 1);
+            const bool on = key > kBsNone;
+            if (__any_sync(0xffffffffu, on && key >= bar)) best.join(key, on ? w * a.vocab + (g.fin[w] ? max(a.eos, 0) : ai) : 0x7fffffff, lane);
         }
     }
-    g.rank[warp][lane] = best.key;
-    g.at[warp][lane] = best.at;
+    warps.key[warp][lane] = best.key;
+    warps.at[warp][lane] = best.at;
 #pragma unroll 1
     for (int half = kBsWarps / 2; half; half >>= 1) {
         __syncthreads();
         if (warp < half) {
-            best.join(g.rank[warp + half][31 - lane], g.at[warp + half][31 - lane], lane);
-            g.rank[warp][lane] = best.key;
-            g.at[warp][lane] = best.at;
+            best.join(warps.key[warp + half][31 - lane], warps.at[warp + half][31 - lane], lane);
+            warps.key[warp][lane] = best.key;
+            warps.at[warp][lane] = best.at;
         }
     }
     if (warp == 0 && lane < W) {
-        const bool there = best.key > -INFINITY;
+        const bool there = best.key > kBsNone;
         const int parent = there ? best.at / a.vocab : lane, token = there ? best.at % a.vocab : max(a.eos, 0);
         const bool grows = there && !g.fin[parent];
         const int was = g.len[parent];
-        a.scores[g0 + lane] = !there ? -INFINITY : g.fin[parent] ? g.score[parent] : (float)(best.key * g.norm[parent]);
+        a.scores[g0 + lane] = !there ? -INFINITY : g.fin[parent] ? g.score[parent] : (float)(bs_rank(best.key) * g.norm[parent]);
         a.lengths[g0 + lane] = was + (grows ? 1 : 0);
         a.finished[g0 + lane] = g.fin[parent] || (grows && token == a.eos);
         a.next_ids[g0 + lane] = token;
@@ -240,15 +308,17 @@ __global__ void __launch_bounds__(kBsThreads, 4)
 beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsPart *__restrict__ parts, unsigned *__restrict__ tickets)
 {
     extern __shared__ float4 beam_smem[];
-    __shared__ float s_hold[kBsWarps][kBsHold + 128];           // a warp's candidates
-    __shared__ int s_hold_at[kBsWarps][kBsHold + 128];
-    __shared__ __align__(8) float2 s_all[kBsThreads];          // all warps' last candidates: logit, element
+    __shared__ float s_hold[kBsWarps][kBsHold + 32];           // a warp's candidates
+    __shared__ int s_hold_at[kBsWarps][kBsHold + 32];
     __shared__ int s_count[kBsWarps];
     __shared__ BsGroup s_group;
     __shared__ double s_sum[kBsWarps];
     __shared__ float s_m[kBsWarps];
     __shared__ int s_bad[kBsWarps], s_last;
     __shared__ __align__(16) float s_bars[4 * kBsWarps];       // the largest of the lanes' largest logits, four of each warp
+    // once the batches are read: all warps' last candidates (logit, element), the group's best
+    float2 *const s_all = reinterpret_cast<float2 *>(beam_smem);
+    BsBest &s_best = *reinterpret_cast<BsBest *>(s_all + kBsThreads);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, W = a.beams;
     const int row = blockIdx.x / splits, split = blockIdx.x % splits, group = row / W;
     const float score = a.scores[row];
@@ -371,8 +441,8 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
                     const int at = held + __popc(who & ((1u << lane) - 1));
                     if (on) s_hold[warp][at] = x[i][j], s_hold_at[warp][at] = element(e0, i, j);
                     held += __popc(who);
+                    if (held > kBsHold) sort_in();
                 }
-                if (held > kBsHold) sort_in();
             }
         }
         // ---- the part's best: a warp brings what it holds, or its best if it has sorted, and each finds its place by counting ----
@@ -433,7 +503,7 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
     __syncthreads();
     if (!s_last) return;
     __threadfence();
-    beam_finish(a, splits, parts, group, s_group);
+    beam_finish(a, splits, parts, group, s_group, s_best);
 }
 
 }  // namespace
@@ -447,7 +517,7 @@ lookat_status launch_beam_select(Ctx *ctx, const BeamArgs &a)
     const long long slots = 4ll * ctx->sm_count;
     long long splits = 1, least = 0;
     int per = batches;
-    for (int s = 1; s <= batches && s <= 64; ++s) {
+    for (int s = 1; s <= batches && s <= kBsSplits; ++s) {
         const int each = (batches + s - 1) / s;
         const long long cost = (rows * s + slots - 1) / slots * (each + 6);
         if (s == 1 || cost < least) least = cost, per = each;

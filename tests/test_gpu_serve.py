@@ -534,6 +534,31 @@ def test_beam_select(G, W, V, L, penalty, first, eos):
     check_beams(case, eos, penalty)
 
 
+@pytest.mark.parametrize("penalty,first,eos", [(0.0, False, 0), (0.7, False, -1), (1.0, True, 3)])
+def test_beam_select_many_parts(penalty, first, eos):
+    """More parts in a group than a CTA has threads."""
+    rng = np.random.default_rng(5)
+    for _ in range(20):                                         # (on the CPU: a case whose ranks can be told apart)
+        case = beam_case(rng, 1, 32, 90001, 3, first=first)
+        if serve.beam_select(*case, eos, penalty)[6] > GAP:
+            break
+    check_beams(case, eos, penalty)
+
+
+def test_beam_select_many_parts_of_equal_logits():
+    """Where every part's first is as good as any other, the lowest tokens of the first beam; and masked ones after the rest."""
+    V = 90001
+    for value in (0.0, -1e4, float(torch.finfo(torch.float32).min)):
+        st = BeamState(torch.zeros(1, 32, device="cuda"), i32([[2] * 32]), i32([[0] * 32]))
+        lk = Lookat(2, 2, 64, 64, 1, 16)
+        ids, parents = lk.lookat_beam_select(st, torch.full((32, V), value, device="cuda"), length_penalty=0.5)
+        assert finding(lk) == "" and ids.tolist() == list(range(32)) and parents.tolist() == [0] * 32
+    scores, lengths, finished, tokens, logits = beam_case(np.random.default_rng(6), 1, 32, V, 3, done=0.0)
+    logits[:] = np.finfo(np.float32).min
+    logits[4, [9, 50000, 90000]], logits[30, [1, 60000]] = [2.0, 1.0, 0.5], [0.25, -1.0]
+    check_beams((scores, lengths, finished, tokens, logits), 0, 0.0)
+
+
 def test_beam_select_rows_at_any_alignment():
     """Rows of an odd vocabulary, dense and inside a wider buffer, at every alignment of 4 bytes."""
     rng = np.random.default_rng(5)
