@@ -3,7 +3,9 @@
 // A line is one (token, query head) pair of a KV head, line = token * g + head, so that a tile's lines share the keys they see.
 // A CTA has 64 lines of one row and KV head, 16 per warp, against blocks of 64 tokens in shared memory; both products on
 // mma.sync.m16n8k16 (fp16 in, fp32 accumulate), the softmax with a running exponent in between.  Dims are padded with zeros to
-// DIM in shared memory.  Head dims of 64 and 128 go to attend_packed_umma.cu, but for short rows: 4 x 4096 tokens, 32 and 8 heads of
+// DIM in shared memory.  The sum is over the weights as they are rounded for the second product, so that what the values have in
+// common is not touched by their rounding (96 dims, 4 x 1024 tokens: 91 us, as over the unrounded ones; by conversions back from
+// fp16 104).  Head dims of 64 and 128 go to attend_packed_umma.cu, but for short rows: 4 x 4096 tokens, 32 and 8 heads of
 // 128, take 2.5 ms here and 0.53 there.  Bound by the issue of the products: one barrier pair, one softmax and 16 to 64 products of
 // 16 x 8 x 16 per warp and 16 dims of a block, with nothing in flight meanwhile.
 #include "serve.cuh"
@@ -96,10 +98,15 @@ __global__ void __launch_bounds__(kPaThreads) attend_packed_kernel(PackedAttendA
         float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
         for (int nt = 0; nt < 8; ++nt) {
-            const float e0 = ex2_approx(s[nt][0] - n0), e1 = ex2_approx(s[nt][1] - n0), e2 = ex2_approx(s[nt][2] - n1), e3 = ex2_approx(s[nt][3] - n1);
-            sum0 += e0 + e1;
-            sum1 += e2 + e3;
-            const __half2 h01 = __floats2half2_rn(e0, e1), h23 = __floats2half2_rn(e2, e3);
+            float e[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float x = ex2_approx(s[nt][i] - (i < 2 ? n0 : n1));
+                e[i] = fmaf(x, -8192.f, fmaf(x, 8192.f, x));   // to 11 bits: the first sum is rounded 13 bits above x's last
+            }
+            sum0 += e[0] + e[1];
+            sum1 += e[2] + e[3];
+            const __half2 h01 = __floats2half2_rn(e[0], e[1]), h23 = __floats2half2_rn(e[2], e[3]);
             w[nt >> 1][(nt & 1) * 2] = *reinterpret_cast<const uint32_t *>(&h01);
             w[nt >> 1][(nt & 1) * 2 + 1] = *reinterpret_cast<const uint32_t *>(&h23);
         }
