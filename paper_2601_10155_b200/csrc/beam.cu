@@ -315,7 +315,7 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
     __shared__ double s_sum[kBsWarps];
     __shared__ float s_m[kBsWarps];
     __shared__ int s_bad[kBsWarps], s_last;
-    __shared__ __align__(16) float s_bars[4 * kBsWarps];       // the largest of the lanes' largest logits, four of each warp
+    __shared__ float s_bars[2][4 * kBsWarps];                  // the largest of the lanes' largest logits, four of each warp
     // once the batches are read: all warps' last candidates (logit, element), the group's best
     float2 *const s_all = reinterpret_cast<float2 *>(beam_smem);
     BsBest &s_best = *reinterpret_cast<BsBest *>(s_all + kBsThreads);
@@ -415,11 +415,13 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
             }
             if ((batch & (batch - 1)) == 0) {
                 // the bar, renewed at batches 1, 2, 4, ...: the `beams`-th of 32 of the part's logits, the largest four lanes' of every
-                // warp (what another warp has not renewed yet are logits of the part as well)
+                // warp.  All warps come here (they have the same batches), and the next renewal writes to the other half: a warp's four
+                // are seen as it wrote them, so that no logit counts twice.
+                float *const bars = s_bars[__popc(batch - 1) & 1];
                 const float in_order = bs_sorted(lane_top, lane);
-                if (lane < 4) *(volatile float *)&s_bars[warp * 4 + lane] = in_order;
-                if (batch == 1) __syncthreads();
-                bar = fmaxf(bar, __shfl_sync(0xffffffffu, bs_sorted(*(volatile float *)&s_bars[lane], lane), W - 1));
+                if (lane < 4) bars[warp * 4 + lane] = in_order;
+                __syncthreads();
+                bar = fmaxf(bar, __shfl_sync(0xffffffffu, bs_sorted(bars[lane], lane), W - 1));
             }
             limit = fminf(bar, m + 20.f);
             float2 add[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};

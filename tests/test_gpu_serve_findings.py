@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2601_10155_b200.binding import Lookat
-from test_gpu_serve import finding, i32, starts_of
+from test_gpu_serve import beam_case, check_beams, finding, i32, starts_of
 
 pytestmark = pytest.mark.gpu
 
@@ -38,3 +38,17 @@ def test_attend_packed_of_values_with_a_common_offset(H, H_kv, d, lens):
             bound = 2.0 ** -11 + rel * apart + (2 * (hi - lo) + 4) * 2.0 ** -23 * want
             err = (out[lo:hi, h].double() - want).abs()
             assert bool((err <= bound).all()), f"off by up to {float((err / bound).max()):.4g} of the bound"
+
+
+# ------------------------------------------------------------------------------------------------ beam selection
+@pytest.mark.parametrize("G,W", [(1, 32), (200, 3), (70, 8)])
+def test_beam_select_logits_that_rise_along_the_row(G, W):
+    """Every renewal of the bar that candidates have to reach moves it, in parts of one batch of 4096 logits and of many; a bar
+    above a part's W-th largest logit would lose a candidate."""
+    rng = np.random.default_rng(W)
+    V = 9 * 4096 + 77
+    scores, lengths, finished, tokens, logits = beam_case(rng, G, W, V, 2, done=0.0, first=True, masked=0.0)
+    rise = np.linspace(-20, 20, V)                              # a neighbour is 1e-3 away
+    logits[:] = rise.astype(np.float32)
+    logits[0] = np.where(np.arange(V) % 7 == 0, -np.inf, rise)
+    check_beams((scores, lengths, finished, tokens, logits), -1, 0.0)
