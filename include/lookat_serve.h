@@ -138,7 +138,7 @@ typedef struct lookat_beam_state {
  *
  *   logits          fp32 [groups * beams] rows of `vocab`, logits_stride elements apart (any alignment of 4 bytes)
  *   eos             the token that ends a beam, or -1
- *   length_penalty  0 compares plain sums; finite and not negative
+ *   length_penalty  0 compares plain sums; 0 to 28 (beyond, the norm of a long beam would leave no fp64 rank)
  * Requires groups * beams <= 65535, vocab * beams <= 2^30, 0 <= max_len <= 2^24.
  */
 lookat_status lookat_beam_select(lookat_ctx *ctx, const lookat_beam_state *state, const float *logits, int64_t logits_stride,

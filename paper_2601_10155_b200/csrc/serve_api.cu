@@ -10,6 +10,9 @@ namespace lookat {
 namespace {
 
 constexpr int64_t kMaxTokens = 1ll << 30;
+// With lengths below 2^31 a norm is at most 2^868, so that the rank of the smallest fp32 score, 2^-149, is still a normal fp64
+// number, and the score is what the rank times the norm is, to 2^-52.
+constexpr double kMaxPenalty = 28.0;
 
 // fp16 vectors of n tokens and `heads` heads
 lookat_status rows_of(Ctx *ctx, const lookat_rows *r, int64_t n, int heads, const char *name, Rows *out)
@@ -209,8 +212,8 @@ lookat_status lookat_beam_select(lookat_ctx *handle, const lookat_beam_state *st
     if (logits_stride < vocab || logits_stride >= (1ll << 31))
         return set_error(ctx, LOOKAT_ERR_INVALID_ARG, "logits_stride=%lld is less than vocab, or 2^31 or more", (long long)logits_stride);
     if (eos < -1 || eos >= vocab) return set_error(ctx, LOOKAT_ERR_INVALID_ARG, "eos=%d is not -1 or a token", (int)eos);
-    if (!(length_penalty >= 0) || !std::isfinite(length_penalty))
-        return set_error(ctx, LOOKAT_ERR_INVALID_ARG, "length_penalty is not a finite number of at least 0");
+    if (!(length_penalty >= 0 && length_penalty <= kMaxPenalty))
+        return set_error(ctx, LOOKAT_ERR_INVALID_ARG, "length_penalty is not a number in 0..%g", kMaxPenalty);
     if (s.max_len < 0 || s.max_len > (1 << 24) || (s.max_len > 0) != (s.tokens != nullptr))
         return set_error(ctx, LOOKAT_ERR_INVALID_ARG, "max_len=%d out of range 0..2^24, or not 0 without tokens", (int)s.max_len);
     Q8_TRY(need(ctx, s.scores, "state.scores", 4));

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2601_10155_b200.binding import Lookat
+from paper_2601_10155_b200.binding import BeamState, Lookat, LookatError
 from test_gpu_serve import beam_case, check_beams, finding, i32, starts_of
 
 pytestmark = pytest.mark.gpu
@@ -52,3 +52,32 @@ def test_beam_select_logits_that_rise_along_the_row(G, W):
     logits[:] = rise.astype(np.float32)
     logits[0] = np.where(np.arange(V) % 7 == 0, -np.inf, rise)
     check_beams((scores, lengths, finished, tokens, logits), -1, 0.0)
+
+
+def test_beam_select_the_largest_length_penalties():
+    """Norms of up to 2^868: beams of one length are ranked as without a penalty and keep their scores; a longer beam goes before
+    a shorter one.  Penalties beyond that are refused: their norms could overflow, and rank times norm is then no score."""
+    rng = np.random.default_rng(4)
+    lk = Lookat(2, 2, 64, 64, 1, 16)
+    x = torch.from_numpy(rng.standard_normal((6, 500)).astype(np.float32)).cuda()
+    scores = torch.from_numpy((-1e-3 * rng.random((2, 3))).astype(np.float32)).cuda()
+    for length in (0, 200, 2 ** 31 - 3):
+        got = []
+        for penalty in (0.0, 28.0):
+            st = BeamState(scores.clone(), i32([[length] * 3] * 2), i32([[0, 0, 0]] * 2))
+            ids, parents = lk.lookat_beam_select(st, x, length_penalty=penalty)
+            assert finding(lk) == ""
+            got.append((ids.tolist(), parents.tolist()))
+            if penalty:                                         # rank times norm: one more rounding in fp64
+                assert bool(((st.scores - plain).abs() <= plain.abs() * 2.0 ** -23).all())
+            plain = st.scores
+        assert got[0] == got[1]
+    st = BeamState(torch.zeros(2, 3, device="cuda"), i32([[9, 199, 10]] * 2), i32([[0, 0, 0]] * 2))
+    ids, parents = lk.lookat_beam_select(st, x, length_penalty=28.0)
+    assert finding(lk) == "" and parents.tolist() == [1] * 3 + [4] * 3
+    want = torch.log_softmax(x[1::3].double(), dim=1).topk(3)
+    assert ids.tolist() == want.indices.reshape(-1).tolist()
+    assert bool(((st.scores.double() - want.values).abs() <= want.values.abs() * 2.0 ** -24 + 2.0 ** -20).all())
+    for penalty in (28.5, 150.0, 1e308, math.nan):
+        with pytest.raises(LookatError, match="length_penalty"):
+            lk.lookat_beam_select(st, x, length_penalty=penalty)
