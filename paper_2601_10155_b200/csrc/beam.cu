@@ -1,8 +1,10 @@
 // lookat_beam_select: one step of beam search.
 //
 // Bound by HBM: the logits are read once.  A row is cut into `splits` parts, a CTA each; in one pass a warp keeps
-//   - sum exp(x - m) against a reference m that it takes from its first logits and seldom moves: fp32 exponentials, their sums
-//     fp64, so that the ranks of different beams are compared to 1e-8;
+//   - sum exp(x - M) against a reference M that follows its largest logit at a distance of at most 1: fp32 exponentials, sixteen
+//     of a lane added in fp32 before they go into fp64 sums.  A term at distance d is off by 2^-22 (ex2.approx), 5 * 2^-24 (the
+//     additions) and d * 1.25 * 2^-24 (its exponent, and log2(e) as an fp32 number) of itself: a row with one likely token by
+//     less than 2^-20, one of very many tokens 20 below the largest by less than 2^-18;
 //   - its best 32 logits (a beam's candidates rank as its logits do), sorted over the lanes.  What reaches a bar is collected in
 //     shared memory and sorted in 32 at a time (a bitonic sort and a merge).  The bar comes from the lanes' largest logits so far
 //     and is renewed at the batches 1, 2, 4, ...: few logits reach it.
@@ -25,11 +27,10 @@ constexpr int kBsRing = 2 * kBsBatch * 4;                      // bytes of the b
 constexpr int kBsSplits = 64;                                  // most parts of a row
 constexpr int kBsHold = 32;                                    // candidates that a warp collects before it sorts them in
 
-struct BsPart {                     // of a row: its best logits, sum exp(x - m) and m
+struct BsPart {                     // of a row: its best logits, sum exp(x - M) and M
     float best[kBsMost];
     int at[kBsMost];
-    double sum;
-    float m;
+    double sum, m;
     int bad;                        // a NaN or +inf among them
 };
 
@@ -68,12 +69,13 @@ __device__ __forceinline__ float bs_max_nan(float a, float b, float c)          
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
     return d;
 }
-// exp(x - m), exp(y - m), added to sum: the differences and products two at a time
-__device__ __forceinline__ void bs_add_exp2(float2 &sum, float x, float y, float minus_m)
+constexpr float kBsLog2e = 1.4426950408889634f;
+// exp(x - M), exp(y - M), added to sum, for M = -c / log2(e): the exponents two at a time, rounded once
+__device__ __forceinline__ void bs_add_exp2(float2 &sum, float x, float y, float c)
 {
     float u, v;
-    asm("{\n.reg .b64 a, b;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %4};\nadd.rn.f32x2 a, a, b;\nmov.b64 b, {%5, %5};\nmul.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}"
-        : "=f"(u), "=f"(v) : "f"(x), "f"(y), "f"(minus_m), "f"(1.4426950408889634f));
+    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %4};\nmov.b64 d, {%5, %5};\nfma.rn.f32x2 a, a, b, d;\nmov.b64 {%0, %1}, a;\n}"
+        : "=f"(u), "=f"(v) : "f"(x), "f"(y), "f"(kBsLog2e), "f"(c));
     u = ex2_approx(u), v = ex2_approx(v);
     asm("{\n.reg .b64 a, b;\nmov.b64 a, {%0, %1};\nmov.b64 b, {%2, %3};\nadd.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}" : "+f"(sum.x), "+f"(sum.y) : "f"(u), "f"(v));
 }
@@ -114,8 +116,7 @@ __device__ __forceinline__ long long bs_key(double rank)
 struct BsGroup {
     float score[kBsMost];
     int len[kBsMost], fin[kBsMost];
-    double base[kBsMost], norm[kBsMost];                       // rank = (base + (x - m)) / norm
-    float m[kBsMost];
+    double base[kBsMost], norm[kBsMost], m[kBsMost];           // rank = (base + (x - m)) / norm
     int parent[kBsMost], slot[kBsMost], token[kBsMost];
 };
 struct BsBest {                     // the warps' best of it, and the parts to look through
@@ -160,8 +161,7 @@ __device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const Bs
         const float sc = row ? g.score[w] : -INFINITY;
         const bool counts = sc > -INFINITY && sc < INFINITY, goes_on = counts && !g.fin[w];
         const BsPart *const p = p0 + (size_t)(row ? w : 0) * splits;
-        float top = -INFINITY;                                 // a lane's parts: sum exp(x - top)
-        double total = 0.0;
+        double top = -INFINITY, total = 0.0;                   // a lane's parts: sum exp(x - top)
         bool bad = false;
         if (goes_on && sub < splits) {
             top = __ldcg(&p[sub].m);
@@ -170,17 +170,16 @@ __device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const Bs
         }
 #pragma unroll 1
         for (int i = sub + lanes; goes_on && i < splits; i += lanes) {
-            const float m = __ldcg(&p[i].m);
-            const double sum = __ldcg(&p[i].sum);
+            const double m = __ldcg(&p[i].m), sum = __ldcg(&p[i].sum);
             bad |= __ldcg(&p[i].bad) != 0;
             if (!(m > -INFINITY)) continue;
-            const double k = exp(-fabs((double)m - (double)top));              // (0 where there was none)
+            const double k = exp(-fabs(m - top));              // (0 where there was none)
             total = m > top ? fma(total, k, sum) : fma(sum, k, total);
-            top = fmaxf(top, m);
+            top = fmax(top, m);
         }
-        float most = top;
-        for (int o = lanes / 2; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-        total = top > -INFINITY ? total * exp((double)top - (double)most) : 0.0;
+        double most = top;
+        for (int o = lanes / 2; o; o >>= 1) most = fmax(most, __shfl_xor_sync(0xffffffffu, most, o));
+        total = top > -INFINITY ? total * exp(top - most) : 0.0;
         for (int o = lanes / 2; o; o >>= 1) {
             total += __shfl_xor_sync(0xffffffffu, total, o);
             bad |= __shfl_xor_sync(0xffffffffu, (int)bad, o) != 0;
@@ -189,7 +188,7 @@ __device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const Bs
             const int grown = max(g.len[w] + (g.fin[w] ? 0 : 1), 1);
             g.base[w] = !counts || (goes_on && (bad || most == -INFINITY)) ? -INFINITY : goes_on ? (double)sc - log(total) : (double)sc;
             g.norm[w] = a.penalty == 0.0 ? 1.0 : pow((double)grown, a.penalty);
-            g.m[w] = goes_on ? most : 0.f;
+            g.m[w] = goes_on ? most : 0.0;
         }
     }
     __syncthreads();
@@ -198,7 +197,7 @@ __device__ __noinline__ void beam_finish(const BeamArgs &a, int splits, const Bs
         const int w = item / splits;
         const double base = g.base[w], norm = g.norm[w];
         if (!(base > -INFINITY) || (g.fin[w] ? item != w * splits || !first : !(x > -INFINITY))) return (double)-INFINITY;    // (finished: itself, once)
-        const double score = g.fin[w] ? base : base + ((double)x - (double)g.m[w]);
+        const double score = g.fin[w] ? base : base + ((double)x - g.m[w]);
         return norm == 1.0 ? score : score / norm;
     };
     int count = items;
@@ -312,8 +311,7 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
     __shared__ int s_hold_at[kBsWarps][kBsHold + 32];
     __shared__ int s_count[kBsWarps];
     __shared__ BsGroup s_group;
-    __shared__ double s_sum[kBsWarps];
-    __shared__ float s_m[kBsWarps];
+    __shared__ double s_sum[kBsWarps], s_m[kBsWarps];
     __shared__ int s_bad[kBsWarps], s_last;
     __shared__ float s_bars[2][4 * kBsWarps];                  // the largest of the lanes' largest logits, four of each warp
     // once the batches are read: all warps' last candidates (logit, element), the group's best
@@ -333,7 +331,12 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
         const float *x0 = a.logits + (long long)row * a.stride;
         const int e1 = min((split + 1) * part, a.vocab);
         BsBlock<float> best = {-INFINITY, 0x7fffffff};
-        float bar = -INFINITY, m = -INFINITY, minus_m = 0.f, limit = -INFINITY;     // limit: what to look at closer
+        float bar = -INFINITY, m = -INFINITY, limit = -INFINITY;     // limit: what to look at closer
+        // The reference M: -c / log2(e), c a whole number (a new one moves the sum by a power of 2, exactly); or where that would
+        // leave too few bits, the logit m itself (`far`), from which those that count differ by exact numbers.
+        float c = 0.f;
+        bool far = false;
+        auto reference = [&]() { return far ? (double)m : -(double)c * (1.0 / (double)kBsLog2e); };
         int held = 0;
         double sum = 0.0;
         float lane_top = -INFINITY;
@@ -344,7 +347,7 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
             best = beam_sort_in(best, s_hold[warp], s_hold_at[warp], held);
             held = 0;
             bar = fmaxf(bar, __shfl_sync(0xffffffffu, best.key, W - 1));
-            limit = fminf(bar, m + 20.f);
+            limit = fminf(bar, m + 1.f);
         };
         // A batch's logits by way of the thread's own places in shared memory, one batch ahead.  Element of a batch: e0 + 4 tid +
         // 1024 i + j (wide), or e0 + tid + 256 (4 i + j); places hold 16 bytes: [buffer][i][thread].
@@ -402,35 +405,55 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
             const bool hit = __any_sync(0xffffffffu, !(top < limit));
             lane_top = fmaxf(lane_top, top);
             ++batch;
+            float to = -INFINITY;                              // where the reference goes
             if (hit) {
                 bad |= __any_sync(0xffffffffu, !(top < INFINITY));             // nothing of the row counts any more
-                if (__any_sync(0xffffffffu, top > m + 20.f)) {
-                    float most = top;
+                if (__any_sync(0xffffffffu, top > m + 1.f)) {
+                    to = top;
 #pragma unroll
-                    for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-                    if (m > -INFINITY) sum *= exp((double)m - (double)most);
-                    m = most;
-                    minus_m = -most;
+                    for (int o = 16; o; o >>= 1) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, o));
                 }
             }
             if ((batch & (batch - 1)) == 0) {
                 // the bar, renewed at batches 1, 2, 4, ...: the `beams`-th of 32 of the part's logits, the largest four lanes' of every
                 // warp.  All warps come here (they have the same batches), and the next renewal writes to the other half: a warp's four
-                // are seen as it wrote them, so that no logit counts twice.
+                // are seen as it wrote them, so that no logit counts twice.  The largest of all is the reference.
                 float *const bars = s_bars[__popc(batch - 1) & 1];
                 const float in_order = bs_sorted(lane_top, lane);
                 if (lane < 4) bars[warp * 4 + lane] = in_order;
                 __syncthreads();
-                bar = fmaxf(bar, __shfl_sync(0xffffffffu, bs_sorted(bars[lane], lane), W - 1));
+                const float of_all = bs_sorted(bars[lane], lane);
+                bar = fmaxf(bar, __shfl_sync(0xffffffffu, of_all, W - 1));
+                to = __shfl_sync(0xffffffffu, of_all, 0);
             }
-            limit = fminf(bar, m + 20.f);
-            float2 add[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+            if (to > m) {
+                const double was = reference();
+                const float c1 = -ceilf(to * kBsLog2e);
+                if (!far && fabsf(to) <= 0x1p20f) {
+                    const int k = min(max((int)(c1 - c), -1023), 0);           // (above 0 only before the first, with nothing summed)
+                    sum *= __hiloint2double((1023 + k) << 20, 0);
+                    c = c1, m = to;
+                } else {
+                    far = !(fabsf(to) <= 0x1p20f);
+                    c = c1, m = to;
+                    sum = sum > 0.0 ? sum * exp(was - reference()) : 0.0;
+                }
+            }
+            limit = fminf(bar, m + 1.f);
+            if (!far) {
+                float2 add[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-            for (int i = 0; i < kBsVecs; ++i) {
-                bs_add_exp2(add[0], x[i][0], x[i][1], minus_m);
-                bs_add_exp2(add[1], x[i][2], x[i][3], minus_m);
+                for (int i = 0; i < kBsVecs; ++i) {
+                    bs_add_exp2(add[0], x[i][0], x[i][1], c);
+                    bs_add_exp2(add[1], x[i][2], x[i][3], c);
+                }
+                sum += (double)((add[0].x + add[0].y) + (add[1].x + add[1].y));
+            } else {
+#pragma unroll 1
+                for (int k = 0; k < 4 * kBsVecs; ++k)
+                    if (element(e0, k >> 2, k & 3) < e1)
+                        sum += (double)ex2_approx((reinterpret_cast<const float *>(place + ((~batch & 1) * kBsVecs + (k >> 2)) * kBsThreads)[k & 3] - m) * kBsLog2e);
             }
-            sum += (double)((add[0].x + add[0].y) + (add[1].x + add[1].y));
             if (!hit) continue;
 #pragma unroll
             for (int i = 0; i < kBsVecs; ++i) {
@@ -457,7 +480,7 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
         }
 #pragma unroll
         for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane == 0) s_sum[warp] = sum, s_m[warp] = m, s_bad[warp] = bad, s_count[warp] = held;
+        if (lane == 0) s_sum[warp] = sum, s_m[warp] = m > -INFINITY ? reference() : -INFINITY, s_bad[warp] = bad, s_count[warp] = held;
         __syncthreads();
         int first = 0, n = 0;
 #pragma unroll
@@ -483,11 +506,10 @@ beam_select_kernel(const __grid_constant__ BeamArgs a, int splits, int part, BsP
         const int real = __syncthreads_count(tid < n && s_all[min(tid, n - 1)].x > -INFINITY);
         if (tid >= real && tid < kBsMost) p.best[tid] = -INFINITY, p.at[tid] = 0x7fffffff;
         if (warp == 0) {
-            float top = -INFINITY;
+            double top = -INFINITY, mine = 0.0;
             bool any_bad = false;
-            for (int w = 0; w < kBsWarps; ++w) top = fmaxf(top, s_m[w]), any_bad |= s_bad[w] != 0;
-            double mine = 0.0;
-            if (lane < kBsWarps && s_m[lane] > -INFINITY) mine = s_sum[lane] * exp((double)s_m[lane] - (double)top);
+            for (int w = 0; w < kBsWarps; ++w) top = fmax(top, s_m[w]), any_bad |= s_bad[w] != 0;
+            if (lane < kBsWarps && s_m[lane] > -INFINITY) mine = s_sum[lane] * exp(s_m[lane] - top);
 #pragma unroll
             for (int o = kBsWarps / 2; o; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
             if (lane == 0) p.sum = mine, p.m = top, p.bad = any_bad;

@@ -81,3 +81,43 @@ def test_beam_select_the_largest_length_penalties():
     for penalty in (28.5, 150.0, 1e308, math.nan):
         with pytest.raises(LookatError, match="length_penalty"):
             lk.lookat_beam_select(st, x, length_penalty=penalty)
+
+
+@pytest.mark.parametrize("kind", ["late", "flat", "spread", "large", "masked", "far", "rising far"])
+def test_beam_select_sums_of_exponentials(kind):
+    """Rows of five batches of logits in one part.  A term at distance d of the reference (at most 1 from the largest) is off by
+    2^-22 (the exponential), 5 * 2^-24 (sixteen terms are added in fp32), 2^-24 d (the exponent's rounding) and 2^-26 d (log2(e)
+    as an fp32 number) of itself; the rest is fp64, and the score is rounded once.
+    late: one logit that holds all the weight, 8 to 17 above what stands in front of it.  flat: one logit, and all others 10 below,
+    which weigh as much together.  masked: the first batches hold the type's lowest value.  far: logits above 2^20, or that get there."""
+    rng = np.random.default_rng(7)
+    G, W, V = 150, 4, 20000
+    x = (rng.standard_normal((G * W, V)) * 2.5).astype(np.float32)
+    if kind == "late":
+        x[np.arange(G * W), rng.integers(4096, V, G * W)] = x[:, :4096].max(axis=1) + rng.uniform(8, 17, G * W).astype(np.float32)
+    if kind == "flat":
+        base = rng.uniform(-3, 3, G * W).astype(np.float32)
+        x[:] = base[:, None]
+        x[np.arange(G * W), rng.integers(0, V, G * W)] = base + np.float32(10)
+    if kind == "large":
+        x = (x + rng.uniform(-1e4, 1e4, (G * W, 1))).astype(np.float32)
+    if kind == "masked":
+        x[:, :9000] = np.finfo(np.float32).min
+    if kind == "far":
+        x = (x * 4 + rng.uniform(2e6, 3e6, (G * W, 1))).astype(np.float32)
+    if kind == "rising far":
+        x[:, 12000:] = (x[:, 12000:] * 4 + np.float32(2e6)).astype(np.float32)
+        x[: G * W // 2, 17000] = np.float32(3e38)
+    st = BeamState.empty(G, W, 0)
+    ids, parents = Lookat(2, 2, 64, 64, 1, 16).lookat_beam_select(st, torch.from_numpy(x).cuda())
+    torch.cuda.synchronize()
+    assert parents.tolist() == [g * W for g in range(G) for _ in range(W)]
+    got, ids = st.scores[:, 0].double().cpu().numpy(), ids.view(G, W)[:, 0].cpu().numpy()
+    y = x[::W].astype(np.float64)
+    d = y.max(axis=1, keepdims=True) - y
+    p = np.exp(-d)
+    total = p.sum(axis=1)
+    want = -np.log(total)
+    assert np.array_equal(ids, y.argmax(axis=1))
+    bound = (10 + 1.25 * ((p * (d + 1)).sum(axis=1) / total)) * 2.0 ** -24 + np.abs(want) * 2.0 ** -24
+    assert (np.abs(got - want) <= bound).all(), (np.abs(got - want) / bound).max()
