@@ -670,6 +670,8 @@ class Lookat:
         dev = self.device
         if q is None and k is None:
             raise ValueError("q and k are both None")
+        if (q is None and q_out is not None) or (k is None and k_out is not None):
+            raise ValueError("a result without its input")
         T = (k if q is None else q).shape[0]
         if table.device != dev:
             raise ValueError(f"the table is on {table.device}, the context on {dev}")
