@@ -41,7 +41,8 @@ typedef enum {
     LOOKAT_ERR_UNSUPPORTED = 2,   /* valid but not implemented for this shape */
     LOOKAT_ERR_CUDA = 3,          /* a CUDA runtime call failed; see lookat_last_error */
     LOOKAT_ERR_NOMEM = 4,         /* scratch allocation failed */
-    LOOKAT_ERR_TIMEOUT = 5        /* a bounded device-side wait expired (reported by the next lookat_attend_prefill) */
+    LOOKAT_ERR_TIMEOUT = 5        /* a bounded device-side wait expired (returned once by the next lookat_attend_prefill, lookat_attend_q8
+                                   * or lookat_attend_packed; until then in lookat_last_error) */
 } lookat_status;
 
 typedef struct {
@@ -317,7 +318,7 @@ lookat_status lookat_probe_read_bandwidth(lookat_ctx *ctx, const void *buf, uint
  * can never be satisfied and gives up after 4096 polls (it ends by itself in
  * microseconds; nothing hangs), raising the context's time-out flag exactly as
  * a prefill kernel would.  After the stream has drained, the next
- * lookat_attend_prefill returns LOOKAT_ERR_TIMEOUT once and clears the flag.
+ * lookat_attend_prefill, lookat_attend_q8 or lookat_attend_packed returns LOOKAT_ERR_TIMEOUT once and clears the flag.
  * The paper has no counterpart.
  */
 lookat_status lookat_selftest_timeout(lookat_ctx *ctx);

@@ -97,7 +97,8 @@ lookat_status lookat_rope(lookat_ctx *ctx, const lookat_rows *q, const lookat_ro
  * infinity among a row's values may reach every query of that row (of other rows never), one among its keys every query that
  * attends it.  out may not overlap q, k or v.
  * Requires 0 <= n_tokens < 2^30 and 1 <= B <= 65535; d_k and d_v multiples of 16 up to 256, else LOOKAT_ERR_UNSUPPORTED.
- * Returns LOOKAT_ERR_TIMEOUT once if an earlier attention kernel of the context gave up a bounded wait (its output is not valid).
+ * Returns LOOKAT_ERR_TIMEOUT once if an earlier attention kernel of the context gave up a bounded wait (its output is not valid);
+ * until a call has returned it, lookat_last_error reports it too, behind the findings above.
  */
 lookat_status lookat_attend_packed(lookat_ctx *ctx, const lookat_rows *q, const lookat_rows *k, const lookat_rows *v, int64_t n_tokens,
                                    int32_t B, const int32_t *starts, const lookat_rows *out);

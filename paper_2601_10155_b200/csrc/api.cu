@@ -352,6 +352,9 @@ const char *lookat_last_error(const lookat_ctx *handle)
         else
             snprintf(ctx->err, sizeof(ctx->err),
                      "debug check: a code >= K was found in a code cache and clamped to K - 1; results computed from it are not valid");
+    } else if (ctx->timeout_flag && *(volatile int *)ctx->timeout_flag && (!ctx->err[0] || ctx->err_read)) {
+        // (the flag stays for the attention call that returns it)
+        snprintf(ctx->err, sizeof(ctx->err), "an earlier attention kernel gave up a bounded barrier wait; its output is not valid");
     }
     ctx->err_read = 1;
     return ctx->err;

@@ -40,6 +40,36 @@ def test_attend_packed_of_values_with_a_common_offset(H, H_kv, d, lens):
             assert bool((err <= bound).all()), f"off by up to {float((err / bound).max()):.4g} of the bound"
 
 
+@pytest.mark.parametrize("d", [64, 32])
+def test_attend_packed_reports_a_time_out_once(d):
+    """The self-test's kernel has one wait that nothing ends and gives up after 4096 polls.  Without another attention call the
+    time-out is in lookat_last_error."""
+    lk = Lookat(2, 1, d, d, 1, 16)
+    q, k, v = (torch.randn(90, h, d, device="cuda").half() for h in (2, 1, 1))
+    starts = i32([0, 40, 90])
+    want = lk.lookat_attend_packed(q, k, v, starts)
+    assert finding(lk) == ""
+    lk._check(lk._lib.lookat_selftest_timeout(lk._h))
+    for _ in range(2):
+        assert "gave up" in finding(lk)
+    with pytest.raises(LookatError, match="gave up") as err:
+        lk.lookat_attend_packed(q, k, v, starts)
+    assert err.value.status == 5
+    got = lk.lookat_attend_packed(q, k, v, starts)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_a_time_out_hides_no_other_finding():
+    lk = Lookat(2, 1, 64, 64, 1, 16)
+    q, k = (torch.randn(90, h, 64, device="cuda").half() for h in (2, 1))
+    with pytest.raises(LookatError, match="B=0"):
+        lk._check(lk._lib.lookat_attend_packed(lk._h, None, None, None, 90, 0, None, None))
+    lk.lookat_attend_packed(q, k, k, i32([0, 100]))
+    lk._check(lk._lib.lookat_selftest_timeout(lk._h))
+    assert "out of range or order" in finding(lk) and "gave up" in finding(lk)
+
+
 # ------------------------------------------------------------------------------------------------ beam selection
 @pytest.mark.parametrize("G,W", [(1, 32), (200, 3), (70, 8)])
 def test_beam_select_logits_that_rise_along_the_row(G, W):
