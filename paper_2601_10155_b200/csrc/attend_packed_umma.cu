@@ -25,6 +25,8 @@
 // free its tensor memory.
 #include <cuda.h>           // CUtensorMap only
 
+#include <atomic>
+
 #include "serve.cuh"
 #include "umma.cuh"
 
@@ -510,18 +512,19 @@ lookat_status launch_pu(Ctx *ctx, const PackedAttendArgs &a)
     auto kern = attend_packed_umma_kernel<DK, DV>;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Lay::kBytes) != cudaSuccess)
         return check_launch(ctx, "attend_packed (tcgen05 form): shared-memory opt-in");
-    // (with fewer registers than it was written for, the split would wait for ever)
-    static const int regs = [&] {
+    // (with fewer registers than it was written for, the split would wait for ever; an answer is kept, a failure to get one is not)
+    static std::atomic<int> regs{0};
+    if (!regs) {
         cudaFuncAttributes attributes;
-        return cudaFuncGetAttributes(&attributes, kern) == cudaSuccess ? attributes.numRegs : 0;
-    }();
-    if (regs < kPuLaunchRegs) return set_error(ctx, LOOKAT_ERR_CUDA, "attend_packed: the kernel was compiled to %d registers, not %d", regs, kPuLaunchRegs);
+        if (cudaFuncGetAttributes(&attributes, kern) == cudaSuccess) regs = attributes.numRegs;
+        else cudaGetLastError();
+    }
+    if (regs < kPuLaunchRegs) return launch_attend_packed_any(ctx, a);
     CUtensorMap k_map, v_map, q_map, out_map;
     int k_order, v_order, q_order = 0, out_order = 0;
     if (!make_rows_map_f16(&k_map, a.k.p, DK, a.H_kv, a.rows.n, a.k.hs, a.k.ts, 1, kPuChunk, &k_order) ||
         !make_rows_map_f16(&v_map, a.v.p, DV, a.H_kv, a.rows.n, a.v.hs, a.v.ts, 1, kPuChunk, &v_order))
         return launch_attend_packed_any(ctx, a);               // (strides that the driver makes no map of)
-    // no more tiles than this, whatever the rows' lengths
     // a tile's lines in one box: g heads of 128 / g tokens, heads innermost
     const bool whole = kPuRows % a.g == 0 &&
                        make_rows_map_f16(&q_map, a.q.p, DK, a.H_q, a.rows.n, a.q.hs, a.q.ts, a.g, kPuRows / a.g, &q_order);
@@ -532,6 +535,7 @@ lookat_status launch_pu(Ctx *ctx, const PackedAttendArgs &a)
                            make_rows_map_f16(&out_map, a.out.p, DV, a.H_q, a.rows.n, a.out.hs, a.out.ts, a.g, 32 / a.g, &out_order);
     const int out_boxes = out_whole && (!out_order || a.g == 1);
     if (!out_boxes) out_map = k_map;
+    // (no more than this, whatever the rows' lengths)
     auto items = [&](int per) { return packed_tiles(a.rows, a.g, per) * a.H_kv; };
     // items of one tile where there is an SM for each (2048 tokens, 8 and 2 heads of 128: 38 us, and 46 with two; 1000 tokens, 32 and 8
     // heads, where there is not, 34 and 32)
