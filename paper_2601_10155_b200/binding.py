@@ -582,6 +582,18 @@ class Lookat:
             _host(out_host, torch.float32, "out_host", (B, c.n_q_heads, c.d_v))))
         return out_host
 
+    def _empty(self, shape, strides, dtype):
+        """A result that the caller did not give.  Its memory comes from the stream that writes it: what another stream had freed
+        may still be in use there.  The caller's stream is recorded, where the result goes next."""
+        dev = self.device
+        if torch._C._cuda_getCurrentRawStream(dev.index) == self._raw_stream:
+            return torch.empty_strided(shape, strides, dtype=dtype, device=dev)            # (takes half the time of empty)
+        caller = torch.cuda.current_stream(dev)
+        with torch.cuda.stream(self.stream):
+            out = torch.empty_strided(shape, strides, dtype=dtype, device=dev)
+        out.record_stream(caller)
+        return out
+
     # -- the 8-bit paged cache (include/lookat_q8.h) --------------------------------
     def _q8(self, cache, tables, seq_lens):
         if cache.heads != self._kv_shape:
@@ -617,10 +629,8 @@ class Lookat:
         dtype = torch.float16 if out_fp16 else torch.float32
         shape = (B, H, d_v) if one else (B, H, L_q, d_v)
         if out is None:
-            n = L_q * d_v                                       # (dense; empty_strided takes half the time of empty)
-            out = torch.empty_strided(shape, (H * d_v, d_v, 1) if one else (H * n, n, d_v, 1), dtype=dtype, device=dev)
-            if torch._C._cuda_getCurrentRawStream(dev.index) != self._raw_stream:
-                out.record_stream(self.stream)                  # allocated for another stream than the one that writes it
+            n = L_q * d_v
+            out = self._empty(shape, (H * d_v, d_v, 1) if one else (H * n, n, d_v, 1), dtype)
             po = out.data_ptr()
         else:
             po = _on(out, dtype, "out", dev, shape)
@@ -657,12 +667,6 @@ class Lookat:
                                                    _on(remap, torch.int32, "remap", self.device, (state.n_pages,))))
 
     # -- what runs around it (include/lookat_serve.h) --------------------------------
-    def _empty(self, shape, strides, dtype):
-        out = torch.empty_strided(shape, strides, dtype=dtype, device=self.device)     # (takes half the time of empty)
-        if torch._C._cuda_getCurrentRawStream(self.device.index) != self._raw_stream:
-            out.record_stream(self.stream)                      # allocated for another stream than the one that writes it
-        return out
-
     def lookat_rope(self, q, k, positions, table, interleaved=False, q_out=None, k_out=None):
         """Rotary positions of q [tokens][H_q][d_k] and k [tokens][H_kv][d_k] (either may be None); new tensors unless results are
         given, which may be q and k themselves."""

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2601_10155_b200.binding import BeamState, Lookat, LookatError
+from paper_2601_10155_b200.binding import BeamState, Lookat, LookatError, PageState, Q8Cache, RopeTable
 from test_gpu_serve import beam_case, check_beams, finding, i32, starts_of
 
 pytestmark = pytest.mark.gpu
@@ -151,3 +151,34 @@ def test_beam_select_sums_of_exponentials(kind):
     assert np.array_equal(ids, y.argmax(axis=1))
     bound = (10 + 1.25 * ((p * (d + 1)).sum(axis=1) / total)) * 2.0 ** -24 + np.abs(want) * 2.0 ** -24
     assert (np.abs(got - want) <= bound).all(), (np.abs(got - want) / bound).max()
+
+
+# ------------------------------------------------------------------------------------------------ results on other streams
+def test_results_do_not_lie_in_memory_that_the_callers_stream_still_writes():
+    """A context on a stream of its own; the caller's stream has freed blocks of just the results' sizes, which work that waits
+    there is still to write."""
+    side = torch.cuda.Stream()
+    T, H, d = 64, 4, 64
+    lk, tb = Lookat(H, H, d, d, 1, 16, stream=side), RopeTable(d)
+    q, k, v = (torch.randn(T, H, d, device="cuda").half() for _ in range(3))
+    pos, starts, logits = torch.arange(T, dtype=torch.int32, device="cuda"), i32([0, 20, T]), torch.randn(6, 50, device="cuda")
+    beams = [BeamState.empty(2, 3, 0) for _ in range(2)]
+    pages, cache = PageState.empty(2, 4, 8, 16), Q8Cache.empty(8, H, 16, d, d)
+    torch.cuda.synchronize()
+    lk.lookat_pages_extend(pages, i32([20, T - 20]), cache.pools())
+    lk.lookat_q8_append_packed(cache, k, v, starts, pages.tables, pages.seq_lens)
+    calls = [lambda: lk.lookat_rope(q, k, pos, tb), lambda: [lk.lookat_attend_packed(q, k, v, starts)],
+             lambda: [lk.lookat_attend_q8(cache, q[:2], pages.tables, pages.seq_lens)]]
+    selects = [lambda st=st: lk.lookat_beam_select(st, logits) for st in beams]
+    for first, again in [(c, c) for c in calls] + [tuple(selects)]:
+        want = first()
+        torch.cuda.synchronize()
+        blocks = [torch.empty_like(x) for x in want for _ in range(8)]
+        torch.cuda.synchronize()
+        torch.cuda._sleep(40_000_000)                           # tens of milliseconds
+        for b in blocks:
+            b.fill_(77)
+        del b, blocks
+        got = again()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
