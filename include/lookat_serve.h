@@ -97,6 +97,8 @@ lookat_status lookat_rope(lookat_ctx *ctx, const lookat_rows *q, const lookat_ro
  * infinity among a row's values may reach every query of that row (of other rows never), one among its keys every query that
  * attends it.  out may not overlap q, k or v.
  * Requires 0 <= n_tokens < 2^30 and 1 <= B <= 65535; d_k and d_v multiples of 16 up to 256, else LOOKAT_ERR_UNSUPPORTED.
+ * The kernel is chosen by the mean length n_tokens / B, empty rows counted: a long row among so many empty ones that a row has no more
+ * than 64 tokens times query heads per KV head on average runs on the kernel for short rows, several times slower.
  * Returns LOOKAT_ERR_TIMEOUT once if an earlier attention kernel of the context gave up a bounded wait (its output is not valid);
  * until a call has returned it, lookat_last_error reports it too, behind the findings above.
  */

@@ -5,7 +5,7 @@
 // weights, fp16 numbers, use fp16's range (up to 2^15), and O in tensor memory is seldom rescaled.
 //
 // A line is one (token, query head) pair of a KV head, line = token * g + head.  An item is two tiles of 128 lines of one row (`per`
-// lines: one tile where there are few items), against chunks of 128 tokens; a persistent CTA per SM goes through every 148th item of the list, which begins with those
+// lines: one tile where there are few items), against chunks of 128 tokens; a persistent CTA per SM goes through every gridDim.x-th item of the list, which begins with those
 // that see the most tokens (packed_tile).  Tensor memory is full: per tile 128 columns of scores, over whose first half the
 // weights are written, and up to 128 of O.  So a tile's products alternate, S, O, S, O, and while the softmax threads work on
 // one tile the tensor pipe works on the other.  With values of 64 dims there is room for the weights of their own (kApart), and a
@@ -553,7 +553,8 @@ bool attend_packed_umma_covers(const Ctx *ctx, const PackedAttendArgs &a)
 {
     // Rows of more than 64 lines (one tile of attend_packed_kernel) on average, as far as the host knows: shorter ones leave most of
     // two tiles of 128 empty.  16384 tokens, 12 heads of 64: rows of 32 tokens 202 us here and 97 there, of 64 109 and 69, of 128 62
-    // and 77; 32 and 8 heads of 128: rows of 16 306 and 259, of 32 160 and 249.
+    // and 77; 32 and 8 heads of 128: rows of 16 306 and 259, of 32 160 and 249.  The average is over all B rows: one of 4096 tokens,
+    // 32 and 8 heads of 128, takes 142 us alone, 149 with 254 empty rows and 654, on the other form, with 255.
     const bool dims = (a.d_k == 64 || a.d_k == 128) && (a.d_v == 64 || a.d_v == 128);
     return dims && (long long)a.rows.n * a.g > 64ll * a.rows.B && ctx->timeout_flag && tile_maps_available();
 }

@@ -12,9 +12,9 @@
 // beams with equal logits and scores get equal ranks, and the lower one goes first.
 // A CTA's candidates find their places by counting those before them.  The last CTA of a group to finish (a counter, no waiting)
 // joins the parts, ranks in fp64, and moves the beams.
-//   32 x 16 beams over 131072 tokens: 71 us (3.8 TB/s: 24 warps an SM, 210 instructions per warp and batch; a batch more on its way
-// changes nothing), histories of 512 tokens 3 us more; 8 x 4 over 50257 tokens 13 us, most of it the chain of dependent steps of
-// a part and of the join.
+//   32 x 16 beams over 131072 tokens: 68 us (3.9 TB/s: 24 of the 32 warps that an SM has room for, on average; 205 instructions per
+// warp and batch; a batch more on its way changes nothing), histories of 512 tokens 5 us more; 64 x 8 over 50257, an odd number, whose
+// rows come by 4-byte copies, 39 us (2.6 TB/s); 8 x 4 13.6 us, most of it the chain of dependent steps of a part and of the join.
 #include "serve.cuh"
 
 namespace lookat {
